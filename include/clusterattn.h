@@ -379,6 +379,139 @@ CA_API int ca_attn_compensated_noalloc(const ca_problem* p, const void* qp, cons
                                        int32_t enable, const int32_t* perm_q, void* out,
                                        float* lse_out, void* stream);
 
+/* ---- Sequence operators ------------------------------------------------------
+ *
+ * What stands around the attention layer of a video, sequence or table model:
+ * rotary positions of several axes, attention with a sliding window and sinks
+ * with its gradients, and a paged key-value cache with the attention of one
+ * new token over it. The conventions above hold (device pointers, the
+ * caller's buffers, validation before anything is enqueued, deterministic
+ * results), with these additions:
+ *
+ * - Tensors of rows of d are given by element strides (the last dimension is
+ *   contiguous): each >= 0 and a multiple of 16 bytes' worth of elements, bases
+ *   16-byte aligned. A stride of 0 repeats an input; rows of an output must not
+ *   overlap (outputs with a stride of 0 over more than one row are refused).
+ * - Query head h of `heads` reads key head h / (heads / heads_k); heads_k
+ *   divides heads.
+ * - Head dimensions: bf16 64 or 128, fp32 any multiple of 4 up to 128 (rotary:
+ *   any multiple of 16 bytes up to 128).
+ * - Every call can be captured into a graph: it allocates nothing, keeps
+ *   nothing from one call for the next and records kernels only. */
+
+/* Rotary positions of up to four axes (time, height, width of a video's
+ * tokens; rows and columns of an image; the place in a text).
+ *
+ * The head's first 2 * npairs dims form npairs = sum of section[] pairs, the
+ * first section[0] pairs belonging to axis 0, the next section[1] to axis 1,
+ * and so on. Pair i turns by t = x * freq[i], x the token's position on the
+ * pair's axis (product, and reduction by multiples of pi/2, in 64 bits):
+ *   (u, w) -> (u cos t - w sin t, u sin t + w cos t)
+ * in fp32, rounded once. Pairs are dims (2 i, 2 i + 1), or with halves != 0
+ * dims (i, i + npairs); the dims from 2 * npairs on are copied. inverse != 0
+ * turns by -t: the transposed map, which takes the gradients of the turned
+ * rows to those of the rows.
+ *
+ * Positions: positions[b pos_stride[0] + a pos_stride[1] + i pos_stride[2]]
+ * for axis a of token i of batch entry b (device int32; any sign; a stride of
+ * 0 repeats). With positions NULL, token i is element i of a row-major grid
+ * grid[0] x .. x grid[axes - 1] (n is at most their product), shifted by
+ * start[]. */
+typedef struct {
+  int32_t batch, heads, heads_k; /* heads_k = 0: no keys (k, k_out NULL); need not divide heads */
+  int32_t n, d, dtype;           /* tokens per head, head dimension, ca_dtype */
+  int32_t axes;                  /* 1..4 */
+  int32_t section[4];            /* pairs per axis, >= 0; 2 * their sum in [2, d] */
+  int32_t halves;                /* halves: npairs a multiple of 16 bytes' worth of elements */
+  int32_t inverse;
+  int32_t grid[4], start[4];     /* positions NULL only */
+  int64_t pos_stride[3];         /* {batch, axis, token}, positions given */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3]; /* {batch, head, token} */
+  double freq[64];               /* radians per position */
+} ca_rope_desc;
+
+/* q_out and k_out may be q and k themselves (with the same strides): the rows
+ * then turn in place. Other overlaps are not allowed. */
+CA_API int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const int32_t* positions,
+                   void* q_out, void* k_out, void* stream);
+
+/* Attention with a sliding window and sinks.
+ *
+ * Query i of batch entry b sits at p = i + len_k[b] - len_q[b] (the last query
+ * beside the last key) and sees key j < len_k[b] where
+ *   (j < sinks  or  p - left <= j <= p + right)  and  (not causal  or  j <= p);
+ * a negative left or right is no limit. len_q, len_k: optional device int32
+ * [batch], clamped to [0, nq] and [0, nk] (NULL: nq, nk).
+ *   out = sum_j e^{s_j - lse} v_j, lse = ln sum_j e^{s_j}, s_j = scale q . k_j
+ * over the keys it sees (scale <= 0 selects 1/sqrt(d)). A query that sees no
+ * key, and every row at or past len_q, has out = 0 and lse = -inf. Rows of k
+ * and v at or past len_k are never read. */
+typedef struct {
+  int32_t batch, heads, heads_k;
+  int32_t nq, nk, d, dtype;      /* 1..2^22 queries and keys */
+  int32_t left, right, sinks, causal;
+  float scale;
+  int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3]; /* {batch, head, token} */
+  /* ca_window_attn_backward only */
+  int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} ca_window;
+
+/* out: strides out_stride; lse: optional dense fp32 [batch][heads][nq]. */
+CA_API int ca_window_attn(const ca_window* p, const void* q, const void* k, const void* v,
+                          const int32_t* len_q, const int32_t* len_k, void* out, float* lse,
+                          void* stream);
+
+/* Bytes of workspace of ca_window_attn_backward (256-byte aligned). Host-only. */
+CA_API int ca_window_workspace_size(const ca_window* p, size_t* bytes);
+
+/* Gradients of ca_window_attn: from out and lse as it wrote them (same
+ * arguments) and dout, with P = e^{s - lse} and D = row sums of dout * out,
+ *   dv = P^T dout,  dS = P (dout v^T - D),  dq = scale dS k,  dk = scale dS^T q,
+ * dk and dv summed over the query heads that share the key head. Rows at or
+ * past the lengths have zero gradients. */
+CA_API int ca_window_attn_backward(const ca_window* p, const void* q, const void* k, const void* v,
+                                   const void* out, const float* lse, const void* dout,
+                                   const int32_t* len_q, const int32_t* len_k, void* dq, void* dk,
+                                   void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* A paged key-value cache: `pages` pages of `page` tokens in two pools, and per
+ * sequence a row of the page table (device int32 [batch][max_pages], rows
+ * table_stride apart): token j of sequence b is token j % page of page
+ * table[b][j / page]. lens: device int32 [batch], tokens of each sequence,
+ * clamped to [0, max_pages * page]. Table entries outside [0, pages) hold no
+ * tokens; entries that no visible token needs are not read. */
+typedef struct {
+  int32_t batch, heads, heads_k, d, dtype;
+  int32_t page, pages, max_pages; /* >= 1; max_pages * page < 2^30 */
+  int32_t left, sinks;            /* ca_paged_attn: as in ca_window, negative left: the whole cache */
+  float scale;
+  int64_t table_stride;
+  int64_t k_stride[3], v_stride[3]; /* pools: {page, token, head} */
+  int64_t q_stride[2], out_stride[2];         /* ca_paged_attn: {batch, head} */
+  int32_t n_new;                              /* ca_cache_append: new tokens per sequence */
+  int64_t k_new_stride[3], v_new_stride[3];   /* ca_cache_append: {batch, token, head} */
+} ca_paged;
+
+/* Writes n_new new keys and values of each sequence at its places lens[b] -
+ * n_new .. lens[b] - 1 (lens counts them already; places before 0, past the
+ * table or on pages outside the pool are left out). Everything else in the
+ * pools stays as it is. Sequences must not write the same place of a page. */
+CA_API int ca_cache_append(const ca_paged* p, const void* k, const void* v, void* k_pages,
+                           void* v_pages, const int32_t* table, const int32_t* lens, void* stream);
+
+/* Bytes of workspace of ca_paged_attn (256-byte aligned; may be 0). Host-only. */
+CA_API int ca_paged_workspace_size(const ca_paged* p, size_t* bytes);
+
+/* Attention of one query per sequence and head, its last token (position
+ * lens[b] - 1), over the sequence's cache: the keys j with j < sinks or
+ * j >= lens[b] - 1 - left. Keys that it does not see are not read, so pages that
+ * hold no visible token may be gone. A sequence that sees no key has out = 0,
+ * lse = -inf. q, out: q_stride, out_stride; lse: optional dense fp32
+ * [batch][heads]. */
+CA_API int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages,
+                         const void* v_pages, const int32_t* table, const int32_t* lens, void* out,
+                         float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,7 +6,9 @@ C-ABI calls (see include/clusterattn.h):
 
     cluster -> select -> block_sparse_attn -> compensate
 
-``forward`` chains them for one attention layer. There is no CPU fallback: if
+``forward`` chains them for one attention layer. The operators around such a
+layer (rotary positions, window attention with its gradients, the paged cache)
+are in ``sequence`` and exported here too. There is no CPU fallback: if
 the library is not built, importing the calls raises.
 """
 from __future__ import annotations
@@ -20,10 +22,13 @@ from . import _lib
 from ._lib import (CA_BF16, CA_F32, CA_LAYOUT_BHND, CA_LAYOUT_BNHD, CA_LAYOUT_STRIDED,
                    CA_SPLIT_BASIC, CA_SPLIT_DIAG, CA_XF_ADAPTIVE, CA_XF_METRIC, CA_XF_NONE,
                    CA_XF_PCA, CA_XF_RANDOM, CAError)
+from .sequence import (Rope, Window, cache_append, paged_attn, rope, rope_axes, window_attn,
+                       window_attn_backward)
 
 __all__ = ["Problem", "bhnd_strides", "workspace_size", "cluster", "select", "select_hist", "block_sparse_attn",
            "compensate", "attn_compensated", "attn_compensated_noalloc", "check_finite",
-           "forward", "CAError", "abi_version"]
+           "forward", "CAError", "abi_version", "Rope", "rope_axes", "rope", "Window",
+           "window_attn", "window_attn_backward", "cache_append", "paged_attn"]
 
 _XF = {"none": CA_XF_NONE, "pca": CA_XF_PCA, "metric": CA_XF_METRIC, "adaptive": CA_XF_ADAPTIVE,
        "random": CA_XF_RANDOM}
@@ -297,7 +302,8 @@ def keep_to_k(keep: float, n_kc: int) -> int:
 
 def forward(q, k, v, cq=128, ck=None, keep=None, keep_k=None, transform="metric",
             compensation=True, scale=None, layout="bhnd", return_parts=False, select="topk",
-            mass_recall=0.9, min_count=16, one_pass=True, checked=False):
+            mass_recall=0.9, min_count=16, one_pass=True, checked=False, rotary=None,
+            rope_grid=None, rope_positions=None):
     """ClusterAttention for one layer. q, k, v: [B,H,N,d] ("bhnd") or [B,N,H,d]
     ("bnhd"), bf16 or fp32, on one GPU; with layout="strided", any [B,H,N,d]
     views whose last dimension is contiguous (for instance slices of a fused
@@ -312,8 +318,13 @@ def forward(q, k, v, cq=128, ck=None, keep=None, keep_k=None, transform="metric"
     pass (attn_compensated) unless one_pass is False or return_parts asks for
     the sparse part's output and lse. checked=True first runs the checked
     mode (check_finite), which synchronises and raises CAError with
-    CA_E_NONFINITE on NaN or Inf inputs."""
+    CA_E_NONFINITE on NaN or Inf inputs. rotary: a Rope that turns queries and
+    keys first (into new tensors), by the tokens' places in rope_grid (a video's
+    frames, rows, columns) or by rope_positions, as in rope(); queries and keys
+    then have as many tokens each."""
     ck = cq if ck is None else ck
+    if rotary is not None:
+        q, k = rope(rotary, q, k, grid=rope_grid, positions=rope_positions, layout=layout)
     if layout in ("bhnd", "strided"):
         B, H, nq, d = q.shape
         nk = k.shape[2]

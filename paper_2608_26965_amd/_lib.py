@@ -26,6 +26,13 @@ EXPORTS = (
     "ca_attn_compensated",
     "ca_attn_compensated_noalloc",
     "ca_check_finite",
+    "ca_rope",
+    "ca_window_attn",
+    "ca_window_workspace_size",
+    "ca_window_attn_backward",
+    "ca_cache_append",
+    "ca_paged_workspace_size",
+    "ca_paged_attn",
 )
 
 _i32 = ctypes.c_int32
@@ -43,6 +50,34 @@ class CaClusterOut(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("perm_q", "perm_k", "cid_q", "cid_k", "count_q", "count_k",
                                    "cent_q", "cent_k", "cent_v", "qp", "kp", "vp", "yq_dbg",
                                    "yk_dbg")]
+
+
+class CaRope(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("batch", "heads", "heads_k", "n", "d", "dtype", "axes")]
+                + [("section", _i32 * 4), ("halves", _i32), ("inverse", _i32), ("grid", _i32 * 4),
+                   ("start", _i32 * 4)]
+                + [(n, ctypes.c_int64 * 3) for n in ("pos_stride", "q_stride", "k_stride",
+                                                     "q_out_stride", "k_out_stride")]
+                + [("freq", ctypes.c_double * 64)])
+
+
+class CaWindow(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("batch", "heads", "heads_k", "nq", "nk", "d", "dtype", "left",
+                                     "right", "sinks", "causal")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride",
+                                                     "out_stride", "dout_stride", "dq_stride",
+                                                     "dk_stride", "dv_stride")])
+
+
+class CaPaged(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("batch", "heads", "heads_k", "d", "dtype", "page", "pages",
+                                     "max_pages", "left", "sinks")]
+                + [("scale", ctypes.c_float), ("table_stride", ctypes.c_int64),
+                   ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+                   ("q_stride", ctypes.c_int64 * 2), ("out_stride", ctypes.c_int64 * 2),
+                   ("n_new", _i32), ("k_new_stride", ctypes.c_int64 * 3),
+                   ("v_new_stride", ctypes.c_int64 * 3)])
 
 
 class CAError(RuntimeError):
@@ -96,6 +131,17 @@ def load() -> ctypes.CDLL:
                                                 ctypes.c_float, _i32, _vp, _vp, _vp, _vp]
     lib.ca_check_finite.restype = ctypes.c_int
     lib.ca_check_finite.argtypes = [P, _vp, _vp, _vp, _vp, _vp]
+    size = ctypes.POINTER(ctypes.c_size_t)
+    lib.ca_rope.argtypes = [ctypes.POINTER(CaRope)] + [_vp] * 6
+    lib.ca_window_attn.argtypes = [ctypes.POINTER(CaWindow)] + [_vp] * 8
+    lib.ca_window_workspace_size.argtypes = [ctypes.POINTER(CaWindow), size]
+    lib.ca_window_attn_backward.argtypes = ([ctypes.POINTER(CaWindow)] + [_vp] * 12
+                                            + [ctypes.c_size_t, _vp])
+    lib.ca_cache_append.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 7
+    lib.ca_paged_workspace_size.argtypes = [ctypes.POINTER(CaPaged), size]
+    lib.ca_paged_attn.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
+    for name in EXPORTS[-7:]:
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 

@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "seq.h"
 
 // Device memory of ca_attn_compensated_noalloc: the staged centroid tiles and
 // the launch schedule. Every device the library runs on holds its own copy,
@@ -173,6 +174,162 @@ int check_attn_shape(const ca::Prob& P) {
   } else if (P.d % 4 != 0) {
     return fail(CA_E_UNSUPPORTED, "fp32 attention needs d %% 4 == 0, got %d", P.d);
   }
+  return CA_OK;
+}
+
+// ---- the sequence operators' checks -----------------------------------------
+
+int check_dtype(int dtype) {
+  if (dtype != CA_F32 && dtype != CA_BF16) return fail(CA_E_INVALID, "unknown dtype");
+  return CA_OK;
+}
+
+int check_strides(const int64_t* st, int n, int dtype, const char* name) {
+  const int64_t unit = dtype == CA_BF16 ? 8 : 4;
+  for (int j = 0; j < n; ++j)
+    if (st[j] < 0 || st[j] % unit != 0)
+      return fail(CA_E_INVALID,
+                  "%s_stride[%d] = %lld: strides must be >= 0 and multiples of %lld elements", name,
+                  j, (long long)st[j], (long long)unit);
+  return CA_OK;
+}
+
+// an output's rows must have places of their own
+int check_written(const int64_t* st, int s0, int s1, int s2, const char* name) {
+  const int size[3] = {s0, s1, s2};
+  for (int j = 0; j < 3; ++j)
+    if (size[j] > 1 && st[j] == 0)
+      return fail(CA_E_INVALID, "%s_stride[%d] is 0: the rows of an output would overlap", name, j);
+  return CA_OK;
+}
+
+int check_base(const void* x, const char* name) {
+  if (!x) return fail(CA_E_INVALID, "%s is NULL", name);
+  if ((uintptr_t)x & 15u) return fail(CA_E_INVALID, "%s must be 16-byte aligned", name);
+  return CA_OK;
+}
+
+ca::Lay lay(const int64_t* st, int H) { return ca::Lay{st[0], st[1], st[2], H}; }
+
+int check_head_dim(int d, int dtype) {
+  if (d < 1 || d > ca::kMaxD) return fail(CA_E_INVALID, "d must be in [1, %d]", ca::kMaxD);
+  if (dtype == CA_BF16 && d != 64 && d != 128)
+    return fail(CA_E_UNSUPPORTED, "bf16 attention needs d in {64, 128}, got %d", d);
+  if (dtype == CA_F32 && d % 4 != 0)
+    return fail(CA_E_UNSUPPORTED, "fp32 attention needs d %% 4 == 0, got %d", d);
+  return CA_OK;
+}
+
+int check_heads(int batch, int heads, int heads_k) {
+  if (batch < 1 || heads < 1 || heads_k < 1)
+    return fail(CA_E_INVALID, "batch, heads and heads_k must be >= 1");
+  if (heads % heads_k != 0)
+    return fail(CA_E_INVALID, "heads = %d is not a multiple of heads_k = %d", heads, heads_k);
+  if ((int64_t)batch * heads > 65535)
+    return fail(CA_E_UNSUPPORTED, "batch * heads above 65535");
+  return CA_OK;
+}
+
+// scale <= 0 (or NaN) selects 1 / sqrt(d)
+float scale_of(float scale, int d) { return scale > 0.0f ? scale : 1.0f / sqrtf((float)d); }
+
+int check_window(const ca_window* p, ca::WinProb* P) {
+  if (!p) return fail(CA_E_INVALID, "window is NULL");
+  int s;
+  if ((s = check_heads(p->batch, p->heads, p->heads_k)) || (s = check_dtype(p->dtype)) ||
+      (s = check_head_dim(p->d, p->dtype)))
+    return s;
+  if (p->nq < 1 || p->nk < 1 || p->nq > (1 << 22) || p->nk > (1 << 22))
+    return fail(CA_E_INVALID, "nq and nk must be in [1, 2^22]");
+  if (p->sinks < 0) return fail(CA_E_INVALID, "sinks = %d must be >= 0", p->sinks);
+  if ((s = check_strides(p->q_stride, 3, p->dtype, "q")) ||
+      (s = check_strides(p->k_stride, 3, p->dtype, "k")) ||
+      (s = check_strides(p->v_stride, 3, p->dtype, "v")) ||
+      (s = check_strides(p->out_stride, 3, p->dtype, "out")))
+    return s;
+  auto side = [](int x) { return x < 0 || x > ca::kUnlimited ? ca::kUnlimited : x; };
+  P->B = p->batch;
+  P->H = p->heads;
+  P->Hk = p->heads_k;
+  P->G = p->heads / p->heads_k;
+  P->nq = p->nq;
+  P->nk = p->nk;
+  P->d = p->d;
+  P->dtype = p->dtype;
+  P->m = ca::WinMask{side(p->left), side(p->right), p->sinks, p->causal != 0};
+  P->scale = scale_of(p->scale, p->d);
+  P->lq = lay(p->q_stride, p->heads);
+  P->lk = lay(p->k_stride, p->heads_k);
+  P->lv = lay(p->v_stride, p->heads_k);
+  P->lo = lay(p->out_stride, p->heads);
+  P->ldo = lay(p->dout_stride, p->heads);
+  P->ldq = lay(p->dq_stride, p->heads);
+  P->ldk = lay(p->dk_stride, p->heads_k);
+  P->ldv = lay(p->dv_stride, p->heads_k);
+  P->len_q = P->len_k = nullptr;
+  return CA_OK;
+}
+
+// what ca_cache_append and ca_paged_attn share
+int check_paged(const ca_paged* p, ca::PagedProb* P) {
+  if (!p) return fail(CA_E_INVALID, "paged is NULL");
+  int s;
+  if ((s = check_heads(p->batch, p->heads, p->heads_k)) || (s = check_dtype(p->dtype)) ||
+      (s = check_head_dim(p->d, p->dtype)))
+    return s;
+  if (p->page < 1 || p->pages < 1 || p->max_pages < 1)
+    return fail(CA_E_INVALID, "page, pages and max_pages must be >= 1");
+  if ((int64_t)p->page * p->max_pages >= (1 << 30))
+    return fail(CA_E_UNSUPPORTED, "max_pages * page must be below 2^30");
+  if (p->table_stride < 0) return fail(CA_E_INVALID, "table_stride must be >= 0");
+  if ((s = check_strides(p->k_stride, 3, p->dtype, "k")) ||
+      (s = check_strides(p->v_stride, 3, p->dtype, "v")))
+    return s;
+  P->B = p->batch;
+  P->H = p->heads;
+  P->Hk = p->heads_k;
+  P->G = p->heads / p->heads_k;
+  P->d = p->d;
+  P->dtype = p->dtype;
+  P->page = p->page;
+  P->pages = p->pages;
+  P->max_pages = p->max_pages;
+  P->left = p->left < 0 || p->left > ca::kNoWindow ? ca::kNoWindow : p->left;
+  P->sinks = p->sinks;
+  P->scale = scale_of(p->scale, p->d);
+  P->table = P->lens = nullptr;
+  P->table_sb = p->table_stride;
+  P->q_sb = p->q_stride[0];
+  P->q_sh = p->q_stride[1];
+  P->o_sb = p->out_stride[0];
+  P->o_sh = p->out_stride[1];
+  P->k_sp = p->k_stride[0];
+  P->k_st = p->k_stride[1];
+  P->k_sh = p->k_stride[2];
+  P->v_sp = p->v_stride[0];
+  P->v_st = p->v_stride[1];
+  P->v_sh = p->v_stride[2];
+  return CA_OK;
+}
+
+int check_paged_attn(const ca_paged* p, ca::PagedProb* P) {
+  int s = check_paged(p, P);
+  if (s) return s;
+  if (p->sinks < 0) return fail(CA_E_INVALID, "sinks = %d must be >= 0", p->sinks);
+  if ((s = check_strides(p->q_stride, 2, p->dtype, "q")) ||
+      (s = check_strides(p->out_stride, 2, p->dtype, "out")))
+    return s;
+  if ((p->batch > 1 && p->out_stride[0] == 0) || (p->heads > 1 && p->out_stride[1] == 0))
+    return fail(CA_E_INVALID, "out_stride is 0: the rows of an output would overlap");
+  return CA_OK;
+}
+
+int check_bytes(size_t need, const void* ws, size_t ws_bytes) {
+  if (ws_bytes < need)
+    return fail(CA_E_WORKSPACE, "workspace of %zu bytes, need %zu", ws_bytes, need);
+  if (need > 0 && !ws) return fail(CA_E_INVALID, "workspace is NULL");
+  if (need > 0 && ((uintptr_t)ws & 255u) != 0)
+    return fail(CA_E_INVALID, "workspace must be 256-byte aligned");
   return CA_OK;
 }
 
@@ -497,6 +654,190 @@ int ca_check_finite(const ca_problem* p, const void* q, const void* k, const voi
     return s;
   return device_status(ca::launch_check_finite(P, q, k, v, flags, (hipStream_t)stream),
                        "ca_check_finite");
+}
+
+int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const int32_t* positions,
+            void* q_out, void* k_out, void* stream) {
+  if (!p) return fail(CA_E_INVALID, "rope is NULL");
+  int s;
+  if ((s = check_dtype(p->dtype))) return s;
+  if (p->batch < 1 || p->heads < 1 || p->heads_k < 0 || p->n < 1)
+    return fail(CA_E_INVALID, "batch, heads and n must be >= 1, heads_k >= 0");
+  if ((int64_t)p->heads + p->heads_k > 65535)
+    return fail(CA_E_UNSUPPORTED, "heads + heads_k above 65535");
+  const int unit = p->dtype == CA_BF16 ? 8 : 4;
+  if (p->d < 1 || p->d > ca::kMaxD) return fail(CA_E_INVALID, "d must be in [1, %d]", ca::kMaxD);
+  if (p->d % unit != 0)
+    return fail(CA_E_UNSUPPORTED, "rotary positions need d a multiple of %d, got %d", unit, p->d);
+  if ((int64_t)p->batch * p->n * (p->d / unit) >= ((int64_t)1 << 31))
+    return fail(CA_E_UNSUPPORTED, "batch * n * d too large");
+  if (p->axes < 1 || p->axes > ca::kMaxAxes)
+    return fail(CA_E_INVALID, "axes must be in [1, %d]", ca::kMaxAxes);
+  ca::RopeProb P;
+  P.npairs = 0;
+  int64_t cells = 1;
+  for (int a = 0; a < ca::kMaxAxes; ++a) {
+    const int n = a < p->axes ? p->section[a] : 0;
+    if (n < 0 || n > p->d) return fail(CA_E_INVALID, "section[%d] = %d", a, n);
+    P.npairs += n;
+    P.end[a] = P.npairs;
+    P.grid[a] = 1;
+    P.start[a] = 0;
+    if (!positions && a < p->axes) {
+      if (p->grid[a] < 1) return fail(CA_E_INVALID, "grid[%d] = %d must be >= 1", a, p->grid[a]);
+      P.grid[a] = p->grid[a];
+      P.start[a] = p->start[a];
+      if ((int64_t)p->start[a] + p->grid[a] > INT32_MAX)
+        return fail(CA_E_INVALID, "start[%d] + grid[%d] leaves 32 bits", a, a);
+      if (cells < p->n) cells *= p->grid[a];
+    }
+  }
+  if (P.npairs < 1 || 2 * P.npairs > p->d)
+    return fail(CA_E_INVALID, "2 * (sum of section) = %d must be in [2, d = %d]", 2 * P.npairs, p->d);
+  if (p->halves && P.npairs % unit != 0)
+    return fail(CA_E_UNSUPPORTED, "halves need a multiple of %d pairs, got %d", unit, P.npairs);
+  if (!positions && cells < p->n)
+    return fail(CA_E_INVALID, "the grid holds %lld tokens, fewer than n = %d", (long long)cells, p->n);
+  for (int i = 0; i < P.npairs; ++i) {
+    if (!isfinite(p->freq[i])) return fail(CA_E_INVALID, "freq[%d] is not finite", i);
+    P.freq[i] = p->freq[i];
+  }
+  for (int i = P.npairs; i < ca::kMaxD / 2; ++i) P.freq[i] = 0.0;
+  if ((s = check_base(q, "q")) || (s = check_base(q_out, "q_out")) ||
+      (s = check_strides(p->q_stride, 3, p->dtype, "q")) ||
+      (s = check_strides(p->q_out_stride, 3, p->dtype, "q_out")) ||
+      (s = check_written(p->q_out_stride, p->batch, p->heads, p->n, "q_out")))
+    return s;
+  if (p->heads_k > 0) {
+    if ((s = check_base(k, "k")) || (s = check_base(k_out, "k_out")) ||
+        (s = check_strides(p->k_stride, 3, p->dtype, "k")) ||
+        (s = check_strides(p->k_out_stride, 3, p->dtype, "k_out")) ||
+        (s = check_written(p->k_out_stride, p->batch, p->heads_k, p->n, "k_out")))
+      return s;
+  }
+  P.B = p->batch;
+  P.H = p->heads;
+  P.Hk = p->heads_k;
+  P.n = p->n;
+  P.d = p->d;
+  P.dtype = p->dtype;
+  P.axes = p->axes;
+  P.halves = p->halves != 0;
+  P.sign = p->inverse ? -1.f : 1.f;
+  P.pos = positions;
+  P.pos_sb = p->pos_stride[0];
+  P.pos_sa = p->pos_stride[1];
+  P.pos_sn = p->pos_stride[2];
+  P.lq = lay(p->q_stride, P.H);
+  P.lk = lay(p->k_stride, P.Hk);
+  P.lqo = lay(p->q_out_stride, P.H);
+  P.lko = lay(p->k_out_stride, P.Hk);
+  return device_status(ca::launch_rope(P, q, k, q_out, k_out, (hipStream_t)stream), "ca_rope");
+}
+
+int ca_window_attn(const ca_window* p, const void* q, const void* k, const void* v,
+                   const int32_t* len_q, const int32_t* len_k, void* out, float* lse,
+                   void* stream) {
+  ca::WinProb P;
+  int s = check_window(p, &P);
+  if (s) return s;
+  if ((s = check_base(q, "q")) || (s = check_base(k, "k")) || (s = check_base(v, "v")) ||
+      (s = check_base(out, "out")) ||
+      (s = check_written(p->out_stride, p->batch, p->heads, p->nq, "out")))
+    return s;
+  P.len_q = len_q;
+  P.len_k = len_k;
+  return device_status(ca::launch_window(P, q, k, v, out, lse, (hipStream_t)stream),
+                       "ca_window_attn");
+}
+
+int ca_window_workspace_size(const ca_window* p, size_t* bytes) {
+  ca::WinProb P;
+  int s = check_window(p, &P);
+  if (s) return s;
+  if (!bytes) return fail(CA_E_INVALID, "bytes is NULL");
+  *bytes = ca::window_backward_bytes(P);
+  return ok();
+}
+
+int ca_window_attn_backward(const ca_window* p, const void* q, const void* k, const void* v,
+                            const void* out, const float* lse, const void* dout,
+                            const int32_t* len_q, const int32_t* len_k, void* dq, void* dk,
+                            void* dv, void* ws, size_t ws_bytes, void* stream) {
+  ca::WinProb P;
+  int s = check_window(p, &P);
+  if (s) return s;
+  if (!lse) return fail(CA_E_INVALID, "lse is NULL");
+  if ((s = check_base(q, "q")) || (s = check_base(k, "k")) || (s = check_base(v, "v")) ||
+      (s = check_base(out, "out")) || (s = check_base(dout, "dout")) ||
+      (s = check_base(dq, "dq")) || (s = check_base(dk, "dk")) || (s = check_base(dv, "dv")))
+    return s;
+  if ((s = check_strides(p->dout_stride, 3, p->dtype, "dout")) ||
+      (s = check_strides(p->dq_stride, 3, p->dtype, "dq")) ||
+      (s = check_strides(p->dk_stride, 3, p->dtype, "dk")) ||
+      (s = check_strides(p->dv_stride, 3, p->dtype, "dv")) ||
+      (s = check_written(p->dq_stride, p->batch, p->heads, p->nq, "dq")) ||
+      (s = check_written(p->dk_stride, p->batch, p->heads_k, p->nk, "dk")) ||
+      (s = check_written(p->dv_stride, p->batch, p->heads_k, p->nk, "dv")))
+    return s;
+  if ((s = check_bytes(ca::window_backward_bytes(P), ws, ws_bytes))) return s;
+  P.len_q = len_q;
+  P.len_k = len_k;
+  return device_status(ca::launch_window_backward(P, q, k, v, out, lse, dout, dq, dk, dv, (char*)ws,
+                                                  (hipStream_t)stream),
+                       "ca_window_attn_backward");
+}
+
+int ca_cache_append(const ca_paged* p, const void* k, const void* v, void* k_pages, void* v_pages,
+                    const int32_t* table, const int32_t* lens, void* stream) {
+  ca::PagedProb P;
+  int s = check_paged(p, &P);
+  if (s) return s;
+  if (p->n_new < 1) return fail(CA_E_INVALID, "n_new = %d must be >= 1", p->n_new);
+  if ((int64_t)p->batch * p->n_new * p->heads_k * (p->d / 4) >= ((int64_t)1 << 31))
+    return fail(CA_E_UNSUPPORTED, "batch * n_new * heads_k * d too large");
+  if (!table || !lens) return fail(CA_E_INVALID, "table and lens are required");
+  if ((s = check_base(k, "k")) || (s = check_base(v, "v")) || (s = check_base(k_pages, "k_pages")) ||
+      (s = check_base(v_pages, "v_pages")) ||
+      (s = check_strides(p->k_new_stride, 3, p->dtype, "k_new")) ||
+      (s = check_strides(p->v_new_stride, 3, p->dtype, "v_new")) ||
+      (s = check_written(p->k_stride, p->pages, p->page, p->heads_k, "k")) ||
+      (s = check_written(p->v_stride, p->pages, p->page, p->heads_k, "v")))
+    return s;
+  P.table = table;
+  P.lens = lens;
+  const ca::AppendProb A{p->n_new,
+                         p->k_new_stride[0], p->k_new_stride[1], p->k_new_stride[2],
+                         p->v_new_stride[0], p->v_new_stride[1], p->v_new_stride[2]};
+  return device_status(ca::launch_append(P, A, k, v, k_pages, v_pages, (hipStream_t)stream),
+                       "ca_cache_append");
+}
+
+int ca_paged_workspace_size(const ca_paged* p, size_t* bytes) {
+  ca::PagedProb P;
+  int s = check_paged_attn(p, &P);
+  if (s) return s;
+  if (!bytes) return fail(CA_E_INVALID, "bytes is NULL");
+  *bytes = ca::paged_bytes(P);
+  return ok();
+}
+
+int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages, const void* v_pages,
+                  const int32_t* table, const int32_t* lens, void* out, float* lse, void* ws,
+                  size_t ws_bytes, void* stream) {
+  ca::PagedProb P;
+  int s = check_paged_attn(p, &P);
+  if (s) return s;
+  if (!table || !lens) return fail(CA_E_INVALID, "table and lens are required");
+  if ((s = check_base(q, "q")) || (s = check_base(k_pages, "k_pages")) ||
+      (s = check_base(v_pages, "v_pages")) || (s = check_base(out, "out")))
+    return s;
+  if ((s = check_bytes(ca::paged_bytes(P), ws, ws_bytes))) return s;
+  P.table = table;
+  P.lens = lens;
+  return device_status(ca::launch_paged(P, q, k_pages, v_pages, out, lse, (char*)ws,
+                                        (hipStream_t)stream),
+                       "ca_paged_attn");
 }
 
 }  // extern "C"

@@ -1,0 +1,612 @@
+"""Parity of the sequence operators (rotary positions, window attention and its
+gradients, the paged cache and its attention) with the fp64 oracle, at the
+sizes and masks where they can go wrong.
+
+Tolerances are bounds on the kernels' roundings, element by element. u = 2^-8
+(bf16) or 2^-24 (fp32) is half a step. A logit is off by at most es =
+(d + 8) 2^-24 scale |q|.|k| (fp32 sums), a probability by a factor 1 +- w with
+w = 2 es + 2^-20 (exponential, sum over the keys in fp32) and, where it is
+rounded for the matrix cores, 1 +- 2^-8; the output is rounded once:
+    |out| off by u |out| + (r + w) sum P |v|,  r = 2^-8 in bf16, else 0.
+Gradients alike: dS is rounded for the products (r), and D = dout . out comes
+from the rounded output, off by Ed = |dout| . |out's error|."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import seq
+
+pytestmark = pytest.mark.gpu
+
+DT = ["bf16", "f32"]
+
+
+def _ca():
+    import paper_2608_26965_amd as ca
+    return ca
+
+
+def _torch(dt):
+    import torch
+    return torch.bfloat16 if dt == "bf16" else torch.float32
+
+
+def _u(dt):
+    return 2.0 ** -8 if dt == "bf16" else 2.0 ** -24
+
+
+def _rand(g, shape, dt, scale=1.0):
+    import torch
+    return (torch.randn(*shape, generator=g) * scale).to(_torch(dt))
+
+
+def _gen(seed):
+    import torch
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _bounds(q, k, v, do, see, scale, dt):
+    """Oracle results and the bounds of one head."""
+    u, r = _u(dt), 2.0 ** -8 if dt == "bf16" else 0.0
+    o, lse, P = seq.attend(q, k, v, see, scale)
+    es = (q.shape[1] + 8) * 2.0 ** -24 * scale * (np.abs(q) @ np.abs(k).T).max(initial=0.0)
+    w = 2 * es + 2.0 ** -20
+    A = P @ np.abs(v)
+    res = {"out": (o, u * np.abs(o) + (r + w) * A), "lse": (lse, 2 * w + 2.0 ** -23 * np.abs(lse))}
+    if do is not None:
+        dq, dk, dv = seq.attend_backward(q, k, v, do, see, scale)
+        Ed = (np.abs(do) * res["out"][1]).sum(1, keepdims=True)
+        dP = do @ v.T
+        D = (do * o).sum(1, keepdims=True)
+        mag = np.abs(do) @ np.abs(v).T + (np.abs(do) * np.abs(o)).sum(1, keepdims=True)
+        dS = np.abs(P * (dP - D))
+        eS = scale * (r * dS + P * (Ed + (w + 130 * 2.0 ** -24) * mag) + w * dS)
+        res["dq"] = (dq, u * np.abs(dq) + eS @ np.abs(k))
+        res["dk"] = (dk, u * np.abs(dk) + eS.T @ np.abs(q))
+        res["dv"] = (dv, u * np.abs(dv) + (r + w) * (P.T @ np.abs(do)))
+    return res
+
+
+def _close(got, want, tol, what):
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), what
+    got, want, tol = got[~inf], want[~inf], tol[~inf]
+    bad = ~(np.abs(got - want) <= tol + 1e-30)
+    assert not bad.any(), (f"{what}: {bad.sum()} of {bad.size} off, worst "
+                           f"{(np.abs(got - want) / (tol + 1e-30)).max():.2f} times the bound")
+
+
+# ---- rotary positions -----------------------------------------------------------------
+
+def _rope_case(dt, B, H, Hk, n, d, dims, pairing, layout, grid, far, inverse, shared=False, seed=0):
+    import torch
+    ca = _ca()
+    r = ca.rope_axes(dims, base=10000.0, pairing=pairing, shared=shared)
+    g = _gen(seed)
+    shape = (lambda h: (B, h, n, d)) if layout == "bhnd" else (lambda h: (B, n, h, d))
+    q, k = _rand(g, shape(H), dt), _rand(g, shape(Hk), dt)
+    kw = {}
+    if grid:
+        kw["grid"] = grid
+        pos = np.broadcast_to(seq.grid_positions(n, grid), (B, len(grid), n))
+    else:
+        p = torch.randint(-far, far, (B, len(dims), n), generator=g, dtype=torch.int32)
+        kw["positions"] = p.cuda()
+        pos = p.numpy()
+    qo, ko = ca.rope(r, q.cuda(), k.cuda(), inverse=inverse, layout=layout, **kw)
+    for x, y in ((q, qo), (k, ko)):
+        assert y.shape == x.shape and y.dtype == x.dtype
+        a, b = (_np(t if layout == "bhnd" else t.transpose(1, 2)) for t in (x, y))
+        for bi in range(B):
+            for h in range(a.shape[1]):
+                want = seq.rope(a[bi, h], pos[bi], r.sections, r.freqs, pairing, inverse)
+                # sine and cosine to 2^-22, two products and a sum in fp32
+                m = sum(r.sections)
+                mag = np.abs(a[bi, h]).copy()
+                i = np.arange(m)
+                e, f = (i, i + m) if pairing == "halves" else (2 * i, 2 * i + 1)
+                mag[:, e] = mag[:, f] = np.abs(a[bi, h][:, e]) + np.abs(a[bi, h][:, f])
+                _close(b[bi, h], want, _u(dt) * np.abs(want) + 2.0 ** -21 * mag, f"batch {bi} head {h}")
+                assert np.array_equal(b[bi, h][:, 2 * m:], a[bi, h][:, 2 * m:])
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("pairing,dims", [("interleaved", (44, 42, 42)), ("halves", (64, 32, 32)), ("halves", (64,)),
+                                          ("interleaved", (2, 0, 4, 10)), ("interleaved", (6,))])
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+def test_rope_grid(dt, pairing, dims, layout):
+    grid = {1: (37,), 3: (3, 4, 5), 4: (2, 1, 5, 6)}[len(dims)]
+    _rope_case(dt, 2, 3, 1, 37, 128, dims, pairing, layout, grid, 0, False)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("pairing", ["interleaved", "halves"])
+@pytest.mark.parametrize("B,n,far,inverse", [(1, 1, 100, False), (3, 1, 1 << 20, True), (2, 257, 1 << 20, False),
+                                             (2, 5, (1 << 31) - 1, False)])
+def test_rope_positions(dt, pairing, B, n, far, inverse):
+    # at 2^31 the 64-bit product is off by 2^-53 2^31 = 2.4e-7 of a radian: within 2^-21
+    _rope_case(dt, B, 5, 2, n, 64, (16, 24, 24), pairing, "bhnd", None, far, inverse, shared=True, seed=n)
+
+
+@pytest.mark.parametrize("d", [8, 40, 96, 120])
+def test_rope_head_dims(d):
+    _rope_case("bf16", 1, 2, 2, 19, d, (d // 2 // 2 * 2,), "interleaved", "bnhd", (19,), 0, False)
+    _rope_case("f32", 1, 2, 2, 19, d, (d // 8 * 8,), "halves", "bnhd", None, 1000, True)
+
+
+def test_rope_in_place_strided_and_back():
+    """Slices of a fused projection turned in place: what lies between them
+    stays; turning back restores the rows to rounding; q alone; start."""
+    import torch
+    ca = _ca()
+    g = _gen(5)
+    r = ca.rope_axes((32, 16, 16))
+    qkv = _rand(g, (2, 30, 3, 4, 64), "f32").cuda()
+    was = qkv.clone()
+    q, k = (qkv[:, :, i].transpose(1, 2) for i in (0, 1))
+    ca.rope(r, q, k, grid=(2, 3, 5), layout="strided", q_out=q, k_out=k)
+    new = ca.rope(r, was[:, :, 0].transpose(1, 2), grid=(2, 3, 5), layout="strided")
+    assert torch.equal(new, q) and torch.equal(qkv[:, :, 2], was[:, :, 2])
+    assert not torch.equal(qkv[:, :, 1], was[:, :, 1])
+    ca.rope(r, q, k, grid=(2, 3, 5), layout="strided", inverse=True, q_out=q, k_out=k)
+    assert (qkv - was).abs().max() < 1e-5
+    p = torch.from_numpy(seq.grid_positions(30, (2, 3, 5), (7, -2, 100)).astype(np.int32)).cuda()
+    assert torch.equal(ca.rope(r, q, grid=(2, 3, 5), start=(7, -2, 100)), ca.rope(r, q, positions=p))
+
+
+def test_rope_dims_that_do_not_turn_keep_any_value():
+    import torch
+    ca = _ca()
+    x = torch.randn(1, 1, 4, 64).cuda()
+    x[..., 6:] = float("nan")
+    x[0, 0, 1, 9] = float("inf")
+    y = ca.rope(ca.rope_axes((6,)), x, grid=(4,))
+    assert torch.isfinite(y[..., :6]).all()
+    assert torch.equal(y[..., 6:].view(torch.int32), x[..., 6:].view(torch.int32))
+
+
+# ---- window attention --------------------------------------------------------------------
+
+def _window_case(dt, B, H, Hk, nq, nk, d, left=-1, right=-1, sinks=0, causal=False, lens=None, layout="bhnd",
+                 grads=True, scale=None, seed=0, big=1.0, fused=False):
+    import torch
+    ca = _ca()
+    g = _gen(seed)
+    lq, lk = lens or ([nq] * B, [nk] * B)
+    shape = (lambda h, n: (B, h, n, d)) if layout != "bnhd" else (lambda h, n: (B, n, h, d))
+    if fused:
+        qkv = _rand(g, (B, nq, 3, H, d), dt, big)
+        q, k, v = (qkv.cuda()[:, :, i].transpose(1, 2) for i in range(3))
+    else:
+        q, k, v = (_rand(g, shape(h, n), dt, big).cuda() for h, n in ((H, nq), (Hk, nk), (Hk, nk)))
+    do = _rand(g, shape(H, nq), dt).cuda()
+    # rows past the lengths hold anything
+    for b in range(B):
+        for t, n in ((q, lq[b]), (do, lq[b]), (k, lk[b]), (v, lk[b])):
+            (t[b] if layout != "bnhd" else t[b].transpose(0, 1))[:, n:] = float("nan")
+    kw = dict(layout=layout, scale=scale)
+    if lens:
+        kw["len_q"], kw["len_k"] = (torch.tensor(x, dtype=torch.int32).cuda() for x in (lq, lk))
+    w = ca.Window(left, right, sinks, causal)
+    out, lse = ca.window_attn(w, q, k, v, want_lse=True, **kw)
+    got = {"out": out, "lse": lse}
+    if grads:
+        got["dq"], got["dk"], got["dv"] = ca.window_attn_backward(w, do, q, k, v, out, lse, **kw)
+    host = {n: _np(t if layout != "bnhd" or n == "lse" else t.transpose(1, 2))
+            for n, t in dict(got, q=q, k=k, v=v, do=do).items()}
+    sc = scale or 1.0 / math.sqrt(d)
+    for b in range(B):
+        a, c = lq[b], lk[b]
+        see = seq.visible(a, c, left, right, sinks, causal)
+        sums = {}
+        for h in range(H):
+            hk = h // (H // Hk)
+            want = _bounds(host["q"][b, h, :a], host["k"][b, hk, :c], host["v"][b, hk, :c],
+                           host["do"][b, h, :a] if grads else None, see, sc, dt)
+            for n in ("out", "lse") + (("dq",) if grads else ()):
+                _close(host[n][b, h, :a], *want[n], f"{n} batch {b} head {h}")
+                past = host[n][b, h, a:]
+                assert np.all(past == (-np.inf if n == "lse" else 0.0)), f"{n} past the length"
+            for n in ("dk", "dv") if grads else ():
+                x, t = sums.get((n, hk), (0.0, 0.0))
+                sums[n, hk] = x + want[n][0], t + want[n][1]
+        for (n, hk), (x, t) in sums.items():
+            _close(host[n][b, hk, :c], x, t, f"{n} batch {b} key head {hk}")
+            assert not host[n][b, hk, c:].any(), f"{n} past the length"
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 2, 15, 31, 33, 64, 65, 127, 129, 200])
+def test_window_lengths(dt, d, n):
+    _window_case(dt, 1, 2, 1, n, n, d, left=20, sinks=3, causal=True, seed=n)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("kw", [
+    dict(), dict(causal=True), dict(left=0, right=0), dict(left=7, right=70), dict(left=70, right=7),
+    dict(left=64, right=64, sinks=64), dict(left=30, causal=True, sinks=100), dict(right=5, sinks=1), dict(left=1, sinks=300),
+    dict(left=100, right=0, sinks=5), dict(left=2 ** 31 - 1, right=2 ** 31 - 1, sinks=2 ** 31 - 1, causal=True),
+    dict(sinks=40, left=0, right=0)])
+def test_window_masks(dt, kw):
+    _window_case(dt, 2, 2, 2, 193, 193, 64, seed=1, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("nq,nk", [(1, 300), (300, 1), (40, 170), (170, 40), (3, 700), (129, 64)])
+@pytest.mark.parametrize("kw", [dict(causal=True), dict(left=50, causal=True, sinks=6), dict(left=20, right=30), dict()])
+def test_window_cross_lengths(dt, nq, nk, kw):
+    """Fewer queries than keys (a chunk of a longer sequence) and more (the
+    first rows of causal attention then see nothing)."""
+    _window_case(dt, 1, 2, 1, nq, nk, 64, seed=nq, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+@pytest.mark.parametrize("kw", [dict(), dict(left=40, causal=True, sinks=10), dict(left=9, right=33, sinks=2)])
+def test_window_ragged(dt, layout, kw):
+    """Padded batches: lengths of 0, 1 and the whole, queries and keys apart;
+    the padding holds NaN."""
+    lens = ([150, 0, 1, 77, 64], [150, 9, 0, 130, 1])
+    _window_case(dt, 5, 4, 2, 150, 150, 64, lens=lens, layout=layout, seed=2, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("H,Hk", [(6, 2), (5, 1), (3, 3)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_window_shared_heads(dt, H, Hk, d):
+    _window_case(dt, 2, H, Hk, 140, 140, d, left=33, right=11, sinks=1, seed=3)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_fused_projection(dt):
+    _window_case(dt, 2, 3, 3, 150, 150, 64, left=45, sinks=2, causal=True, layout="strided", fused=True, seed=4)
+
+
+@pytest.mark.parametrize("d", [4, 20, 32, 36, 100])
+def test_window_f32_head_dims(d):
+    _window_case("f32", 1, 2, 1, 90, 90, d, left=17, right=5, sinks=3, seed=d)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("kw", [dict(left=500, sinks=128, causal=True), dict(left=300, right=200, sinks=70), dict()])
+def test_window_longer(dt, kw):
+    _window_case(dt, 1, 2, 1, 1537, 1537, 64 if kw else 128, seed=5, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_large_logits(dt):
+    """Logits of some hundreds, growing along the keys: one key takes a row, and
+    every tile raises the maximum."""
+    _window_case(dt, 1, 1, 1, 260, 260, 64, causal=True, seed=6, big=6.0, scale=0.5)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_rising_maximum(dt):
+    import torch
+    ca = _ca()
+    g = _gen(9)
+    n, d = 700, 64
+    q, v = torch.ones(1, 1, n, d), torch.randn(1, 1, n, d, generator=g)
+    k = torch.linspace(-40, 40, n)[None, None, :, None].expand(1, 1, n, d).contiguous()
+    q, k, v = (x.to(_torch(dt)).cuda() for x in (q, k, v))
+    for kk in (k, k.flip(2).contiguous()):
+        out, lse = ca.window_attn(ca.Window(), q, kk, v, want_lse=True)
+        want = _bounds(*(_np(x)[0, 0] for x in (q, kk, v)), None, np.ones((n, n), bool), 0.125, dt)
+        _close(_np(out)[0, 0], *want["out"], "out")
+        _close(_np(lse)[0, 0], *want["lse"], "lse")
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_repeated_inputs(dt):
+    """Strides of 0: keys and values shared by the batch, the gradient of a sum."""
+    import torch
+    ca = _ca()
+    g = _gen(7)
+    q = _rand(g, (3, 4, 70, 64), dt).cuda()
+    k, v = (_rand(g, (1, 2, 70, 64), dt).cuda() for _ in range(2))
+    ke, ve = k.expand(3, 2, 70, 64), v.expand(3, 2, 70, 64)
+    w = ca.Window(left=20, sinks=2, causal=True)
+    a = ca.window_attn(w, q, ke, ve, want_lse=True)
+    b = ca.window_attn(w, q, ke.contiguous(), ve.contiguous(), want_lse=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    one = torch.ones(1, 1, 1, 64, dtype=_torch(dt), device="cuda")
+    ga = ca.window_attn_backward(w, one.expand(3, 4, 70, 64), q, ke, ve, *a)
+    gb = ca.window_attn_backward(w, one.expand(3, 4, 70, 64).contiguous(), q, ke, ve, *a)
+    assert all(torch.equal(x, y) for x, y in zip(ga, gb))
+    with pytest.raises(ca.CAError, match="dk_stride"):
+        ca.window_attn_backward(w, q, q, ke, ve, *a, dk=ke)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_gradients_into_a_fused_gradient(dt):
+    import torch
+    ca = _ca()
+    g = _gen(8)
+    qkv = _rand(g, (2, 50, 3, 2, 64), dt).cuda()
+    q, k, v = (qkv[:, :, i].transpose(1, 2) for i in range(3))
+    do = _rand(g, (2, 2, 50, 64), dt).cuda()
+    w = ca.Window(left=10, right=3)
+    out, lse = ca.window_attn(w, q, k, v, layout="strided", want_lse=True)
+    want = ca.window_attn_backward(w, do, q, k, v, out, lse, layout="strided")
+    grad = torch.full_like(qkv, 9.0)
+    views = [grad[:, :, i].transpose(1, 2) for i in range(3)]
+    ca.window_attn_backward(w, do, q, k, v, out, lse, layout="strided", dq=views[0], dk=views[1], dv=views[2])
+    assert all(torch.equal(a, b) for a, b in zip(views, want))
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_window_same_bits_twice(dt):
+    import torch
+    ca = _ca()
+    g = _gen(10)
+    q, do = (_rand(g, (1, 4, 900, 64), dt).cuda() for _ in range(2))
+    k, v = (_rand(g, (1, 2, 900, 64), dt).cuda() for _ in range(2))
+    w = ca.Window(left=200, sinks=70, causal=True)
+    runs = []
+    for _ in range(2):
+        out, lse = ca.window_attn(w, q, k, v, want_lse=True)
+        runs.append((out, lse) + ca.window_attn_backward(w, do, q, k, v, out, lse))
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+# ---- paged cache -----------------------------------------------------------------------------
+
+def _pages(g, dt, lens, page, Hk, d, heads_first=False, extra=2):
+    """Pools of random pages in random order; rows that hold no token are NaN."""
+    import torch
+    need = [-(-n // page) for n in lens]
+    pool = sum(need) + extra
+    order = torch.randperm(pool, generator=g).to(torch.int32)
+    width = max(max(need), 1) + 1
+    table = torch.full((len(lens), width), -1, dtype=torch.int32)
+    shape = (pool, Hk, page, d) if heads_first else (pool, page, Hk, d)
+    kp, vp = (torch.full(shape, float("nan"), dtype=_torch(dt)) for _ in range(2))
+    if heads_first:
+        kp, vp = kp.transpose(1, 2), vp.transpose(1, 2)
+    at, rows = 0, []
+    for b, n in enumerate(lens):
+        table[b, :need[b]] = order[at:at + need[b]]
+        at += need[b]
+        k, v = _rand(g, (n, Hk, d), dt), _rand(g, (n, Hk, d), dt)
+        for j in range(n):
+            pg = int(table[b, j // page])
+            kp[pg, j % page], vp[pg, j % page] = k[j], v[j]
+        rows.append((_np(k), _np(v)))
+    return kp.cuda(), vp.cuda(), table.cuda(), rows
+
+
+def _paged_check(q, out, lse, lens, rows, left, sinks, dt, scale=None):
+    B, H, d = q.shape
+    for b in range(B):
+        see = seq.visible(1, lens[b], left, -1, sinks) if lens[b] else np.zeros((1, 0), bool)
+        for h in range(H):
+            hk = h // (H // rows[b][0].shape[1])
+            want = _bounds(_np(q)[b, h][None], rows[b][0][:, hk], rows[b][1][:, hk], None, see,
+                           scale or 1.0 / math.sqrt(d), dt)
+            _close(_np(out)[b, h][None], *want["out"], f"sequence {b} head {h}")
+            _close(_np(lse)[b, h][None], *want["lse"], f"lse of sequence {b} head {h}")
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("page", [1, 7, 16, 64, 100, 128])
+@pytest.mark.parametrize("left,sinks", [(-1, 0), (0, 0), (90, 5), (33, 200)])
+def test_paged_lengths(dt, page, left, sinks):
+    import torch
+    ca = _ca()
+    g = _gen(page)
+    lens = [0, 1, 2, 63, 64, 65, 129, 300, 777]
+    kp, vp, table, rows = _pages(g, dt, lens, page, 2, 64)
+    q = _rand(g, (len(lens), 4, 64), dt).cuda()
+    n = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, n, left=left, sinks=sinks, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, left, sinks, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("H,Hk", [(1, 1), (5, 1), (16, 1), (17, 1), (40, 1), (24, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_heads(dt, H, Hk, d):
+    import torch
+    ca = _ca()
+    g = _gen(H)
+    lens = [200, 31]
+    kp, vp, table, rows = _pages(g, dt, lens, 16, Hk, d, heads_first=H % 2 == 0)
+    q = _rand(g, (2, H, d), dt).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, torch.tensor(lens, dtype=torch.int32).cuda(), want_lse=True, scale=0.2)
+    _paged_check(q, out, lse, lens, rows, -1, 0, dt, scale=0.2)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_paged_long_cache(dt):
+    """Some thousand keys: cut into parts and joined. A table wider than needed
+    (many parts of nothing) gives the same."""
+    import torch
+    ca = _ca()
+    g = _gen(11)
+    lens = [5003]
+    kp, vp, table, rows = _pages(g, dt, lens, 32, 1, 64)
+    q = _rand(g, (1, 2, 64), dt, 4.0).cuda()
+    n = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, n, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, -1, 0, dt)
+    wide = torch.full((1, 4000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    out, lse = ca.paged_attn(q, kp, vp, wide, n, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, -1, 0, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_paged_hidden_pages_are_not_read(dt):
+    """Pages behind the window may be gone: their entries lie outside the pool.
+    Shared pages (a common beginning) are read by both sequences."""
+    import torch
+    ca = _ca()
+    g = _gen(12)
+    lens = [640, 640]
+    kp, vp, table, rows = _pages(g, dt, lens, 16, 2, 64)
+    table[1, :2] = table[0, :2]
+    for i in range(2):
+        rows[1][i][:32] = rows[0][i][:32]
+    table[:, 2:30] = torch.tensor([-1, -5, 10 ** 6, 2 ** 31 - 1], dtype=torch.int32).repeat(7).cuda()
+    q = _rand(g, (2, 2, 64), dt).cuda()
+    n = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, n, left=640 - 30 * 16 - 1, sinks=32, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, 640 - 30 * 16 - 1, 32, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_paged_bad_entries_hold_no_tokens(dt):
+    """Entries outside the pool inside what is seen: their keys are not there.
+    Lengths beyond the table are cut to it, negative ones are 0."""
+    import torch
+    ca = _ca()
+    g = _gen(13)
+    lens = [100, 96, 20]
+    kp, vp, table, rows = _pages(g, dt, lens, 16, 1, 64)
+    table = table[:, :6].contiguous()
+    table[0, 2] = 10 ** 6
+    q = _rand(g, (3, 1, 64), dt).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, torch.tensor([10 ** 9, 96, -3], dtype=torch.int32).cuda(), want_lse=True)
+    keep = [j for j in range(96) if j // 16 != 2]
+    rows = [(rows[0][0][keep], rows[0][1][keep]), rows[1], (rows[2][0][:0], rows[2][1][:0])]
+    _paged_check(q, out, lse, [80, 96, 0], rows, -1, 0, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("page,n", [(16, 1), (5, 1), (5, 13), (1, 3)])
+def test_append(dt, page, n):
+    """The last n places of each sequence are written, nothing else; places
+    before 0 and bad pages are left out."""
+    import torch
+    ca = _ca()
+    g = _gen(14)
+    lens = [40, 3, 17, 0, 30]
+    kp, vp, table, _ = _pages(g, dt, lens, page, 2, 64)
+    kp, vp = torch.nan_to_num(kp), torch.nan_to_num(vp)
+    table[4, 29 // page] = kp.shape[0]  # outside the pool
+    k, v = _rand(g, (5, n, 2, 64), dt).cuda(), _rand(g, (5, n, 2, 64), dt).cuda()
+    wk, wv = kp.clone(), vp.clone()
+    for b, m in enumerate(lens):
+        for t in range(n):
+            j = m - n + t
+            if j >= 0 and 0 <= int(table[b, j // page]) < kp.shape[0]:
+                wk[int(table[b, j // page]), j % page] = k[b, t]
+                wv[int(table[b, j // page]), j % page] = v[b, t]
+    ca.cache_append(k, v, kp, vp, table, torch.tensor(lens, dtype=torch.int32).cuda())
+    assert torch.equal(kp, wk) and torch.equal(vp, wv)
+
+
+# ---- together ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", DT)
+def test_serving_steps_equal_one_pass(dt):
+    """Tokens served one at a time (rotary, append, paged attention with window
+    and sinks) against one causal pass over the whole sequence."""
+    import torch
+    ca = _ca()
+    g = _gen(15)
+    B, H, Hk, d, n, page = 2, 4, 2, 64, 40, 16
+    r = ca.rope_axes((32, 16, 16))
+    q, k, v = (_rand(g, (B, n, h, d), dt).cuda() for h in (H, Hk, Hk))
+    w = ca.Window(left=11, sinks=3, causal=True)
+    pos = torch.from_numpy(seq.grid_positions(n, (4, 2, 5)).astype(np.int32)).cuda()
+    qr, kr = ca.rope(r, q, k, grid=(4, 2, 5), layout="bnhd")
+    whole, _ = ca.window_attn(w, qr, kr, v, layout="bnhd")
+    kp, vp = (torch.zeros(B * 3, page, Hk, d, dtype=_torch(dt), device="cuda") for _ in range(2))
+    table = torch.arange(B * 3, dtype=torch.int32, device="cuda").view(B, 3)
+    for t in range(n):
+        lens = torch.full((B,), t + 1, dtype=torch.int32, device="cuda")
+        qt, kt = ca.rope(r, q[:, t:t + 1], k[:, t:t + 1], positions=pos[:, t:t + 1], layout="bnhd")
+        assert torch.equal(qt[:, 0], qr[:, t])
+        ca.cache_append(kt, v[:, t:t + 1], kp, vp, table, lens)
+        out, _ = ca.paged_attn(qt[:, 0], kp, vp, table, lens, left=11, sinks=3)
+        # both are within 2 u of the exact result, whose size is that of the values' mean
+        assert (out.float() - whole[:, t].float()).abs().max() <= 4 * (_u(dt) + 2.0 ** -20) * v.float().abs().max()
+
+
+def test_training_step_gradients():
+    """rotary -> window attention -> loss, and back through window_attn_backward
+    and the transposed rotation, against differences of the fp64 oracle's
+    gradients through the same chain."""
+    ca = _ca()
+    g = _gen(16)
+    B, H, Hk, n, d = 1, 2, 1, 60, 64
+    r = ca.rope_axes((32, 32))
+    q, k, v, do = (_rand(g, (B, h, n, d), "f32") for h in (H, Hk, Hk, H))
+    w = ca.Window(left=13, right=4, sinks=2)
+    qr, kr = ca.rope(r, q.cuda(), k.cuda(), grid=(6, 10))
+    out, lse = ca.window_attn(w, qr, kr, v.cuda(), want_lse=True)
+    dqr, dkr, dv = ca.window_attn_backward(w, do.cuda(), qr, kr, v.cuda(), out, lse)
+    dq, dk = ca.rope(r, dqr, dkr, grid=(6, 10), inverse=True)
+    pos, see = seq.grid_positions(n, (6, 10)), seq.visible(n, n, 13, 4, 2)
+    turn = lambda x, inv=False: seq.rope(x, pos, r.sections, r.freqs, inverse=inv)  # noqa: E731
+    wk, wv = 0.0, 0.0
+    for h in range(H):
+        a, b, c = seq.attend_backward(turn(_np(q)[0, h]), turn(_np(k)[0, 0]), _np(v)[0, 0], _np(do)[0, h], see, 0.125)
+        assert np.abs(turn(a, True) - _np(dq)[0, h]).max() < 2e-5
+        wk, wv = wk + turn(b, True), wv + c
+    assert np.abs(wk - _np(dk)[0, 0]).max() < 4e-5 and np.abs(wv - _np(dv)[0, 0]).max() < 4e-5
+
+
+def test_forward_turns_first():
+    """forward(rotary=...) is forward on the turned queries and keys."""
+    import torch
+    ca = _ca()
+    g = _gen(17)
+    q, k, v = (_rand(g, (1, 2, 600, 64), "bf16").cuda() for _ in range(3))
+    r = ca.rope_axes((24, 20, 20))
+    a = ca.forward(q, k, v, cq=64, keep=0.5, rotary=r, rope_grid=(6, 10, 10))
+    qr, kr = ca.rope(r, q, k, grid=(6, 10, 10))
+    assert torch.equal(a, ca.forward(qr, kr, v, cq=64, keep=0.5))
+
+
+def test_other_stream_and_graph_replays():
+    """A step captured on a side stream and replayed on new inputs equals the
+    eager calls, with eager work between the replays."""
+    import torch
+    ca = _ca()
+    g = _gen(18)
+    r, w = ca.rope_axes((32, 32)), ca.Window(left=50, sinks=4, causal=True)
+    q, k, v, do = (torch.empty(1, h, 300, 64, dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2, 4))
+
+    def step():
+        qr, kr = ca.rope(r, q, k, grid=(15, 20))
+        out, lse = ca.window_attn(w, qr, kr, v, want_lse=True)
+        return (out, lse) + ca.window_attn_backward(w, do, qr, kr, v, out, lse)
+
+    def serve():
+        kp, vp = k[0].transpose(0, 1)[:, None], v[0].transpose(0, 1)[:, None]  # pages of one token
+        table = torch.arange(300, dtype=torch.int32, device="cuda")[None]
+        lens = table[:, -1] + 1
+        return ca.paged_attn(q[:, :, -1], kp, vp, table, lens, want_lse=True)
+
+    def fill(seed):
+        s = _gen(seed)
+        for t in (q, k, v, do):
+            t.copy_(torch.randn(t.shape, generator=s))
+
+    fill(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(), serve()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = step() + serve()
+    for seed in range(1, 5):
+        fill(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = step() + serve()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
