@@ -456,13 +456,15 @@ typedef struct {
   int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
 } ca_window;
 
-/* out: strides out_stride; lse: optional dense fp32 [batch][heads][nq]. */
+/* out: strides out_stride; lse: optional dense fp32 [batch][heads][nq]. ws:
+ * workspace (long keys for few queries are cut into parts and joined). */
 CA_API int ca_window_attn(const ca_window* p, const void* q, const void* k, const void* v,
                           const int32_t* len_q, const int32_t* len_k, void* out, float* lse,
-                          void* stream);
+                          void* ws, size_t ws_bytes, void* stream);
 
-/* Bytes of workspace of ca_window_attn_backward (256-byte aligned). Host-only. */
-CA_API int ca_window_workspace_size(const ca_window* p, size_t* bytes);
+/* Bytes of workspace of ca_window_attn (backward 0; may be 0 bytes) or
+ * ca_window_attn_backward (backward 1), 256-byte aligned. Host-only. */
+CA_API int ca_window_workspace_size(const ca_window* p, int32_t backward, size_t* bytes);
 
 /* Gradients of ca_window_attn: from out and lse as it wrote them (same
  * arguments) and dout, with P = e^{s - lse} and D = row sums of dout * out,

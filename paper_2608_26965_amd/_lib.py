@@ -133,8 +133,9 @@ def load() -> ctypes.CDLL:
     lib.ca_check_finite.argtypes = [P, _vp, _vp, _vp, _vp, _vp]
     size = ctypes.POINTER(ctypes.c_size_t)
     lib.ca_rope.argtypes = [ctypes.POINTER(CaRope)] + [_vp] * 6
-    lib.ca_window_attn.argtypes = [ctypes.POINTER(CaWindow)] + [_vp] * 8
-    lib.ca_window_workspace_size.argtypes = [ctypes.POINTER(CaWindow), size]
+    lib.ca_window_attn.argtypes = ([ctypes.POINTER(CaWindow)] + [_vp] * 8
+                                   + [ctypes.c_size_t, _vp])
+    lib.ca_window_workspace_size.argtypes = [ctypes.POINTER(CaWindow), _i32, size]
     lib.ca_window_attn_backward.argtypes = ([ctypes.POINTER(CaWindow)] + [_vp] * 12
                                             + [ctypes.c_size_t, _vp])
     lib.ca_cache_append.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 7

@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "common.h"
@@ -247,6 +248,16 @@ int check_window(const ca_window* p, ca::WinProb* P) {
       (s = check_strides(p->v_stride, 3, p->dtype, "v")) ||
       (s = check_strides(p->out_stride, 3, p->dtype, "out")))
     return s;
+  // the bf16 kernels reach the 64 rows of a tile by 32-bit offsets, and launch
+  // 256 threads per 128 rows
+  if (p->dtype == CA_BF16) {
+    const int64_t* st[3] = {p->q_stride, p->k_stride, p->v_stride};
+    for (int t = 0; t < 3; ++t)
+      if (st[t][2] > (1 << 23))
+        return fail(CA_E_UNSUPPORTED, "bf16 window attention needs token strides of at most 2^23");
+    if ((int64_t)p->batch * p->heads * ((std::max(p->nq, p->nk) + 127) / 128 + 8) >= (1 << 23))
+      return fail(CA_E_UNSUPPORTED, "bf16 window attention: batch * heads * tokens too large");
+  }
   auto side = [](int x) { return x < 0 || x > ca::kUnlimited ? ca::kUnlimited : x; };
   P->B = p->batch;
   P->H = p->heads;
@@ -736,8 +747,8 @@ int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const int32_t* 
 }
 
 int ca_window_attn(const ca_window* p, const void* q, const void* k, const void* v,
-                   const int32_t* len_q, const int32_t* len_k, void* out, float* lse,
-                   void* stream) {
+                   const int32_t* len_q, const int32_t* len_k, void* out, float* lse, void* ws,
+                   size_t ws_bytes, void* stream) {
   ca::WinProb P;
   int s = check_window(p, &P);
   if (s) return s;
@@ -745,18 +756,19 @@ int ca_window_attn(const ca_window* p, const void* q, const void* k, const void*
       (s = check_base(out, "out")) ||
       (s = check_written(p->out_stride, p->batch, p->heads, p->nq, "out")))
     return s;
+  if ((s = check_bytes(ca::window_bytes(P), ws, ws_bytes))) return s;
   P.len_q = len_q;
   P.len_k = len_k;
-  return device_status(ca::launch_window(P, q, k, v, out, lse, (hipStream_t)stream),
+  return device_status(ca::launch_window(P, q, k, v, out, lse, (char*)ws, (hipStream_t)stream),
                        "ca_window_attn");
 }
 
-int ca_window_workspace_size(const ca_window* p, size_t* bytes) {
+int ca_window_workspace_size(const ca_window* p, int32_t backward, size_t* bytes) {
   ca::WinProb P;
   int s = check_window(p, &P);
   if (s) return s;
   if (!bytes) return fail(CA_E_INVALID, "bytes is NULL");
-  *bytes = ca::window_backward_bytes(P);
+  *bytes = backward ? ca::window_backward_bytes(P) : ca::window_bytes(P);
   return ok();
 }
 

@@ -286,17 +286,16 @@ hipError_t run_backward_f32(const WinProb& P, const T* q, const T* k, const T* v
 
 }  // namespace
 
+size_t window_bytes(const WinProb& P) { return P.dtype == CA_BF16 ? window_bf16_bytes(P) : 0; }
+
 hipError_t launch_window(const WinProb& P, const void* q, const void* k, const void* v, void* out,
-                         float* lse, hipStream_t st) {
-#define CA_WINDOW(DP, T) \
-  return run_f32<DP, T>(P, (const T*)q, (const T*)k, (const T*)v, (T*)out, lse, st)
-  if (P.dtype == CA_BF16) {
-    if (P.d == 64) CA_WINDOW(64, bf16);
-    CA_WINDOW(128, bf16);
-  }
-  if (P.d <= 32) CA_WINDOW(32, float);
-  if (P.d <= 64) CA_WINDOW(64, float);
-  CA_WINDOW(128, float);
+                         float* lse, char* ws, hipStream_t st) {
+  if (P.dtype == CA_BF16) return launch_window_bf16(P, q, k, v, out, lse, ws, st);
+#define CA_WINDOW(DP) \
+  return run_f32<DP, float>(P, (const float*)q, (const float*)k, (const float*)v, (float*)out, lse, st)
+  if (P.d <= 32) CA_WINDOW(32);
+  if (P.d <= 64) CA_WINDOW(64);
+  CA_WINDOW(128);
 #undef CA_WINDOW
 }
 

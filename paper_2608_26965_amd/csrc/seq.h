@@ -76,8 +76,13 @@ struct WinProb {
   __device__ __forceinline__ int klen(int b) const { return len_k ? min(max(len_k[b], 0), nk) : nk; }
 };
 
+// workspace of the forward pass: partial results where the keys are cut into parts
+size_t window_bytes(const WinProb& P);
 hipError_t launch_window(const WinProb& P, const void* q, const void* k, const void* v, void* out,
-                         float* lse, hipStream_t st);
+                         float* lse, char* ws, hipStream_t st);
+size_t window_bf16_bytes(const WinProb& P);
+hipError_t launch_window_bf16(const WinProb& P, const void* q, const void* k, const void* v,
+                              void* out, float* lse, char* ws, hipStream_t st);
 // Workspace of the backward pass: delta (the row sums of dout * out), fp32 [B H][nq]
 size_t window_backward_bytes(const WinProb& P);
 hipError_t launch_window_backward(const WinProb& P, const void* q, const void* k, const void* v,

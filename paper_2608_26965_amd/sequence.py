@@ -107,12 +107,17 @@ def _call(name, device, *args):
         _lib.check(st, name)
 
 
-def _workspace(nbytes, device, ws, name):
-    if ws is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    if ws.device != device or not ws.is_contiguous():
-        raise ValueError(f"{name}: the workspace must be contiguous and on {device}")
-    return ws
+def _workspace(size, *args, device, ws):
+    """The caller's workspace, or a new one of the bytes that the library asks for."""
+    if ws is not None:
+        if ws.device != device or not ws.is_contiguous():
+            raise ValueError(f"ws: expected a contiguous tensor on {device}")
+        return ws
+    n = ctypes.c_size_t(0)
+    st = getattr(_lib.load(), size)(*args, n)
+    if st:
+        _lib.check(st, size)
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
 
 
 def _ptr(t):
@@ -262,7 +267,7 @@ def _lse(q, layout):
 
 
 def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layout="bhnd",
-                want_lse=False, out=None):
+                want_lse=False, out=None, ws=None):
     """Attention with a sliding window and sinks. q: [B,H,nq,d] ("bhnd",
     "strided") or [B,nq,H,d] ("bnhd"), any strides; k, v the same with nk
     tokens and heads_k heads (a divisor of H). len_q, len_k: int32 [B], the
@@ -272,8 +277,9 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     c = _window(w, q, k, v, out, scale, len_q, len_k, layout)
     lse = _lse(q, layout) if want_lse else None
+    ws = _workspace("ca_window_workspace_size", c, 0, device=q.device, ws=ws)
     _call("ca_window_attn", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(len_q),
-          _ptr(len_k), out.data_ptr(), _ptr(lse))
+          _ptr(len_k), out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes)
     return out, lse
 
 
@@ -293,9 +299,7 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
         raise ValueError("lse: expected a contiguous fp32 tensor on the same device")
     _expect(lse, (c.batch, c.heads, c.nq), "lse")
-    n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().ca_window_workspace_size(c, n), "ca_window_workspace_size")
-    ws = _workspace(n.value, q.device, ws, "window_attn_backward")
+    ws = _workspace("ca_window_workspace_size", c, 1, device=q.device, ws=ws)
     _call("ca_window_attn_backward", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           out.data_ptr(), lse.data_ptr(), dout.data_ptr(), _ptr(len_q), _ptr(len_k),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes)
@@ -363,9 +367,7 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     c = _paged(q, H, k_pages, v_pages, page_table, lens, left, sinks, scale, _strides_of(q, 2),
                _strides_of(out, 2))
     lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
-    n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().ca_paged_workspace_size(c, n), "ca_paged_workspace_size")
-    ws = _workspace(n.value, q.device, ws, "paged_attn")
+    ws = _workspace("ca_paged_workspace_size", c, device=q.device, ws=ws)
     _call("ca_paged_attn", q.device, c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
           page_table.data_ptr(), lens.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(ws),
           0 if ws is None else ws.nbytes)

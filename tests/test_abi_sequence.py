@@ -72,14 +72,15 @@ _BAD_WINDOW = [
     (dict(batch=0), 1, "batch"), (dict(nq=0), 1, "nq"), (dict(nk=0), 1, "nk"), (dict(nk=(1 << 22) + 1), 1, "2^22"),
     (dict(d=96), 2, "64, 128"), (dict(d=192), 1, "d must"), (dict(dtype=0, d=62), 2, "fp32"), (dict(sinks=-1), 1, "sinks"),
     (dict(batch=8192), 2, "65535"), (dict(q_stride=I3(64, 64, 4)), 1, "q_stride[2]"),
-    (dict(v_stride=I3(64, 4, 64)), 1, "v_stride[1]"), (dict(out_stride=I3(-64, 64, 64)), 1, "out_stride[0]"),
+    (dict(v_stride=I3(64, 4, 64)), 1, "v_stride[1]"), (dict(k_stride=I3(64, 64, 1 << 24)), 2, "2^23"),
+    (dict(batch=1000, heads=64, nq=1 << 22), 2, "too large"), (dict(out_stride=I3(-64, 64, 64)), 1, "out_stride[0]"),
 ]
 
 
 @pytest.mark.parametrize("kw,status,word", _BAD_WINDOW + [(dict(out_stride=I3(51200, 0, 64)), 1, "out_stride[1]")])
 def test_window_refusals(kw, status, word):
     L, lib = _lib()
-    assert lib.ca_window_attn(_window(**kw), FAKE, FAKE, FAKE, None, None, FAKE, None, None) == status
+    assert lib.ca_window_attn(_window(**kw), FAKE, FAKE, FAKE, None, None, FAKE, None, FAKE, 1 << 40, None) == status
     assert word in L.last_error()
 
 
@@ -97,13 +98,16 @@ def test_window_backward_refusals(kw, status, word):
 def test_window_pointers_and_workspace():
     L, lib = _lib()
     n = ctypes.c_size_t(0)
-    assert lib.ca_window_workspace_size(None, n) == L.CA_E_INVALID
-    assert lib.ca_window_workspace_size(_window(), n) == L.CA_OK and n.value >= 2 * 8 * 100 * 4
+    assert lib.ca_window_workspace_size(None, 0, n) == L.CA_E_INVALID
+    assert lib.ca_window_workspace_size(_window(nk=100000), 0, n) == L.CA_OK and n.value > 0
+    assert lib.ca_window_attn(_window(nk=100000), FAKE, FAKE, FAKE, None, None, FAKE, None, FAKE, n.value - 1, None) == \
+        L.CA_E_WORKSPACE
+    assert lib.ca_window_workspace_size(_window(), 1, n) == L.CA_OK and n.value >= 2 * 8 * 100 * 4
     for i in range(4):
         a = [FAKE, FAKE, FAKE, FAKE]
         for bad in (None, FAKE + 2):
             a[i] = bad
-            assert lib.ca_window_attn(_window(), *a[:3], None, None, a[3], None, None) == L.CA_E_INVALID
+            assert lib.ca_window_attn(_window(), *a[:3], None, None, a[3], None, FAKE, n.value, None) == L.CA_E_INVALID
     for i in range(9):
         a = [FAKE] * 9
         a[i] = None
