@@ -93,7 +93,6 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
   const KeyRange ra = visible_keys(P.m, w0 + off, lk);
   const KeyRange rz = visible_keys(P.m, w0 + max(wreal, 1) - 1 + off, lk);
   const int i = min(w0 + min(l32, max(wreal, 1) - 1), P.nq - 1);  // this lane's query
-  const KeyRange rr = visible_keys(P.m, i + off, lk);
 
   bf16x8 qreg[KS];
   {
@@ -113,11 +112,12 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
   const uint32_t lds0 = lds_addr(smem);
   auto issue_k = [&](int t, int buf) __attribute__((always_inline)) {
     const int k0 = KT * list.tile(t);
-    kcopy.issue(kbase + (int64_t)k0 * P.lk.sn, lds0 + buf * TILE, w, lk - 1 - k0);
+    kcopy.issue(kbase + (int64_t)k0 * P.lk.sn, lds0 + buf * TILE, w, lane, lk - 1 - k0);
   };
   auto issue_v = [&](int t, int buf) __attribute__((always_inline)) {
     const int k0 = KT * list.tile(t);
-    vcopy.issue(vbase + (int64_t)k0 * P.lv.sn, lds0 + (2 + buf) * TILE, w, lk - 1 - k0);
+    vcopy.issue(vbase + (int64_t)k0 * P.lv.sn, lds0 + (2 + buf) * TILE, w, lane,
+                lk - 1 - k0);
   };
   int koff[KS], voff[DT][2];
 #pragma unroll
@@ -129,9 +129,10 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
 
   f32x16 oacc[DT], sacc[2];
   bf16x8 pb[2][2];  // probabilities, the value product's operand
-  float m = -INFINITY, l = 0.f;  // reference (log2 units), this lane's part of the sum
-  bool set = false;              // every row of the wavefront has a reference
-  int pend = 0;                  // class of the tile whose value product is due
+  float m, l;       // reference (log2 units) and this lane's part of the sum
+  float alpha;      // what a raised reference scales the results so far by
+  bool set;         // every row of the wavefront has a reference
+  bool safe = false;
 
   auto logits = [&](const char* ks) __attribute__((always_inline)) {
 #pragma unroll
@@ -148,7 +149,11 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     }
   };
   // accumulator r of row tile mt is key k0 + 32 mt + 8 (r / 4) + 4 h + r % 4
+  // (the query's ranges are formed here: kept over the loop they cost registers)
   auto mask = [&](int k0) __attribute__((always_inline)) {
+    int p = i + off;
+    asm volatile("" : "+v"(p));
+    const KeyRange rr = visible_keys(P.m, p, lk);
     const int a0 = k0 + 4 * h - rr.lo, b0 = rr.s_end - k0 - 4 * h;
     const uint32_t len = (uint32_t)max(0, rr.hi - rr.lo);
 #pragma unroll
@@ -175,14 +180,17 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
       oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pb[mt][s2], oacc[dt], 0, 0, 0);
     }
   };
-  auto pv = [&](const char* vs) __attribute__((always_inline)) {
+  // The reference of a tile of class c: the rows' own where every row has one and
+  // sees all of the tile, else raised to the tile's maximum. True if raised.
+  auto reference = [&](int c, int k0) __attribute__((always_inline)) {
+    if (c == 2 && set && !safe) return false;
+    if (c == 1) mask(k0);
+    if (c == 0) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) pv_group(vs, mt, s2);
-  };
-  // a tile against its own maximum: the sums and outputs so far are rescaled
-  auto careful = [&]() __attribute__((always_inline)) {
+        for (int r = 0; r < 16; ++r) sacc[mt][r] = -INFINITY;
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
@@ -190,21 +198,12 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[mt][r]);
     mx = fmaxf(mx, wave_xor32(mx));
     const float m_new = fmaxf(m, mx * sl2);
-    const float ref = m_new == -INFINITY ? 0.f : m_new;  // nothing visible yet
-    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
-      const float alpha = __builtin_amdgcn_exp2f(m - ref);
-      l *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-      m = m_new;
-    }
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) exp_group(mt, s2, ref);
+    alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+    l *= alpha;
+    const bool raised = __builtin_amdgcn_ballot_w64(m_new > m) != 0;
+    m = m_new;
     set = __builtin_amdgcn_ballot_w64(m == -INFINITY) == 0;
+    return raised;
   };
   auto sync_stage = [&]() __attribute__((always_inline)) {
     wait_vmcnt<0>();
@@ -216,66 +215,89 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
   // (g counted from t0). After iteration g's barrier every wavefront is past
   // iteration g - 1 and the copies that it issued have landed: the keys of tile
   // g + 1 and the values of tile g are copied, the logits of tile g formed, and
-  // the value product of tile g - 1 runs among the exponentials of tile g.
-  auto run = [&](auto safe_tag) __attribute__((always_inline)) {
-    constexpr bool SAFE = decltype(safe_tag)::value;
+  // the value product of tile g - 1 runs among the exponentials of tile g. The
+  // two edge cases (a tile that none of the wavefront's rows sees, a raised
+  // reference) stay around that one piece of code, so that the accumulators stay
+  // in place.
+  auto copies = [&](auto par_tag, int t) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_tag)::value;
+    sync_stage();
+    if (t + 1 < t1) issue_k(t + 1, PAR ^ 1);
+    issue_v(t, PAR);
+  };
+  auto step = [&](auto par_tag, int t) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_tag)::value;
+    copies(par_tag, t);
+    const int k0 = KT * list.tile(t), c = tile_class(ra, rz, k0);
+    logits(smem + PAR * TILE);
+    const bool raised = reference(c, k0);
+    const float ref = m == -INFINITY ? 0.f : m;  // no key yet
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        pv_group(smem + (2 + (PAR ^ 1)) * TILE, mt, s2);
+        exp_group(mt, s2, ref);
+      }
+    if (raised) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+    }
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  float l_tot;
+  for (;;) {
     m = -INFINITY;
     l = 0.f;
     set = false;
-    pend = 0;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
-    auto step = [&](auto par_tag, int t) __attribute__((always_inline)) {
-      constexpr int PAR = decltype(par_tag)::value;
-      const char* vs = smem + (2 + (PAR ^ 1)) * TILE;  // values of the tile before
-      sync_stage();
-      if (t + 1 < t1) issue_k(t + 1, PAR ^ 1);
-      issue_v(t, PAR);
-      const int k0 = KT * list.tile(t);
-      const int c = tile_class(ra, rz, k0);
-      if (wreal == 0) return;
-      if (c) logits(smem + PAR * TILE);
-      if (!SAFE && c == 2 && set && pend) {
+    if (t0 < t1) {
+      issue_k(t0, 0);
+      copies(even, t0);
+      if (wreal == 0) {  // no rows: copies only
+        for (int t = t0 + 1; t < t1; t += 2) {
+          copies(odd, t);
+          if (t + 1 < t1) copies(even, t + 1);
+        }
+        sync_stage();
+      } else {
+        const int k0 = KT * list.tile(t0);
+        logits(smem);
+        reference(tile_class(ra, rz, k0), k0);
+        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) {
-            pv_group(vs, mt, s2);
-            exp_group(mt, s2, m);
-          }
-      } else {
-        if (pend) pv(vs);
-        if (c == 1) mask(k0);
-        if (c) careful();
-      }
-      pend = c;
-    };
-    if (t0 < t1) {
-      issue_k(t0, 0);
-      for (int t = t0; t < t1; t += 2) {
-        step(std::integral_constant<int, 0>{}, t);
-        if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1);
+          for (int s2 = 0; s2 < 2; ++s2) exp_group(mt, s2, ref);
+        for (int t = t0 + 1; t < t1; t += 2) {
+          step(odd, t);
+          if (t + 1 < t1) step(even, t + 1);
+        }
+        sync_stage();
+        const char* vs = smem + (2 + ((t1 - 1 - t0) & 1)) * TILE;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) pv_group(vs, mt, s2);
       }
     }
-    sync_stage();
-    if (pend) pv(smem + (2 + ((t1 - 1 - t0) & 1)) * TILE);
-  };
-  run(std::false_type{});
-  float l_tot = l + wave_xor32(l);
-  {
+    l_tot = l + wave_xor32(l);
+    if (safe) break;
     bool fine = l_tot <= 0x1p126f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) fine &= fabsf(oacc[dt][r]) <= 0x1p127f;
     if (__builtin_amdgcn_ballot_w64(!fine) && lane == 0) redo = 1;
-  }
-  __syncthreads();
-  if (redo) {
-    run(std::true_type{});
-    l_tot = l + wave_xor32(l);
+    __syncthreads();
+    if (!redo) break;
+    safe = true;
   }
 
   if constexpr (SPLIT) {

@@ -23,42 +23,43 @@ __device__ __forceinline__ int row_key(int r) {
 
 // Copies ROWS rows of RB bytes, `stride` bytes apart, into an LDS tile, NW
 // wavefronts together (direct global-to-LDS copies, 1024 bytes each).
+// An instruction of all wavefronts holds a multiple of sixteen rows, so every one of
+// a lane's rows has the same key and its offsets differ by whole rows only.
 template <int RB, int ROWS, int NW>
 struct RowCopy {
   static constexpr int NI = ROWS * RB / 1024 / NW;
   static constexpr int RPI = 1024 / RB;  // rows of an instruction
-  static_assert(NI * 1024 * NW == ROWS * RB, "tile split");
-  uint32_t off[NI];
-  uint32_t stride;
-  int row0;        // this lane's row of the wavefront's first instruction
-  uint32_t chunk[NI];
+  static_assert(NI * 1024 * NW == ROWS * RB && NW * RPI % 16 == 0, "tile split");
+  uint32_t off;     // of this lane's first row and chunk
+  uint32_t stride;  // bytes between rows
 
+  static __device__ __forceinline__ int row0(int w, int lane) { return w * RPI + lane / (RB / 16); }
+  static __device__ __forceinline__ uint32_t chunk(int w, int lane) {
+    return (uint32_t)(((lane % (RB / 16)) ^ row_key<RB>(row0(w, lane))) << 4);
+  }
   __device__ __forceinline__ RowCopy(int w, int lane, uint32_t stride_bytes) {
     stride = stride_bytes;
-    row0 = w * RPI + lane / (RB / 16);
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int r = row0 + i * NW * RPI;
-      chunk[i] = (uint32_t)(((lane % (RB / 16)) ^ row_key<RB>(r)) << 4);
-      off[i] = (uint32_t)r * stride + chunk[i];
-    }
+    off = (uint32_t)row0(w, lane) * stride + chunk(w, lane);
+  }
+  __device__ __forceinline__ static uint32_t dst(uint32_t lds, int i, int w) {
+    return __builtin_amdgcn_readfirstlane(lds + (uint32_t)((i * NW + w) * 1024));
   }
   __device__ __forceinline__ void issue(const void* base, uint32_t lds, int w) const {
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      lds_dma16(base, off[i],
-                __builtin_amdgcn_readfirstlane(lds + (uint32_t)((i * NW + w) * 1024)));
+      lds_dma16((const char*)base + (int64_t)i * NW * RPI * stride, off, dst(lds, i, w));
   }
   // rows past `last` are copies of it
-  __device__ __forceinline__ void issue(const void* base, uint32_t lds, int w, int last) const {
+  __device__ __forceinline__ void issue(const void* base, uint32_t lds, int w, int lane,
+                                        int last) const {
     if (last >= ROWS - 1) {
       issue(base, lds, w);
       return;
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      lds_dma16(base, (uint32_t)min(row0 + i * NW * RPI, last) * stride + chunk[i],
-                __builtin_amdgcn_readfirstlane(lds + (uint32_t)((i * NW + w) * 1024)));
+      lds_dma16(base, (uint32_t)min(row0(w, lane) + i * NW * RPI, last) * stride + chunk(w, lane),
+                dst(lds, i, w));
   }
 };
 
