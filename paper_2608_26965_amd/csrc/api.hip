@@ -249,13 +249,13 @@ int check_window(const ca_window* p, ca::WinProb* P) {
       (s = check_strides(p->out_stride, 3, p->dtype, "out")))
     return s;
   // the bf16 kernels reach the 64 rows of a tile by 32-bit offsets, and launch
-  // 256 threads per 128 rows
+  // up to 512 threads per 128 rows
   if (p->dtype == CA_BF16) {
     const int64_t* st[3] = {p->q_stride, p->k_stride, p->v_stride};
     for (int t = 0; t < 3; ++t)
       if (st[t][2] > (1 << 23))
         return fail(CA_E_UNSUPPORTED, "bf16 window attention needs token strides of at most 2^23");
-    if ((int64_t)p->batch * p->heads * ((std::max(p->nq, p->nk) + 127) / 128 + 8) >= (1 << 23))
+    if ((int64_t)p->batch * p->heads * ((std::max(p->nq, p->nk) + 127) / 128 + 8) >= (1 << 22))
       return fail(CA_E_UNSUPPORTED, "bf16 window attention: batch * heads * tokens too large");
   }
   auto side = [](int x) { return x < 0 || x > ca::kUnlimited ? ca::kUnlimited : x; };

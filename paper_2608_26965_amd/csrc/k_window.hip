@@ -300,22 +300,22 @@ hipError_t launch_window(const WinProb& P, const void* q, const void* k, const v
 }
 
 size_t window_backward_bytes(const WinProb& P) {
+  if (P.dtype == CA_BF16) return window_grad_bf16_bytes(P);
   return ((size_t)P.B * P.H * P.nq * 4 + 255) & ~(size_t)255;
 }
 
 hipError_t launch_window_backward(const WinProb& P, const void* q, const void* k, const void* v,
                                   const void* out, const float* lse, const void* dout, void* dq,
                                   void* dk, void* dv, char* ws, hipStream_t st) {
-#define CA_WINDOW(DP, T)                                                                          \
-  return run_backward_f32<DP, T>(P, (const T*)q, (const T*)k, (const T*)v, (const T*)out, lse,    \
-                                 (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (float*)ws, st)
-  if (P.dtype == CA_BF16) {
-    if (P.d == 64) CA_WINDOW(64, bf16);
-    CA_WINDOW(128, bf16);
-  }
-  if (P.d <= 32) CA_WINDOW(32, float);
-  if (P.d <= 64) CA_WINDOW(64, float);
-  CA_WINDOW(128, float);
+  if (P.dtype == CA_BF16)
+    return launch_window_grad_bf16(P, q, k, v, out, lse, dout, dq, dk, dv, ws, st);
+#define CA_WINDOW(DP)                                                                             \
+  return run_backward_f32<DP, float>(P, (const float*)q, (const float*)k, (const float*)v,        \
+                                     (const float*)out, lse, (const float*)dout, (float*)dq,      \
+                                     (float*)dk, (float*)dv, (float*)ws, st)
+  if (P.d <= 32) CA_WINDOW(32);
+  if (P.d <= 64) CA_WINDOW(64);
+  CA_WINDOW(128);
 #undef CA_WINDOW
 }
 

@@ -1,0 +1,548 @@
+// Gradients of attention with a sliding window and sinks, bf16, on the matrix
+// cores.
+//
+// Two kernels of one form. Each keeps 16 rows a wavefront (128 a workgroup) of
+// two tensors in registers, streams 64-row tiles of two others through LDS
+// (row_tile.h) and forms per tile, with P = e^{s - lse},
+//     S = X A^T,  E = Y B^T - D,  dS = P E
+// on 16x16x32 products, whose output (a lane holds one kept row and four
+// streamed rows of every 16) is the next product's operand as it stands:
+//   queries kept (A = q, B = dout), keys streamed (X = k, Y = v):
+//     dq += dS k            and the mean key  kbar += P k
+//   keys kept (A = k, B = v), queries streamed (X = q, Y = dout):
+//     dk += dS^T q,  dv += P^T dout
+// Logits and E are formed twice that way, but every sum has one owner and a fixed
+// order; adding dq up from the second kernel would need atomics or hundreds of
+// megabytes of partial sums.
+//
+// P and dS are rounded to bf16 for their products (2^-8 each), everything else is
+// fp32. A row's dS sum to zero, so that what the keys have in common drops out of
+// dq; rounded ones, and a D = rowsum(dout * out) from an output that was rounded to
+// bf16, leave a sum r of their own, and r times the mean key of an error. So the
+// first kernel sums the dS as rounded and takes it out, dq = scale (sum dS k -
+// r kbar), and D + r goes to the second. Without it dq is off by 0.0037 of its
+// size (keys of one mixture, 8,192 tokens) where rounding the result alone
+// is 0.0017.
+#include <math.h>
+
+#include "row_tile.h"
+#include "seq.h"
+
+namespace ca {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
+constexpr int kRows = 128;       // kept rows of a workgroup
+constexpr int KT = 64;           // streamed rows of a tile
+constexpr int NW = 8;
+
+// Row blocks and the parts that their streamed tiles are cut into. Blocks 0 ..
+// nsink - 1 are cut into `psink` parts (keys kept: the blocks that hold sinks,
+// which every query sees), the others into `p`.
+struct Parts {
+  int nb, nsink, psink, p;
+  __host__ __device__ int items() const { return nsink * psink + (nb - nsink) * p; }
+  // places of partial sums: blocks of one part need none
+  __host__ __device__ int places() const {
+    return (psink > 1 ? nsink * psink : 0) + (p > 1 ? (nb - nsink) * p : 0);
+  }
+  // block, part and number of parts of item v; the place of its partial sums
+  __device__ __forceinline__ void at(int v, int* a, int* part, int* parts, int* place) const {
+    const int s = nsink * psink;
+    if (v < s) {
+      *a = v / psink;
+      *part = v - *a * psink;
+      *parts = psink;
+      *place = v;
+    } else {
+      const int x = (v - s) / p;
+      *a = nsink + x;
+      *part = v - s - x * p;
+      *parts = p;
+      *place = (psink > 1 ? s : 0) + v - s;
+    }
+  }
+};
+
+// All XCDs work on one head at a time, each on a contiguous eighth of its items
+// where the window is short (they read the same streamed rows), else on every
+// eighth (the work of causal blocks grows or falls along the sequence).
+__device__ __forceinline__ bool item_of(int wg, int n, int G, int contiguous, int* bh, int* v) {
+  const int chunk = (n + 7) >> 3, loc = wg >> 3;
+  *bh = loc / chunk;
+  const int s = loc - *bh * chunk, x = ((wg & 7) + *bh / G) & 7;
+  if (contiguous) {
+    const int first = (int)((int64_t)x * n >> 3), end = (int)((int64_t)(x + 1) * n >> 3);
+    *v = first + s;
+    return *v < end;
+  }
+  *v = 8 * s + x;
+  return *v < n;
+}
+
+struct GradArgs {
+  const bf16 *x, *y, *a, *b;  // streamed and kept tensors
+  Lay lx, ly, la, lb;
+  const bf16* out;            // queries kept: the attention's output, for D
+  const float* lse;
+  float *lse2, *delta;        // [B H][nq padded to kRows]: lse log2(e), D (inf and 0 past the lengths)
+  bf16 *g0, *g1;
+  Lay lg0, lg1;
+  float* part;                // [heads][places][kRows][2][d]
+  float* rpart;               // queries kept: [heads][places][kRows], then D as it starts
+  Parts parts;
+  int contiguous;
+  float sl2;
+};
+
+template <int D, bool KEYS>
+__global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
+  constexpr int KK = D / 32, DT = D / 16, RB = 2 * D, TILE = KT * RB;
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
+  __shared__ __attribute__((aligned(16))) float rows[KEYS ? 2 : 1][2][KEYS ? KT : 4];
+  const int nitem = g.parts.items();
+  int hx, v;  // the kept tensors' head
+  if (!item_of(blockIdx.x, nitem, KEYS ? 1 : P.G, g.contiguous, &hx, &v)) return;
+  int blk, part, parts, place;
+  g.parts.at(v, &blk, &part, &parts, &place);
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, gr = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int HX = KEYS ? P.Hk : P.H;
+  const int b = hx / HX, lq = P.qlen(b), lk = P.klen(b), off = lk - lq;
+  const int n = KEYS ? lk : lq, nmax = KEYS ? P.nk : P.nq, r0 = blk * kRows;
+  const int real = max(0, min(kRows, n - r0));
+  const int nqp = (P.nq + kRows - 1) / kRows * kRows;
+
+  // the tiles that one of the block's rows sees
+  TileList list{0, 0, 0};
+  int first = 0, per_head = 1, ntile = 0;
+  if (real > 0) {
+    if constexpr (KEYS) {
+      const int i0 = max(0, seeing_positions(P.m, r0).lo - off);
+      const int hi = r0 < P.m.sinks ? kUnlimited : seeing_positions(P.m, r0 + real - 1).hi;
+      const int i1 = min(lq, hi - off + 1);
+      if (i1 > i0) {
+        first = i0 / KT;
+        per_head = (i1 + KT - 1) / KT - first;
+        ntile = per_head * P.G;
+      }
+    } else {
+      list = visible_tiles<KT>(P.m, r0 + off, r0 + real - 1 + off, lk);
+      ntile = list.n;
+    }
+  }
+  const int per = (ntile + parts - 1) / parts;
+  const int t0 = min(ntile, part * per), t1 = min(ntile, t0 + per);
+
+  // this wavefront's rows, and this lane's
+  const int w0 = r0 + 16 * w, wreal = max(0, min(16, n - w0));
+  const int row = min(w0 + min(l16, max(wreal, 1) - 1), nmax - 1);
+  KeyRange ra, rz;       // queries kept: of the first and last row
+  int plo0, plo1, phi0, phi1;  // keys kept: least and greatest bounds of their positions
+  if constexpr (KEYS) {
+    const int last = w0 + max(wreal, 1) - 1;
+    plo0 = seeing_positions(P.m, w0).lo;
+    plo1 = seeing_positions(P.m, last).lo;
+    phi0 = last < P.m.sinks ? kUnlimited : max(w0, P.m.sinks) + P.m.left;
+    phi1 = w0 < P.m.sinks ? kUnlimited : last + P.m.left;
+  } else {
+    ra = visible_keys(P.m, w0 + off, lk);
+    rz = visible_keys(P.m, w0 + max(wreal, 1) - 1 + off, lk);
+  }
+  // 0: no pair of the wavefront's rows and the tile's is visible, 2: all, 1: else
+  auto tile_class = [&](int s0) __attribute__((always_inline)) {
+    if (wreal == 0) return 0;
+    if constexpr (KEYS) {
+      const int p0 = s0 + off, p1 = min(s0 + KT, lq) - 1 + off;
+      if (p1 < plo0 || p0 > phi1) return 0;
+      return plo1 <= p0 && phi0 >= p1 ? 2 : 1;
+    } else {
+      if (s0 >= rz.s_end && (s0 >= rz.hi || s0 + KT <= ra.lo)) return 0;
+      return s0 + KT <= ra.s_end || (s0 >= rz.lo && s0 + KT <= ra.hi) ? 2 : 1;
+    }
+  };
+
+  bf16x8 af[KK], bf[KK];
+  float mylse = INFINITY, mydel = 0.f;
+  {
+    const bf16* ar = g.a + row_off(hx, row, g.la);
+    const bf16* br = g.b + row_off(hx, row, g.lb);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      af[kk] = *(const bf16x8*)(ar + 32 * kk + 8 * gr);
+      bf[kk] = *(const bf16x8*)(br + 32 * kk + 8 * gr);
+    }
+    if constexpr (!KEYS) {
+      const bf16* orow = g.out + row_off(hx, row, P.lo);
+      float d = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8 o = *(const bf16x8*)(orow + 32 * kk + 8 * gr);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d = fmaf(bf2f(o[j]), bf2f(bf[kk][j]), d);
+      }
+      d += __shfl_xor(d, 16, 64);
+      d += __shfl_xor(d, 32, 64);
+      const float ls = g.lse[(size_t)hx * P.nq + row];
+      if (l16 < wreal && ls != -INFINITY) {
+        mylse = ls * kLog2e;
+        mydel = d;
+      }
+    }
+  }
+  // Retire the loads here, so that no vmcnt wait of theirs lands in the loop
+  __builtin_amdgcn_s_waitcnt(kVmcnt0);
+
+  const RowCopy<RB, KT, NW> xcopy(w, lane, (uint32_t)(g.lx.sn * 2));
+  const RowCopy<RB, KT, NW> ycopy(w, lane, (uint32_t)(g.ly.sn * 2));
+  const uint32_t lds0 = lds_addr(smem);
+  // head and first row of streamed tile t
+  auto where = [&](int t, int* h, int* s0) __attribute__((always_inline)) {
+    if constexpr (KEYS) {
+      const int gh = t / per_head;
+      *h = b * P.H + (hx - b * P.Hk) * P.G + gh;
+      *s0 = KT * (first + t - gh * per_head);
+    } else {
+      *h = b * P.Hk + (hx - b * P.H) / P.G;
+      *s0 = KT * list.tile(t);
+    }
+  };
+  auto issue = [&](int t, int buf) __attribute__((always_inline)) {
+    int h, s0;
+    where(t, &h, &s0);
+    const int last = (KEYS ? lq : lk) - 1 - s0;
+    xcopy.issue(g.x + row_off(h, s0, g.lx), lds0 + buf * TILE, w, lane, last);
+    ycopy.issue(g.y + row_off(h, s0, g.ly), lds0 + (2 + buf) * TILE, w, lane, last);
+    if constexpr (KEYS) {  // the rows' lse and D, 256 bytes each
+      const size_t at = (size_t)h * nqp + s0;
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(&rows[buf][w & 1][0]));
+      if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
+    }
+  };
+  int xoff[KK], coff[DT];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    xoff[kk] = l16 * RB + (((4 * kk + gr) ^ row_key<RB>(l16)) << 4);
+  // transposing read of dims 16 dt .. + 15, rows 4 gr .. + 3 of a 16-row tile
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    const int r = 4 * gr + (l16 >> 2), lc = 2 * dt + ((l16 & 3) >> 1);
+    coff[dt] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (l16 & 1);
+  }
+
+  f32x4 acc0[DT], acc1[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc0[dt] = acc1[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float rsum = 0.f;
+
+  auto compute = [&](auto buf_tag, int t) __attribute__((always_inline)) {
+    constexpr int BUF = decltype(buf_tag)::value;
+    int h, s0;
+    where(t, &h, &s0);
+    const int c = tile_class(s0);
+    if (c == 0) return;
+    const char* xs = smem + BUF * TILE;
+    const char* ys = smem + (2 + BUF) * TILE;
+    f32x4 s[4], e[4], ls[4];
+#pragma unroll
+    for (int T = 0; T < 4; ++T) {
+      s[T] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (KEYS) {
+        ls[T] = *(const f32x4*)&rows[BUF][0][16 * T + 4 * gr];
+        const f32x4 d = *(const f32x4*)&rows[BUF][1][16 * T + 4 * gr];
+        e[T] = f32x4{-d[0], -d[1], -d[2], -d[3]};
+      } else {
+        ls[T] = f32x4{mylse, mylse, mylse, mylse};
+        e[T] = f32x4{-mydel, -mydel, -mydel, -mydel};
+      }
+    }
+#pragma unroll
+    for (int T = 0; T < 4; ++T)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8 xv = *(const bf16x8*)(xs + 16 * T * RB + xoff[kk]);
+        s[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, af[kk], s[T], 0, 0, 0);
+        const bf16x8 yv = *(const bf16x8*)(ys + 16 * T * RB + xoff[kk]);
+        e[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yv, bf[kk], e[T], 0, 0, 0);
+      }
+    if (c == 1) {
+      // element r of tile T is streamed row s0 + 16 T + 4 gr + r
+      int rw = row;
+      asm volatile("" : "+v"(rw));
+      if constexpr (KEYS) {
+        const PosRange see = seeing_positions(P.m, rw);
+        const uint32_t len = (uint32_t)max(0, see.hi - see.lo + 1);
+        const int p0 = s0 + off + 4 * gr - see.lo;
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((uint32_t)(p0 + 16 * T + r) >= len) {
+              s[T][r] = -INFINITY;
+              e[T][r] = 0.f;
+            }
+      } else {
+        const KeyRange rr = visible_keys(P.m, rw + off, lk);
+        const uint32_t len = (uint32_t)max(0, rr.hi - rr.lo);
+        const int a0 = s0 + 4 * gr - rr.lo, b0 = rr.s_end - s0 - 4 * gr;
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!((uint32_t)(a0 + 16 * T + r) < len || 16 * T + r < b0)) {
+              s[T][r] = -INFINITY;
+              e[T][r] = 0.f;
+            }
+      }
+    }
+    // two 16-row tiles make one operand of 32 rows: element j of lane group gr
+    // is row 16 (j / 4) + 4 gr + j % 4
+#pragma unroll
+    for (int U = 0; U < 2; ++U) {
+      float p[8], ds[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int T = 2 * U + (j >> 2), r = j & 3;
+        p[j] = __builtin_amdgcn_exp2f(fmaf(s[T][r], g.sl2, -ls[T][r]));
+        ds[j] = p[j] * e[T][r];
+      }
+      const bf16x8 pp = pack8(p), dd = pack8(ds);
+      if constexpr (!KEYS) rsum = sum8(dd, rsum);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const char* at = xs + 32 * U * RB + coff[dt];
+        const bf16x8 xt = read_cols(at, at + 16 * RB);
+        acc0[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt, dd, acc0[dt], 0, 0, 0);
+        if constexpr (KEYS) {
+          const char* yt = ys + 32 * U * RB + coff[dt];
+          acc1[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_cols(yt, yt + 16 * RB), pp,
+                                                             acc1[dt], 0, 0, 0);
+        } else {
+          acc1[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt, pp, acc1[dt], 0, 0, 0);
+        }
+      }
+    }
+  };
+  // One barrier a tile: behind it tile t's copies have landed and every
+  // wavefront is past tile t - 1, whose buffers take tile t + 1.
+  auto step = [&](auto buf_tag, int t) __attribute__((always_inline)) {
+    constexpr int BUF = decltype(buf_tag)::value;
+    wait_vmcnt<0>();
+    wait_lgkm();
+    raw_barrier();
+    if (t + 1 < t1) issue(t + 1, BUF ^ 1);
+    compute(buf_tag, t);
+  };
+  if (t0 < t1) {
+    issue(t0, 0);
+    for (int t = t0; t < t1; t += 2) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1);
+    }
+  }
+
+  const int rout = w0 + l16;  // accumulators: row l % 16, dims 16 dt + 4 gr + r
+  if (!KEYS) {
+    rsum += __shfl_xor(rsum, 16, 64);
+    rsum += __shfl_xor(rsum, 32, 64);
+  }
+  if (parts > 1) {
+    const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + 16 * w + l16;
+    float* p = g.part + slot * 2 * D;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      *(f32x4*)(p + 16 * dt + 4 * gr) = acc0[dt];
+      *(f32x4*)(p + D + 16 * dt + 4 * gr) = acc1[dt];
+    }
+    if (!KEYS && gr == 0) {
+      g.rpart[slot] = rsum;
+      if (part == 0) {
+        g.lse2[(size_t)hx * nqp + rout] = mylse;
+        g.delta[(size_t)hx * nqp + rout] = mydel;
+      }
+    }
+    return;
+  }
+  if (!KEYS && gr == 0) {
+    g.lse2[(size_t)hx * nqp + rout] = mylse;
+    g.delta[(size_t)hx * nqp + rout] = mydel + rsum;
+  }
+  if (rout >= nmax) return;
+  const bool on = l16 < wreal;
+  bf16* o0 = g.g0 + row_off(hx, rout, g.lg0);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    bf16x4 x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float d = KEYS ? acc0[dt][r] : acc0[dt][r] - rsum * acc1[dt][r];
+      x[r] = f2bf(on ? d * P.scale : 0.f);
+    }
+    *(bf16x4*)(o0 + 16 * dt + 4 * gr) = x;
+  }
+  if constexpr (KEYS) {
+    bf16* o1 = g.g1 + row_off(hx, rout, g.lg1);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      bf16x4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = f2bf(on ? acc1[dt][r] : 0.f);
+      *(bf16x4*)(o1 + 16 * dt + 4 * gr) = x;
+    }
+  }
+}
+
+// Adds up the parts of the blocks that were cut, in order: 32 lanes a row.
+template <int D, bool KEYS>
+__global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, const GradArgs g,
+                                                               int ncut, int first_cut) {
+  constexpr int E = D / 32;  // elements of a lane
+  const int HX = KEYS ? P.Hk : P.H, nmax = KEYS ? P.nk : P.nq;
+  const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const int64_t rows = (int64_t)ncut * kRows;
+  const int hx = (int)(id / rows), x = (int)(id - hx * rows);
+  if (hx >= P.B * HX) return;
+  const int blk = first_cut + x / kRows, r = blk * kRows + x % kRows, b = hx / HX;
+  const bool sink = blk < g.parts.nsink;
+  const int parts = sink ? g.parts.psink : g.parts.p;
+  const int place = sink ? blk * parts
+                         : (g.parts.psink > 1 ? g.parts.nsink * g.parts.psink : 0) +
+                               (blk - g.parts.nsink) * parts;
+  const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + x % kRows;
+  float a0[E], a1[E], rs = 0.f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) a0[i] = a1[i] = 0.f;
+  for (int p = 0; p < parts; ++p) {
+    const float* q = g.part + (slot + (size_t)p * kRows) * 2 * D + lane;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      a0[i] += q[32 * i];
+      a1[i] += q[D + 32 * i];
+    }
+    if (!KEYS) rs += g.rpart[slot + (size_t)p * kRows];
+  }
+  const bool on = r < (KEYS ? P.klen(b) : P.qlen(b));
+  if (!KEYS && lane == 0) {
+    const int nqp = (P.nq + kRows - 1) / kRows * kRows;
+    if (on) g.delta[(size_t)hx * nqp + r] += rs;
+  }
+  if (r >= nmax) return;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float d = KEYS ? a0[i] : a0[i] - rs * a1[i];
+    g.g0[row_off(hx, r, g.lg0) + lane + 32 * i] = f2bf(on ? d * P.scale : 0.f);
+    if (KEYS) g.g1[row_off(hx, r, g.lg1) + lane + 32 * i] = f2bf(on ? a1[i] : 0.f);
+  }
+}
+
+int clamp_parts(int64_t want, int64_t room) {
+  int64_t p = want < room ? want : room;
+  p = p < 64 ? p : 64;
+  return (int)(p < 1 ? 1 : p);
+}
+
+// Parts of both kernels. A launch of fewer than 384 workgroups (256 compute
+// units, one or two workgroups each) is cut into about 512, of eight tiles at least;
+// blocks that hold sinks, whose tiles go with all queries, into parts of about
+// the other blocks' tiles, but no more than balance needs (a part costs its
+// partial sums' way through memory).
+Parts query_parts(const WinProb& P) {
+  const int nb = (P.nq + kRows - 1) / kRows;
+  const int64_t wgs = (int64_t)nb * P.B * P.H;
+  int64_t keys = (int64_t)P.m.left + P.m.right + kRows + P.m.sinks;
+  if (keys > P.nk) keys = P.nk;
+  return Parts{nb, 0, 1, wgs >= 384 ? 1 : clamp_parts((512 + wgs - 1) / wgs, keys / (8 * KT))};
+}
+Parts key_parts(const WinProb& P) {
+  const int nb = (P.nk + kRows - 1) / kRows;
+  const int64_t wgs = (int64_t)nb * P.B * P.Hk, all = (int64_t)(P.nq + KT - 1) / KT * P.G;
+  int64_t seen = ((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1;
+  seen *= P.G;
+  if (seen > all) seen = all;
+  const int p = wgs >= 384 ? 1 : clamp_parts((512 + wgs - 1) / wgs, seen / 8);
+  const int nsink = P.m.sinks < P.nk ? (P.m.sinks + kRows - 1) / kRows : nb;
+  const int64_t total = (nsink * all + (nb - nsink) * seen) * P.B * P.Hk;
+  int64_t each = (seen + p - 1) / p;
+  if (each < total / 2048) each = total / 2048;  // enough to balance the compute units
+  if (each < 16) each = 16;
+  return Parts{nb, nsink, clamp_parts((all + each - 1) / each, all), p};
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct GradPlan {
+  size_t lse2, delta, part, rpart, total;
+};
+GradPlan plan(const WinProb& P) {
+  const size_t nqp = (size_t)(P.nq + kRows - 1) / kRows * kRows, rows = (size_t)P.B * P.H * nqp;
+  // the two kernels' partial sums follow one another in the same place
+  const size_t pq = (size_t)P.B * P.H * query_parts(P).places() * kRows;
+  const size_t pk = (size_t)P.B * P.Hk * key_parts(P).places() * kRows;
+  GradPlan g;
+  g.lse2 = 0;
+  g.delta = align256(rows * 4);
+  g.rpart = g.delta + align256(rows * 4);
+  g.part = g.rpart + align256(pq * 4);
+  g.total = g.part + align256((pq > pk ? pq : pk) * 2 * P.d * 4);
+  return g;
+}
+
+template <int D, bool KEYS>
+hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
+  const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
+  hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
+                     dim3(512), 0, st, P, g);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || g.parts.places() == 0) return e;
+  const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
+  const int ncut = (g.parts.p > 1 ? g.parts.nb : g.parts.nsink) - first;
+  hipLaunchKernelGGL((window_grad_join_kernel<D, KEYS>),
+                     dim3((unsigned)(((int64_t)heads * ncut * kRows + 7) / 8)), dim3(256), 0, st, P, g,
+                     ncut, first);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t run_both(const WinProb& P, GradArgs& g, const bf16* q, const bf16* k, const bf16* v,
+                    const bf16* dout, bf16* dq, bf16* dk, bf16* dv, hipStream_t st) {
+  g.contiguous = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) < P.nk / 2;
+  g.x = k, g.lx = P.lk, g.y = v, g.ly = P.lv;
+  g.a = q, g.la = P.lq, g.b = dout, g.lb = P.ldo;
+  g.g0 = dq, g.lg0 = P.ldq, g.g1 = nullptr, g.lg1 = P.ldq;
+  g.parts = query_parts(P);
+  const hipError_t e = run_grad<D, false>(P, g, st);
+  if (e != hipSuccess) return e;
+  g.x = q, g.lx = P.lq, g.y = dout, g.ly = P.ldo;
+  g.a = k, g.la = P.lk, g.b = v, g.lb = P.lv;
+  g.g0 = dk, g.lg0 = P.ldk, g.g1 = dv, g.lg1 = P.ldv;
+  g.parts = key_parts(P);
+  return run_grad<D, true>(P, g, st);
+}
+
+}  // namespace
+
+size_t window_grad_bf16_bytes(const WinProb& P) { return plan(P).total; }
+
+hipError_t launch_window_grad_bf16(const WinProb& P, const void* q, const void* k, const void* v,
+                                   const void* out, const float* lse, const void* dout, void* dq,
+                                   void* dk, void* dv, char* ws, hipStream_t st) {
+  const GradPlan p = plan(P);
+  GradArgs g{};
+  g.out = (const bf16*)out;
+  g.lse = lse;
+  g.lse2 = (float*)(ws + p.lse2);
+  g.delta = (float*)(ws + p.delta);
+  g.part = (float*)(ws + p.part);
+  g.rpart = (float*)(ws + p.rpart);
+  g.sl2 = P.scale * kLog2e;
+  if (P.d == 64)
+    return run_both<64>(P, g, (const bf16*)q, (const bf16*)k, (const bf16*)v, (const bf16*)dout,
+                        (bf16*)dq, (bf16*)dk, (bf16*)dv, st);
+  return run_both<128>(P, g, (const bf16*)q, (const bf16*)k, (const bf16*)v, (const bf16*)dout,
+                       (bf16*)dq, (bf16*)dk, (bf16*)dv, st);
+}
+
+}  // namespace ca

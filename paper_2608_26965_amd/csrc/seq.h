@@ -83,7 +83,11 @@ hipError_t launch_window(const WinProb& P, const void* q, const void* k, const v
 size_t window_bf16_bytes(const WinProb& P);
 hipError_t launch_window_bf16(const WinProb& P, const void* q, const void* k, const void* v,
                               void* out, float* lse, char* ws, hipStream_t st);
-// Workspace of the backward pass: delta (the row sums of dout * out), fp32 [B H][nq]
+size_t window_grad_bf16_bytes(const WinProb& P);
+hipError_t launch_window_grad_bf16(const WinProb& P, const void* q, const void* k, const void* v,
+                                   const void* out, const float* lse, const void* dout, void* dq,
+                                   void* dk, void* dv, char* ws, hipStream_t st);
+// Workspace of the backward pass (fp32): delta (the row sums of dout * out), fp32 [B H][nq]
 size_t window_backward_bytes(const WinProb& P);
 hipError_t launch_window_backward(const WinProb& P, const void* q, const void* k, const void* v,
                                   const void* out, const float* lse, const void* dout, void* dq,
