@@ -139,8 +139,7 @@ struct AppendProb {
 
 hipError_t launch_append(const PagedProb& P, const AppendProb& A, const void* k, const void* v,
                          void* kp, void* vp, hipStream_t st);
-// parts that a sequence's keys are cut into, and the workspace of their partial results
-int paged_splits(const PagedProb& P);
+// workspace of the partial results of the parts that a sequence's keys are cut into
 size_t paged_bytes(const PagedProb& P);
 hipError_t launch_paged(const PagedProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st);
