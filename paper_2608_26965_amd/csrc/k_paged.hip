@@ -18,10 +18,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTile = 32;   // keys of a tile
-// parts of a launch whose sequences are all as long as can be, and tiles of a part
-// at least
-constexpr int kPagedParts = 2048, kPartTiles = 8;
-constexpr int kJoin = 256;  // threads of the joining kernel
+constexpr int kPartTiles = 8;  // tiles of a part, at least
+constexpr int kJoin = 1024;  // threads of the joining kernel
 
 // The keys that the token of a sequence of len keys sees, and their tiles
 struct SeenKeys {
@@ -104,11 +102,16 @@ struct PagedKeys {
 // g0 + 15 of its group. Parts that a sequence does not have end at once.
 struct PartOf {
   int b, hk, g0, rows, sp;
+  // Parts go slowest and the heads rotate with them: workgroup i runs on XCD
+  // i % 8, and with a sequence's parts on neighbouring workgroups the XCDs that
+  // hold the late parts had only the longest sequences (32 sequences of 512 to
+  // 32,768, eight parts: 451 us, now 240).
   __device__ __forceinline__ PartOf(const PagedProb& P, int splits) {
-    const int qt = (P.G + 15) / 16;
-    sp = blockIdx.x % splits;
-    g0 = 16 * (blockIdx.x / splits % qt);
-    const int bk = blockIdx.x / splits / qt;
+    const int qt = (P.G + 15) / 16, heads = P.B * P.Hk;
+    const int s = blockIdx.x / heads, x = blockIdx.x - s * heads;
+    sp = s / qt;
+    g0 = 16 * (s - sp * qt);
+    const int bk = (x + sp) % heads;
     b = bk / P.Hk;
     hk = bk - b * P.Hk;
     rows = min(16, P.G - g0);
@@ -415,7 +418,9 @@ __global__ __launch_bounds__(64 * paged_waves<D>(), 1) void paged_bf16_kernel(
 
 // ---- joining the parts -----------------------------------------------------------------
 
-// One workgroup a head: its wavefronts take every fourth part, lanes the dims.
+// One workgroup a head: its wavefronts take every sixteenth part, lanes the dims (a
+// few heads of many parts: with four wavefronts joining 128 parts of 16 heads took
+// 10 us longer).
 template <typename T>
 __global__ __launch_bounds__(kJoin) void paged_join_kernel(const PagedProb P,
                                                            const float* __restrict__ part,
@@ -475,7 +480,13 @@ PagedPlan paged_plan(const PagedProb& P) {
   if (P.left < kNoWindow && (int64_t)P.left + 1 + P.sinks < most) seen = (int64_t)P.left + 1 + P.sinks;
   const int64_t all = (seen + kTile - 1) / kTile + 2;  // a window may begin and end inside a tile
   const int64_t wgs = (int64_t)P.B * P.Hk * ((P.G + 15) / 16);
-  int64_t tiles = (all * wgs + kPagedParts - 1) / kPagedParts;
+  // Workgroups of the launch if all sequences are as long as can be. Many
+  // sequences often have different lengths and balance in smaller parts (32 of 512 to
+  // 32,768: 276 us with 2,048, 239 with 4,096), few pay more for their joining
+  // (one of 262,144 with 16 heads: 203 and 210; four with 40 heads and 6,240 keys in
+  // the window: 114 and 119).
+  const int parts = P.B >= 8 ? 4096 : 2048;
+  int64_t tiles = (all * wgs + parts - 1) / parts;
   if (tiles < kPartTiles) tiles = kPartTiles;
   if (all <= tiles + 2) return PagedPlan{1, (int)all};
   return PagedPlan{(int)((all + tiles - 1) / tiles), (int)tiles};

@@ -63,26 +63,31 @@ def _sizes(t, layout, name):
     return tuple(s)
 
 
-def _stride(size, stride):
-    # the stride of a dimension of one element is never used
-    return stride if size > 1 else 0
-
-
 def _strides(t, layout):
-    """(batch, head, token) element strides."""
-    s, z = t.stride(), t.shape
+    """(batch, head, token) element strides (0 where there is one: never used)."""
+    a, b, c, _ = t.stride()
+    x, y, z, _ = t.shape
     if layout == "bnhd":
-        return _I64x3(_stride(z[0], s[0]), _stride(z[2], s[2]), _stride(z[1], s[1]))
-    return _I64x3(_stride(z[0], s[0]), _stride(z[1], s[1]), _stride(z[2], s[2]))
+        b, c, y, z = c, b, z, y
+    return _I64x3(a if x > 1 else 0, b if y > 1 else 0, c if z > 1 else 0)
 
 
-def _strides_of(t, n):
-    s, z = t.stride(), t.shape
-    return (ctypes.c_int64 * n)(*(_stride(z[i], s[i]) for i in range(n)))
+def _lead(t):
+    """The strides of a tensor's first three (four dimensions) or two (three)."""
+    if t.dim() == 4:
+        return _strides(t, "bhnd")
+    a, b, _ = t.stride()
+    x, y, _ = t.shape
+    return _I64x2(a if x > 1 else 0, b if y > 1 else 0)
+
+
+def _new(t):
+    """A dense tensor of t's shape."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _expect(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:  # (a torch.Size compares with a tuple)
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
@@ -98,11 +103,13 @@ def _call(name, device, *args):
     """The library's call on the current stream of `device`, made the current
     device for the launch."""
     f = getattr(_lib.load(), name)
-    if device.index == torch.cuda.current_device():
-        st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    i = device.index
+    if i == torch.cuda.current_device():
+        # the handle alone: a torch.cuda.Stream object costs 2 us of a small call's 12
+        st = f(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
-        with torch.cuda.device(device):
-            st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(i):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(i))
     if st:
         _lib.check(st, name)
 
@@ -177,7 +184,7 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     B, H, n, d = _sizes(q, layout, "q")
     axes, section, freq = r._c
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _new(q)
     else:
         _same(q_out, q, "q_out")
         _rows(q_out, "q_out", 4)
@@ -190,7 +197,7 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
         if (Bk, nk, dk) != (B, n, d):
             raise ValueError("q and k must have the same batch, tokens and head dimension")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            k_out = _new(k)
         else:
             _same(k_out, q, "k_out")
             _rows(k_out, "k_out", 4)
@@ -263,7 +270,7 @@ def _window(w, q, k, v, out, scale, len_q, len_k, layout, grads=()):
 def _lse(q, layout):
     z = q.shape
     H, n = (z[2], z[1]) if layout == "bnhd" else (z[1], z[2])
-    return torch.empty(z[0], H, n, dtype=torch.float32, device=q.device)
+    return q.new_empty((z[0], H, n), dtype=torch.float32)
 
 
 def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layout="bhnd",
@@ -274,7 +281,7 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
     lengths in a padded batch. Returns (out, lse [B,H,nq] fp32 or None); rows
     that see no key, and rows past len_q, are 0 with lse -inf."""
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(q)
     c = _window(w, q, k, v, out, scale, len_q, len_k, layout)
     lse = _lse(q, layout) if want_lse else None
     ws = _workspace("ca_window_workspace_size", c, 0, device=q.device, ws=ws)
@@ -289,8 +296,7 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     dout, from out and lse as window_attn gave them for the same arguments.
     dq, dk, dv: outputs of the inputs' shapes (any strides, for example slices
     of a fused projection's gradient), new dense tensors by default."""
-    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
-    dq, dk, dv = (new(t) if g is None else g for t, g in ((q, dq), (k, dk), (v, dv)))
+    dq, dk, dv = (_new(t) if g is None else g for t, g in ((q, dq), (k, dk), (v, dv)))
     for t, like, name in ((dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
         _same(t, q, name)
         _rows(t, name, 4)
@@ -327,8 +333,8 @@ def _paged(q, heads, k_pages, v_pages, table, lens, left, sinks, scale, q_st=Non
     z3, z2 = _I64x3(), _I64x2()
     return _lib.CaPaged(B, heads, Hk, d, dt, page, P, table.shape[1], left, sinks,
                         0.0 if scale is None else float(scale),
-                        table.stride(0) if B > 1 else 0, _strides_of(k_pages, 3),
-                        _strides_of(v_pages, 3), q_st or z2, o_st or z2, n_new, kn or z3, vn or z3)
+                        table.stride(0) if B > 1 else 0, _lead(k_pages),
+                        _lead(v_pages), q_st or z2, o_st or z2, n_new, kn or z3, vn or z3)
 
 
 def cache_append(k, v, k_pages, v_pages, page_table, lens):
@@ -343,7 +349,7 @@ def cache_append(k, v, k_pages, v_pages, page_table, lens):
     if k_pages.dim() == 4 and k.shape[2] != k_pages.shape[2]:
         raise ValueError(f"expected {k_pages.shape[2]} key heads, got {k.shape[2]}")
     c = _paged(k, k.shape[2], k_pages, v_pages, page_table, lens, -1, 0, None, n_new=k.shape[1],
-               kn=_strides_of(k, 3), vn=_strides_of(v, 3))
+               kn=_lead(k), vn=_lead(v))
     _call("ca_cache_append", k.device, c, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
           v_pages.data_ptr(), page_table.data_ptr(), lens.data_ptr())
 
@@ -358,15 +364,15 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     None); a sequence of no tokens gives 0 and -inf."""
     _rows(q, "q", 3)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(q)
     else:
         _same(out, q, "out")
         _rows(out, "out", 3)
         _expect(out, q.shape, "out")
     B, H = q.shape[0], q.shape[1]
-    c = _paged(q, H, k_pages, v_pages, page_table, lens, left, sinks, scale, _strides_of(q, 2),
-               _strides_of(out, 2))
-    lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
+    c = _paged(q, H, k_pages, v_pages, page_table, lens, left, sinks, scale, _lead(q),
+               _lead(out))
+    lse = q.new_empty((B, H), dtype=torch.float32) if want_lse else None
     ws = _workspace("ca_paged_workspace_size", c, device=q.device, ws=ws)
     _call("ca_paged_attn", q.device, c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
           page_table.data_ptr(), lens.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(ws),
