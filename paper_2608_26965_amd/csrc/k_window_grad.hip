@@ -36,7 +36,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
 constexpr int kRows = 128;       // kept rows of a workgroup
 constexpr int KT = 64;           // streamed rows of a tile
-constexpr int NW = 8;
+constexpr int NW = 4;
 
 // Row blocks and the parts that their streamed tiles are cut into. Blocks 0 ..
 // nsink - 1 are cut into `psink` parts (keys kept: the blocks that hold sinks,
@@ -98,8 +98,8 @@ struct GradArgs {
 };
 
 template <int D, bool KEYS>
-__global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
-  constexpr int KK = D / 32, DT = D / 16, RB = 2 * D, TILE = KT * RB;
+__global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel(const WinProb P, const GradArgs g) {
+  constexpr int KK = D / 16, DT = D / 32, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
   __shared__ __attribute__((aligned(16))) float rows[KEYS ? 2 : 1][2][KEYS ? KT : 4];
   const int nitem = g.parts.items();
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
   if (!item_of(blockIdx.x, nitem, KEYS ? 1 : P.G, g.contiguous, &hx, &v)) return;
   int blk, part, parts, place;
   g.parts.at(v, &blk, &part, &parts, &place);
-  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, gr = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int HX = KEYS ? P.Hk : P.H;
   const int b = hx / HX, lq = P.qlen(b), lk = P.klen(b), off = lk - lq;
@@ -137,8 +137,8 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
   const int t0 = min(ntile, part * per), t1 = min(ntile, t0 + per);
 
   // this wavefront's rows, and this lane's
-  const int w0 = r0 + 16 * w, wreal = max(0, min(16, n - w0));
-  const int row = min(w0 + min(l16, max(wreal, 1) - 1), nmax - 1);
+  const int w0 = r0 + 32 * w, wreal = max(0, min(32, n - w0));
+  const int row = min(w0 + min(l32, max(wreal, 1) - 1), nmax - 1);
   KeyRange ra, rz;       // queries kept: of the first and last row
   int plo0, plo1, phi0, phi1;  // keys kept: least and greatest bounds of their positions
   if constexpr (KEYS) {
@@ -171,22 +171,21 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
     const bf16* br = g.b + row_off(hx, row, g.lb);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      af[kk] = *(const bf16x8*)(ar + 32 * kk + 8 * gr);
-      bf[kk] = *(const bf16x8*)(br + 32 * kk + 8 * gr);
+      af[kk] = *(const bf16x8*)(ar + 16 * kk + 8 * h);
+      bf[kk] = *(const bf16x8*)(br + 16 * kk + 8 * h);
     }
     if constexpr (!KEYS) {
       const bf16* orow = g.out + row_off(hx, row, P.lo);
       float d = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 o = *(const bf16x8*)(orow + 32 * kk + 8 * gr);
+        const bf16x8 o = *(const bf16x8*)(orow + 16 * kk + 8 * h);
 #pragma unroll
         for (int j = 0; j < 8; ++j) d = fmaf(bf2f(o[j]), bf2f(bf[kk][j]), d);
       }
-      d += __shfl_xor(d, 16, 64);
-      d += __shfl_xor(d, 32, 64);
+      d += wave_xor32(d);
       const float ls = g.lse[(size_t)hx * P.nq + row];
-      if (l16 < wreal && ls != -INFINITY) {
+      if (l32 < wreal && ls != -INFINITY) {
         mylse = ls * kLog2e;
         mydel = d;
       }
@@ -199,131 +198,143 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
   const RowCopy<RB, KT, NW> ycopy(w, lane, (uint32_t)(g.ly.sn * 2));
   const uint32_t lds0 = lds_addr(smem);
   // head and first row of streamed tile t
-  auto where = [&](int t, int* h, int* s0) __attribute__((always_inline)) {
+  auto where = [&](int t, int* head, int* s0) __attribute__((always_inline)) {
     if constexpr (KEYS) {
       const int gh = t / per_head;
-      *h = b * P.H + (hx - b * P.Hk) * P.G + gh;
+      *head = b * P.H + (hx - b * P.Hk) * P.G + gh;
       *s0 = KT * (first + t - gh * per_head);
     } else {
-      *h = b * P.Hk + (hx - b * P.H) / P.G;
+      *head = b * P.Hk + (hx - b * P.H) / P.G;
       *s0 = KT * list.tile(t);
     }
   };
   auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-    int h, s0;
-    where(t, &h, &s0);
+    int head, s0;
+    where(t, &head, &s0);
     const int last = (KEYS ? lq : lk) - 1 - s0;
-    xcopy.issue(g.x + row_off(h, s0, g.lx), lds0 + buf * TILE, w, lane, last);
-    ycopy.issue(g.y + row_off(h, s0, g.ly), lds0 + (2 + buf) * TILE, w, lane, last);
+    xcopy.issue(g.x + row_off(head, s0, g.lx), lds0 + buf * TILE, w, lane, last);
+    ycopy.issue(g.y + row_off(head, s0, g.ly), lds0 + (2 + buf) * TILE, w, lane, last);
     if constexpr (KEYS) {  // the rows' lse and D, 256 bytes each
-      const size_t at = (size_t)h * nqp + s0;
+      const size_t at = (size_t)head * nqp + s0;
       const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(&rows[buf][w & 1][0]));
       if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
     }
   };
-  int xoff[KK], coff[DT];
+  int xoff[KK], coff[DT][2];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk)
-    xoff[kk] = l16 * RB + (((4 * kk + gr) ^ row_key<RB>(l16)) << 4);
-  // transposing read of dims 16 dt .. + 15, rows 4 gr .. + 3 of a 16-row tile
+  for (int kk = 0; kk < KK; ++kk) xoff[kk] = row_operand<RB>(lane, kk);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    const int r = 4 * gr + (l16 >> 2), lc = 2 * dt + ((l16 & 3) >> 1);
-    coff[dt] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (l16 & 1);
-  }
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) coff[dt][t] = col_operand<RB>(lane, dt, t);
 
-  f32x4 acc0[DT], acc1[DT];
+  f32x16 acc0[DT], acc1[DT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) acc0[dt] = acc1[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
   float rsum = 0.f;
 
   auto compute = [&](auto buf_tag, int t) __attribute__((always_inline)) {
     constexpr int BUF = decltype(buf_tag)::value;
-    int h, s0;
-    where(t, &h, &s0);
+    int head, s0;
+    where(t, &head, &s0);
     const int c = tile_class(s0);
     if (c == 0) return;
     const char* xs = smem + BUF * TILE;
     const char* ys = smem + (2 + BUF) * TILE;
-    f32x4 s[4], e[4], ls[4];
+    f32x16 s[2], e[2];
 #pragma unroll
-    for (int T = 0; T < 4; ++T) {
-      s[T] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
       if constexpr (KEYS) {
-        ls[T] = *(const f32x4*)&rows[BUF][0][16 * T + 4 * gr];
-        const f32x4 d = *(const f32x4*)&rows[BUF][1][16 * T + 4 * gr];
-        e[T] = f32x4{-d[0], -d[1], -d[2], -d[3]};
-      } else {
-        ls[T] = f32x4{mylse, mylse, mylse, mylse};
-        e[T] = f32x4{-mydel, -mydel, -mydel, -mydel};
-      }
-    }
 #pragma unroll
-    for (int T = 0; T < 4; ++T)
+        for (int x = 0; x < 4; ++x) {
+          const f32x4 d = *(const f32x4*)&rows[BUF][1][32 * mt + 8 * x + 4 * h];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) e[mt][4 * x + r] = -d[r];
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[mt][r] = -mydel;
+      }
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 xv = *(const bf16x8*)(xs + 16 * T * RB + xoff[kk]);
-        s[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, af[kk], s[T], 0, 0, 0);
-        const bf16x8 yv = *(const bf16x8*)(ys + 16 * T * RB + xoff[kk]);
-        e[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yv, bf[kk], e[T], 0, 0, 0);
+        const bf16x8 xv = *(const bf16x8*)(xs + 32 * mt * RB + xoff[kk]);
+        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xv, af[kk], s[mt], 0, 0, 0);
+        const bf16x8 yv = *(const bf16x8*)(ys + 32 * mt * RB + xoff[kk]);
+        e[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yv, bf[kk], e[mt], 0, 0, 0);
       }
+    }
     if (c == 1) {
-      // element r of tile T is streamed row s0 + 16 T + 4 gr + r
+      // accumulator r of row tile mt is streamed row s0 + 32 mt + 8 (r / 4) + 4 h + r % 4
       int rw = row;
       asm volatile("" : "+v"(rw));
       if constexpr (KEYS) {
         const PosRange see = seeing_positions(P.m, rw);
         const uint32_t len = (uint32_t)max(0, see.hi - see.lo + 1);
-        const int p0 = s0 + off + 4 * gr - see.lo;
+        const int p0 = s0 + off + 4 * h - see.lo;
 #pragma unroll
-        for (int T = 0; T < 4; ++T)
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if ((uint32_t)(p0 + 16 * T + r) >= len) {
-              s[T][r] = -INFINITY;
-              e[T][r] = 0.f;
+          for (int r = 0; r < 16; ++r)
+            if ((uint32_t)(p0 + 32 * mt + 8 * (r >> 2) + (r & 3)) >= len) {
+              s[mt][r] = -INFINITY;
+              e[mt][r] = 0.f;
             }
       } else {
         const KeyRange rr = visible_keys(P.m, rw + off, lk);
         const uint32_t len = (uint32_t)max(0, rr.hi - rr.lo);
-        const int a0 = s0 + 4 * gr - rr.lo, b0 = rr.s_end - s0 - 4 * gr;
+        const int a0 = s0 + 4 * h - rr.lo, b0 = rr.s_end - s0 - 4 * h;
 #pragma unroll
-        for (int T = 0; T < 4; ++T)
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (!((uint32_t)(a0 + 16 * T + r) < len || 16 * T + r < b0)) {
-              s[T][r] = -INFINITY;
-              e[T][r] = 0.f;
+          for (int r = 0; r < 16; ++r) {
+            const int x = 32 * mt + 8 * (r >> 2) + (r & 3);
+            if (!((uint32_t)(a0 + x) < len || x < b0)) {
+              s[mt][r] = -INFINITY;
+              e[mt][r] = 0.f;
             }
+          }
       }
     }
-    // two 16-row tiles make one operand of 32 rows: element j of lane group gr
-    // is row 16 (j / 4) + 4 gr + j % 4
+    // accumulators 8 u .. 8 u + 7 of a row tile are one operand (col_operand)
 #pragma unroll
-    for (int U = 0; U < 2; ++U) {
-      float p[8], ds[8];
+    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int T = 2 * U + (j >> 2), r = j & 3;
-        p[j] = __builtin_amdgcn_exp2f(fmaf(s[T][r], g.sl2, -ls[T][r]));
-        ds[j] = p[j] * e[T][r];
-      }
-      const bf16x8 pp = pack8(p), dd = pack8(ds);
-      if constexpr (!KEYS) rsum = sum8(dd, rsum);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const char* at = xs + 32 * U * RB + coff[dt];
-        const bf16x8 xt = read_cols(at, at + 16 * RB);
-        acc0[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt, dd, acc0[dt], 0, 0, 0);
+      for (int u = 0; u < 2; ++u) {
+        float p[8], ds[8];
+        float ls[8];
         if constexpr (KEYS) {
-          const char* yt = ys + 32 * U * RB + coff[dt];
-          acc1[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_cols(yt, yt + 16 * RB), pp,
-                                                             acc1[dt], 0, 0, 0);
-        } else {
-          acc1[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt, pp, acc1[dt], 0, 0, 0);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const f32x4 y = *(const f32x4*)&rows[BUF][0][32 * mt + 16 * u + 8 * x + 4 * h];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ls[4 * x + r] = y[r];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * u + j], g.sl2, KEYS ? -ls[j] : -mylse));
+          ds[j] = p[j] * e[mt][8 * u + j];
+        }
+        const bf16x8 pp = pack8(p), dd = pack8(ds);
+        if constexpr (!KEYS) rsum = sum8(dd, rsum);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const char* at = xs + (32 * mt + 16 * u) * RB;
+          const bf16x8 xt = read_cols(at + coff[dt][0], at + coff[dt][1]);
+          acc0[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xt, dd, acc0[dt], 0, 0, 0);
+          if constexpr (KEYS) {
+            const char* yt = ys + (32 * mt + 16 * u) * RB;
+            acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                read_cols(yt + coff[dt][0], yt + coff[dt][1]), pp, acc1[dt], 0, 0, 0);
+          } else {
+            acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xt, pp, acc1[dt], 0, 0, 0);
+          }
         }
       }
-    }
   };
   // One barrier a tile: behind it tile t's copies have landed and every
   // wavefront is past tile t - 1, whose buffers take tile t + 1.
@@ -343,20 +354,26 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
     }
   }
 
-  const int rout = w0 + l16;  // accumulators: row l % 16, dims 16 dt + 4 gr + r
-  if (!KEYS) {
-    rsum += __shfl_xor(rsum, 16, 64);
-    rsum += __shfl_xor(rsum, 32, 64);
-  }
+  const int rout = w0 + l32;  // accumulators: row l % 32, dims 32 dt + 8 x + 4 h + r
+  if (!KEYS) rsum += wave_xor32(rsum);
+  auto dims = [&](int dt, int x) { return 32 * dt + 8 * x + 4 * h; };
   if (parts > 1) {
-    const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + 16 * w + l16;
+    const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + 32 * w + l32;
     float* p = g.part + slot * 2 * D;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      *(f32x4*)(p + 16 * dt + 4 * gr) = acc0[dt];
-      *(f32x4*)(p + D + 16 * dt + 4 * gr) = acc1[dt];
-    }
-    if (!KEYS && gr == 0) {
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        f32x4 a, c;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          a[r] = acc0[dt][4 * x + r];
+          c[r] = acc1[dt][4 * x + r];
+        }
+        *(f32x4*)(p + dims(dt, x)) = a;
+        *(f32x4*)(p + D + dims(dt, x)) = c;
+      }
+    if (!KEYS && h == 0) {
       g.rpart[slot] = rsum;
       if (part == 0) {
         g.lse2[(size_t)hx * nqp + rout] = mylse;
@@ -365,32 +382,36 @@ __global__ __launch_bounds__(512, 2) void window_grad_kernel(const WinProb P, co
     }
     return;
   }
-  if (!KEYS && gr == 0) {
+  if (!KEYS && h == 0) {
     g.lse2[(size_t)hx * nqp + rout] = mylse;
     g.delta[(size_t)hx * nqp + rout] = mydel + rsum;
   }
   if (rout >= nmax) return;
-  const bool on = l16 < wreal;
+  const bool on = l32 < wreal;
   bf16* o0 = g.g0 + row_off(hx, rout, g.lg0);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    bf16x4 x;
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float d = KEYS ? acc0[dt][r] : acc0[dt][r] - rsum * acc1[dt][r];
-      x[r] = f2bf(on ? d * P.scale : 0.f);
+    for (int x = 0; x < 4; ++x) {
+      bf16x4 y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float a = acc0[dt][4 * x + r], d = KEYS ? a : a - rsum * acc1[dt][4 * x + r];
+        y[r] = f2bf(on ? d * P.scale : 0.f);
+      }
+      *(bf16x4*)(o0 + dims(dt, x)) = y;
     }
-    *(bf16x4*)(o0 + 16 * dt + 4 * gr) = x;
-  }
   if constexpr (KEYS) {
     bf16* o1 = g.g1 + row_off(hx, rout, g.lg1);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      bf16x4 x;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = f2bf(on ? acc1[dt][r] : 0.f);
-      *(bf16x4*)(o1 + 16 * dt + 4 * gr) = x;
-    }
+      for (int x = 0; x < 4; ++x) {
+        bf16x4 y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][4 * x + r] : 0.f);
+        *(bf16x4*)(o1 + dims(dt, x)) = y;
+      }
   }
 }
 
@@ -494,7 +515,7 @@ template <int D, bool KEYS>
 hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
   const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
   hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
-                     dim3(512), 0, st, P, g);
+                     dim3(64 * NW), 0, st, P, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts.places() == 0) return e;
   const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
