@@ -197,25 +197,38 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
   const RowCopy<RB, KT, NW> xcopy(w, lane, (uint32_t)(g.lx.sn * 2));
   const RowCopy<RB, KT, NW> ycopy(w, lane, (uint32_t)(g.ly.sn * 2));
   const uint32_t lds0 = lds_addr(smem);
-  // head and first row of streamed tile t
-  auto where = [&](int t, int* head, int* s0) __attribute__((always_inline)) {
+  // The walk over the streamed tiles: keys kept, query head gh of the group and its
+  // tile, the heads one after another
+  struct Walk {
+    int t, gh, tile;
+  };
+  auto start = [&](int t) {
+    Walk x{t, 0, t};
     if constexpr (KEYS) {
-      const int gh = t / per_head;
-      *head = b * P.H + (hx - b * P.Hk) * P.G + gh;
-      *s0 = KT * (first + t - gh * per_head);
-    } else {
-      *head = b * P.Hk + (hx - b * P.H) / P.G;
-      *s0 = KT * list.tile(t);
+      x.gh = t / per_head;
+      x.tile = t - x.gh * per_head;
+    }
+    return x;
+  };
+  auto advance = [&](Walk& x) __attribute__((always_inline)) {
+    ++x.t;
+    ++x.tile;
+    if (KEYS && x.tile == per_head) {
+      x.tile = 0;
+      ++x.gh;
     }
   };
-  auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-    int head, s0;
-    where(t, &head, &s0);
-    const int last = (KEYS ? lq : lk) - 1 - s0;
-    xcopy.issue(g.x + row_off(head, s0, g.lx), lds0 + buf * TILE, w, lane, last);
-    ycopy.issue(g.y + row_off(head, s0, g.ly), lds0 + (2 + buf) * TILE, w, lane, last);
+  auto first_row = [&](const Walk& x) __attribute__((always_inline)) {
+    return KT * (KEYS ? first + x.tile : list.tile(x.t));
+  };
+  const int xhead = KEYS ? b * P.H + (hx - b * P.Hk) * P.G : b * P.Hk + (hx - b * P.H) / P.G;
+  const bf16 *xbase = g.x + row_off(xhead, 0, g.lx), *ybase = g.y + row_off(xhead, 0, g.ly);
+  auto issue = [&](const Walk& x, int buf) __attribute__((always_inline)) {
+    const int s0 = first_row(x), last = (KEYS ? lq : lk) - 1 - s0;
+    xcopy.issue(xbase + x.gh * g.lx.sh + s0 * g.lx.sn, lds0 + buf * TILE, w, lane, last);
+    ycopy.issue(ybase + x.gh * g.ly.sh + s0 * g.ly.sn, lds0 + (2 + buf) * TILE, w, lane, last);
     if constexpr (KEYS) {  // the rows' lse and D, 256 bytes each
-      const size_t at = (size_t)head * nqp + s0;
+      const size_t at = (size_t)(xhead + x.gh) * nqp + s0;
       const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(&rows[buf][w & 1][0]));
       if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
     }
@@ -235,17 +248,40 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
     for (int r = 0; r < 16; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
   float rsum = 0.f;
 
-  auto compute = [&](auto buf_tag, int t) __attribute__((always_inline)) {
+  auto compute = [&](auto buf_tag, int s0) __attribute__((always_inline)) {
     constexpr int BUF = decltype(buf_tag)::value;
-    int head, s0;
-    where(t, &head, &s0);
     const int c = tile_class(s0);
     if (c == 0) return;
     const char* xs = smem + BUF * TILE;
     const char* ys = smem + (2 + BUF) * TILE;
     f32x16 s[2], e[2];
+    bf16x8 pp[2], dd[2];  // of the row tile whose products are due
+
+    // Steps, each a fence apart: the operands of the next step are read before the
+    // products of this one, which run beside some of the exponentials. (Left to
+    // itself the compiler reads each operand right before its product and waits.)
+    bf16x8 xr[2][2], yr[2][2];  // [slot][kk % 2]: rows
+    bf16x8 xc[2][2], yc[2][2];  // [slot][dt % 2]: columns
+    auto load_rows = [&](int slot, int mt, int st) __attribute__((always_inline)) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+      for (int i = 0; i < 2; ++i) {
+        xr[slot][i] = *(const bf16x8*)(xs + 32 * mt * RB + xoff[2 * st + i]);
+        yr[slot][i] = *(const bf16x8*)(ys + 32 * mt * RB + xoff[2 * st + i]);
+      }
+    };
+    auto load_cols = [&](int slot, int mt, int u, int st) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int dt = 2 * st + i;
+        const char* at = xs + (32 * mt + 16 * u) * RB;
+        xc[slot][i] = read_cols(at + coff[dt][0], at + coff[dt][1]);
+        if constexpr (KEYS) {
+          const char* yt = ys + (32 * mt + 16 * u) * RB;
+          yc[slot][i] = read_cols(yt + coff[dt][0], yt + coff[dt][1]);
+        }
+      }
+    };
+    auto begin = [&](int mt) __attribute__((always_inline)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
       if constexpr (KEYS) {
@@ -259,98 +295,152 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
 #pragma unroll
         for (int r = 0; r < 16; ++r) e[mt][r] = -mydel;
       }
+    };
+    auto logits = [&](int slot, int mt, int st) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 xv = *(const bf16x8*)(xs + 32 * mt * RB + xoff[kk]);
-        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xv, af[kk], s[mt], 0, 0, 0);
-        const bf16x8 yv = *(const bf16x8*)(ys + 32 * mt * RB + xoff[kk]);
-        e[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yv, bf[kk], e[mt], 0, 0, 0);
+      for (int i = 0; i < 2; ++i) {
+        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xr[slot][i], af[2 * st + i], s[mt], 0, 0, 0);
+        e[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yr[slot][i], bf[2 * st + i], e[mt], 0, 0, 0);
       }
-    }
-    if (c == 1) {
+    };
+    // P and dS of accumulators 8 u .. 8 u + 7: one operand (col_operand)
+    auto probs = [&](int mt, int u) __attribute__((always_inline)) {
+      float p[8], ds[8], ls[8];
+      if constexpr (KEYS) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const f32x4 y = *(const f32x4*)&rows[BUF][0][32 * mt + 16 * u + 8 * x + 4 * h];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) ls[4 * x + r] = y[r];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * u + j], g.sl2, KEYS ? -ls[j] : -mylse));
+        ds[j] = p[j] * e[mt][8 * u + j];
+      }
+      pp[u] = pack8(p);
+      dd[u] = pack8(ds);
+      if constexpr (!KEYS) rsum = sum8(dd[u], rsum);
+    };
+    auto products = [&](int slot, int u, int st) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int dt = 2 * st + i;
+        acc0[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xc[slot][i], dd[u], acc0[dt], 0, 0, 0);
+        acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(KEYS ? yc[slot][i] : xc[slot][i], pp[u],
+                                                           acc1[dt], 0, 0, 0);
+      }
+    };
+    auto mask = [&](int mt) __attribute__((always_inline)) {
       // accumulator r of row tile mt is streamed row s0 + 32 mt + 8 (r / 4) + 4 h + r % 4
       int rw = row;
       asm volatile("" : "+v"(rw));
       if constexpr (KEYS) {
         const PosRange see = seeing_positions(P.m, rw);
         const uint32_t len = (uint32_t)max(0, see.hi - see.lo + 1);
-        const int p0 = s0 + off + 4 * h - see.lo;
+        const int p0 = s0 + off + 4 * h - see.lo + 32 * mt;
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if ((uint32_t)(p0 + 32 * mt + 8 * (r >> 2) + (r & 3)) >= len) {
-              s[mt][r] = -INFINITY;
-              e[mt][r] = 0.f;
-            }
+        for (int r = 0; r < 16; ++r)
+          if ((uint32_t)(p0 + 8 * (r >> 2) + (r & 3)) >= len) {
+            s[mt][r] = -INFINITY;
+            e[mt][r] = 0.f;
+          }
       } else {
         const KeyRange rr = visible_keys(P.m, rw + off, lk);
         const uint32_t len = (uint32_t)max(0, rr.hi - rr.lo);
-        const int a0 = s0 + 4 * h - rr.lo, b0 = rr.s_end - s0 - 4 * h;
+        const int a0 = s0 + 32 * mt + 4 * h - rr.lo, b0 = rr.s_end - s0 - 32 * mt - 4 * h;
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int x = 32 * mt + 8 * (r >> 2) + (r & 3);
-            if (!((uint32_t)(a0 + x) < len || x < b0)) {
-              s[mt][r] = -INFINITY;
-              e[mt][r] = 0.f;
-            }
+        for (int r = 0; r < 16; ++r) {
+          const int x = 8 * (r >> 2) + (r & 3);
+          if (!((uint32_t)(a0 + x) < len || x < b0)) {
+            s[mt][r] = -INFINITY;
+            e[mt][r] = 0.f;
           }
+        }
+      }
+    };
+    constexpr int SR = KK / 2, SC = DT / 2;  // steps of a row tile's logits, of an operand's products
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    load_rows(0, 0, 0);
+    begin(0);
+    fence();
+#pragma unroll
+    for (int st = 0; st < SR; ++st) {
+      if (st + 1 < SR)
+        load_rows((st + 1) & 1, 0, st + 1);
+      else
+        load_rows((st + 1) & 1, 1, 0);
+      fence();
+      logits(st & 1, 0, st);
+      fence();
+    }
+    if (c == 1) mask(0);
+    begin(1);
+#pragma unroll
+    for (int st = 0; st < SR; ++st) {
+      if (st + 1 < SR)
+        load_rows((st + 1) & 1, 1, st + 1);
+      else
+        load_cols(0, 0, 0, 0);
+      fence();
+      logits(st & 1, 1, st);
+      if (st < 2) probs(0, st);
+      fence();
+    }
+    if (c == 1) mask(1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int st = 0; st < SC; ++st) {
+        const int n = u * SC + st;  // of 2 SC steps
+        if (st + 1 < SC)
+          load_cols((n + 1) & 1, 0, u, st + 1);
+        else
+          load_cols((n + 1) & 1, u ? 1 : 0, u ? 0 : 1, 0);
+        fence();
+        products(n & 1, u, st);
+        fence();
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      probs(1, u);
+#pragma unroll
+      for (int st = 0; st < SC; ++st) {
+        const int n = u * SC + st;
+        if (st + 1 < SC)
+          load_cols((n + 1) & 1, 1, u, st + 1);
+        else if (u == 0)
+          load_cols((n + 1) & 1, 1, 1, 0);
+        fence();
+        products(n & 1, u, st);
+        fence();
       }
     }
-    // accumulators 8 u .. 8 u + 7 of a row tile are one operand (col_operand)
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float p[8], ds[8];
-        float ls[8];
-        if constexpr (KEYS) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const f32x4 y = *(const f32x4*)&rows[BUF][0][32 * mt + 16 * u + 8 * x + 4 * h];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) ls[4 * x + r] = y[r];
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[j] = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * u + j], g.sl2, KEYS ? -ls[j] : -mylse));
-          ds[j] = p[j] * e[mt][8 * u + j];
-        }
-        const bf16x8 pp = pack8(p), dd = pack8(ds);
-        if constexpr (!KEYS) rsum = sum8(dd, rsum);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const char* at = xs + (32 * mt + 16 * u) * RB;
-          const bf16x8 xt = read_cols(at + coff[dt][0], at + coff[dt][1]);
-          acc0[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xt, dd, acc0[dt], 0, 0, 0);
-          if constexpr (KEYS) {
-            const char* yt = ys + (32 * mt + 16 * u) * RB;
-            acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                read_cols(yt + coff[dt][0], yt + coff[dt][1]), pp, acc1[dt], 0, 0, 0);
-          } else {
-            acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xt, pp, acc1[dt], 0, 0, 0);
-          }
-        }
-      }
   };
   // One barrier a tile: behind it tile t's copies have landed and every
   // wavefront is past tile t - 1, whose buffers take tile t + 1.
-  auto step = [&](auto buf_tag, int t) __attribute__((always_inline)) {
+  Walk next = start(t0);
+  auto step = [&](auto buf_tag, int t, int s0) __attribute__((always_inline)) {
     constexpr int BUF = decltype(buf_tag)::value;
     wait_vmcnt<0>();
     wait_lgkm();
     raw_barrier();
-    if (t + 1 < t1) issue(t + 1, BUF ^ 1);
-    compute(buf_tag, t);
+    int s1 = 0;
+    if (t + 1 < t1) {
+      advance(next);
+      s1 = first_row(next);
+      issue(next, BUF ^ 1);
+    }
+    compute(buf_tag, s0);
+    return s1;
   };
   if (t0 < t1) {
-    issue(t0, 0);
+    issue(next, 0);
+    int s0 = first_row(next);
     for (int t = t0; t < t1; t += 2) {
-      step(std::integral_constant<int, 0>{}, t);
-      if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1);
+      s0 = step(std::integral_constant<int, 0>{}, t, s0);
+      if (t + 1 < t1) s0 = step(std::integral_constant<int, 1>{}, t + 1, s0);
     }
   }
 
