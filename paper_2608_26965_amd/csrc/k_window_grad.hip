@@ -1,12 +1,12 @@
 // Gradients of attention with a sliding window and sinks, bf16, on the matrix
 // cores.
 //
-// Two kernels of one form. Each keeps 16 rows a wavefront (128 a workgroup) of
-// two tensors in registers, streams 64-row tiles of two others through LDS
-// (row_tile.h) and forms per tile, with P = e^{s - lse},
-//     S = X A^T,  E = Y B^T - D,  dS = P E
-// on 16x16x32 products, whose output (a lane holds one kept row and four
-// streamed rows of every 16) is the next product's operand as it stands:
+// Two kernels of one form. Each keeps 128 rows a workgroup of two tensors in
+// registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
+// per tile, with P = e^{s - lse},
+//     S = X A^T,  E = Y B^T - D,  dS = P E,
+// whose accumulators (a lane holds one kept row and several streamed ones) are the
+// next products' operand as they stand:
 //   queries kept (A = q, B = dout), keys streamed (X = k, Y = v):
 //     dq += dS k            and the mean key  kbar += P k
 //   keys kept (A = k, B = v), queries streamed (X = q, Y = dout):
@@ -36,7 +36,36 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
 constexpr int kRows = 128;       // kept rows of a workgroup
 constexpr int KT = 64;           // streamed rows of a tile
-constexpr int NW = 4;
+
+// Kept rows of a wavefront: 32 at d = 64, 16 at d = 128, where the operands and sums of
+// 32 take more than the 256 registers that two waves a SIMD have (one wave with 512,
+// half of them accumulation registers that its operands are copied through, took 793 us
+// for the padded batch of three, 16 rows 726; at d = 64 16 rows took 187 us for 8,192
+// tokens, 32 rows 168).
+template <int D>
+constexpr int grad_rows() {
+  return D == 64 ? 32 : 16;
+}
+// A product of W kept rows: W x W x K, accumulator r of a lane being row 8 (r / 4) + 4 g
+// + r % 4 (g = lane / W) of kept row lane % W
+template <int W>
+struct Mma;
+template <>
+struct Mma<32> {
+  typedef f32x16 Acc;
+  static constexpr int K = 16, N = 16;
+  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<16> {
+  typedef f32x4 Acc;
+  static constexpr int K = 32, N = 4;
+  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
 
 // Row blocks and the parts that their streamed tiles are cut into. Blocks 0 ..
 // nsink - 1 are cut into `psink` parts (keys kept: the blocks that hold sinks,
@@ -98,8 +127,10 @@ struct GradArgs {
 };
 
 template <int D, bool KEYS>
-__global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel(const WinProb P, const GradArgs g) {
-  constexpr int KK = D / 16, DT = D / 32, RB = 2 * D, TILE = KT * RB;
+__global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
+  constexpr int W = grad_rows<D>(), NW = kRows / W;
+  typedef Mma<W> M;
+  constexpr int KK = D / M::K, DT = D / W, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
   __shared__ __attribute__((aligned(16))) float rows[KEYS ? 2 : 1][2][KEYS ? KT : 4];
   const int nitem = g.parts.items();
@@ -107,7 +138,7 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
   if (!item_of(blockIdx.x, nitem, KEYS ? 1 : P.G, g.contiguous, &hx, &v)) return;
   int blk, part, parts, place;
   g.parts.at(v, &blk, &part, &parts, &place);
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, lw = lane % W, gr = lane / W;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int HX = KEYS ? P.Hk : P.H;
   const int b = hx / HX, lq = P.qlen(b), lk = P.klen(b), off = lk - lq;
@@ -137,8 +168,8 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
   const int t0 = min(ntile, part * per), t1 = min(ntile, t0 + per);
 
   // this wavefront's rows, and this lane's
-  const int w0 = r0 + 32 * w, wreal = max(0, min(32, n - w0));
-  const int row = min(w0 + min(l32, max(wreal, 1) - 1), nmax - 1);
+  const int w0 = r0 + W * w, wreal = max(0, min(W, n - w0));
+  const int row = min(w0 + min(lw, max(wreal, 1) - 1), nmax - 1);
   KeyRange ra, rz;       // queries kept: of the first and last row
   int plo0, plo1, phi0, phi1;  // keys kept: least and greatest bounds of their positions
   if constexpr (KEYS) {
@@ -171,21 +202,22 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
     const bf16* br = g.b + row_off(hx, row, g.lb);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      af[kk] = *(const bf16x8*)(ar + 16 * kk + 8 * h);
-      bf[kk] = *(const bf16x8*)(br + 16 * kk + 8 * h);
+      af[kk] = *(const bf16x8*)(ar + M::K * kk + 8 * gr);
+      bf[kk] = *(const bf16x8*)(br + M::K * kk + 8 * gr);
     }
     if constexpr (!KEYS) {
       const bf16* orow = g.out + row_off(hx, row, P.lo);
       float d = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 o = *(const bf16x8*)(orow + 16 * kk + 8 * h);
+        const bf16x8 o = *(const bf16x8*)(orow + M::K * kk + 8 * gr);
 #pragma unroll
         for (int j = 0; j < 8; ++j) d = fmaf(bf2f(o[j]), bf2f(bf[kk][j]), d);
       }
-      d += wave_xor32(d);
+      if (W == 16) d += __shfl_xor(d, 16, 64);
+      d += __shfl_xor(d, 32, 64);
       const float ls = g.lse[(size_t)hx * P.nq + row];
-      if (l32 < wreal && ls != -INFINITY) {
+      if (lw < wreal && ls != -INFINITY) {
         mylse = ls * kLog2e;
         mydel = d;
       }
@@ -233,19 +265,32 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
       if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
     }
   };
+  // Operand offsets. Rows: this lane's chunk of row l % W of a row tile. Columns: its
+  // pieces in the two transposing reads that make an operand of M::K streamed rows
+  // whose other operand is 8 accumulators: W = 32, accumulators 8 u .. 8 u + 7 of a row
+  // tile (col_operand); W = 16, two row tiles, element j being row 16 (j / 4) + 4 g + j % 4.
   int xoff[KK], coff[DT][2];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk) xoff[kk] = row_operand<RB>(lane, kk);
+  for (int kk = 0; kk < KK; ++kk)
+    xoff[kk] = lw * RB + (((M::K / 8 * kk + gr) ^ row_key<RB>(lw)) << 4);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt) {
+    if constexpr (W == 32) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) coff[dt][t] = col_operand<RB>(lane, dt, t);
+      for (int t = 0; t < 2; ++t) coff[dt][t] = col_operand<RB>(lane, dt, t);
+    } else {
+      const int r = 4 * gr + (lw >> 2), lc = 2 * dt + ((lw & 3) >> 1);
+      coff[dt][0] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (lw & 1);
+      coff[dt][1] = coff[dt][0] + 16 * RB;
+    }
+  }
 
-  f32x16 acc0[DT], acc1[DT];
+  typedef typename M::Acc Acc;
+  Acc acc0[DT], acc1[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
+    for (int r = 0; r < M::N; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
   float rsum = 0.f;
 
   auto compute = [&](auto buf_tag, int s0) __attribute__((always_inline)) {
@@ -254,168 +299,146 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
     if (c == 0) return;
     const char* xs = smem + BUF * TILE;
     const char* ys = smem + (2 + BUF) * TILE;
-    f32x16 s[2], e[2];
-    bf16x8 pp[2], dd[2];  // of the row tile whose products are due
+    constexpr int RT = KT / W, NO = KT / M::K;  // row tiles, and operands of 8 accumulators
+    Acc s[RT], e[RT];
+    bf16x8 pp[NO], dd[NO];
 
-    // Steps, each a fence apart: the operands of the next step are read before the
+    // Steps, a fence apart each: the operands of the next step are read before the
     // products of this one, which run beside some of the exponentials. (Left to
     // itself the compiler reads each operand right before its product and waits.)
-    bf16x8 xr[2][2], yr[2][2];  // [slot][kk % 2]: rows
-    bf16x8 xc[2][2], yc[2][2];  // [slot][dt % 2]: columns
-    auto load_rows = [&](int slot, int mt, int st) __attribute__((always_inline)) {
+    bf16x8 xr[2][2], yr[2][2];  // [step % 2][kk % 2]: rows
+    bf16x8 xc[2][2], yc[2][2];  // [step % 2][dt % 2]: columns
+    constexpr int SR = KK / 2, SC = DT / 2;  // steps of a row tile's logits, an operand's products
+    auto load_rows = [&](int n) __attribute__((always_inline)) {  // step n: row tile n / SR
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        xr[slot][i] = *(const bf16x8*)(xs + 32 * mt * RB + xoff[2 * st + i]);
-        yr[slot][i] = *(const bf16x8*)(ys + 32 * mt * RB + xoff[2 * st + i]);
+        const int at = W * (n / SR) * RB + xoff[2 * (n % SR) + i];
+        xr[n & 1][i] = *(const bf16x8*)(xs + at);
+        yr[n & 1][i] = *(const bf16x8*)(ys + at);
       }
     };
-    auto load_cols = [&](int slot, int mt, int u, int st) __attribute__((always_inline)) {
+    auto load_cols = [&](int n) __attribute__((always_inline)) {  // step n: operand n / SC
+      const char *xo = xs + M::K * (n / SC) * RB, *yo = ys + M::K * (n / SC) * RB;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int dt = 2 * st + i;
-        const char* at = xs + (32 * mt + 16 * u) * RB;
-        xc[slot][i] = read_cols(at + coff[dt][0], at + coff[dt][1]);
-        if constexpr (KEYS) {
-          const char* yt = ys + (32 * mt + 16 * u) * RB;
-          yc[slot][i] = read_cols(yt + coff[dt][0], yt + coff[dt][1]);
+        const int dt = 2 * (n % SC) + i;
+        xc[n & 1][i] = read_cols(xo + coff[dt][0], xo + coff[dt][1]);
+        if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt][0], yo + coff[dt][1]);
+      }
+    };
+    auto begin = [&](int T) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < M::N / 4; ++x) {
+        f32x4 d = {mydel, mydel, mydel, mydel};
+        if constexpr (KEYS) d = *(const f32x4*)&rows[BUF][1][W * T + 8 * x + 4 * gr];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[T][4 * x + r] = 0.f;
+          e[T][4 * x + r] = -d[r];
         }
       }
     };
-    auto begin = [&](int mt) __attribute__((always_inline)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
-      if constexpr (KEYS) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const f32x4 d = *(const f32x4*)&rows[BUF][1][32 * mt + 8 * x + 4 * h];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) e[mt][4 * x + r] = -d[r];
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) e[mt][r] = -mydel;
-      }
-    };
-    auto logits = [&](int slot, int mt, int st) __attribute__((always_inline)) {
+    auto logits = [&](int n) __attribute__((always_inline)) {
+      const int T = n / SR;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xr[slot][i], af[2 * st + i], s[mt], 0, 0, 0);
-        e[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yr[slot][i], bf[2 * st + i], e[mt], 0, 0, 0);
+        const int kk = 2 * (n % SR) + i;
+        s[T] = M::mma(xr[n & 1][i], af[kk], s[T]);
+        e[T] = M::mma(yr[n & 1][i], bf[kk], e[T]);
       }
     };
-    // P and dS of accumulators 8 u .. 8 u + 7: one operand (col_operand)
-    auto probs = [&](int mt, int u) __attribute__((always_inline)) {
-      float p[8], ds[8], ls[8];
-      if constexpr (KEYS) {
+    auto probs = [&](int o) __attribute__((always_inline)) {
+      float p[8], ds[8];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const f32x4 y = *(const f32x4*)&rows[BUF][0][32 * mt + 16 * u + 8 * x + 4 * h];
+      for (int x = 0; x < 2; ++x) {  // four accumulators from r on of row tile T
+        const int T = W == 32 ? o / 2 : 2 * o + x, r0 = W == 32 ? 8 * (o % 2) + 4 * x : 0;
+        f32x4 ls = {mylse, mylse, mylse, mylse};
+        if constexpr (KEYS) ls = *(const f32x4*)&rows[BUF][0][W * T + 2 * r0 + 4 * gr];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) ls[4 * x + r] = y[r];
+        for (int r = 0; r < 4; ++r) {
+          p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r0 + r], g.sl2, -ls[r]));
+          ds[4 * x + r] = p[4 * x + r] * e[T][r0 + r];
         }
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        p[j] = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * u + j], g.sl2, KEYS ? -ls[j] : -mylse));
-        ds[j] = p[j] * e[mt][8 * u + j];
-      }
-      pp[u] = pack8(p);
-      dd[u] = pack8(ds);
-      if constexpr (!KEYS) rsum = sum8(dd[u], rsum);
+      pp[o] = pack8(p);
+      dd[o] = pack8(ds);
+      if constexpr (!KEYS) rsum = sum8(dd[o], rsum);
     };
-    auto products = [&](int slot, int u, int st) __attribute__((always_inline)) {
+    auto products = [&](int n) __attribute__((always_inline)) {
+      const int o = n / SC;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int dt = 2 * st + i;
-        acc0[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xc[slot][i], dd[u], acc0[dt], 0, 0, 0);
-        acc1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(KEYS ? yc[slot][i] : xc[slot][i], pp[u],
-                                                           acc1[dt], 0, 0, 0);
+        const int dt = 2 * (n % SC) + i;
+        acc0[dt] = M::mma(xc[n & 1][i], dd[o], acc0[dt]);
+        acc1[dt] = M::mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
       }
     };
-    auto mask = [&](int mt) __attribute__((always_inline)) {
-      // accumulator r of row tile mt is streamed row s0 + 32 mt + 8 (r / 4) + 4 h + r % 4
-      int rw = row;
+    // row tiles T0 .. T0 + RT / 2 - 1
+    auto mask = [&](int T0) __attribute__((always_inline)) {
+      int rw = row;  // (the ranges are formed here: kept over the loop they cost registers)
       asm volatile("" : "+v"(rw));
       if constexpr (KEYS) {
         const PosRange see = seeing_positions(P.m, rw);
         const uint32_t len = (uint32_t)max(0, see.hi - see.lo + 1);
-        const int p0 = s0 + off + 4 * h - see.lo + 32 * mt;
+        const int p0 = s0 + off + 4 * gr - see.lo;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if ((uint32_t)(p0 + 8 * (r >> 2) + (r & 3)) >= len) {
-            s[mt][r] = -INFINITY;
-            e[mt][r] = 0.f;
-          }
+        for (int T = T0; T < T0 + RT / 2; ++T)
+#pragma unroll
+          for (int r = 0; r < M::N; ++r)
+            if ((uint32_t)(p0 + W * T + 8 * (r >> 2) + (r & 3)) >= len) {
+              s[T][r] = -INFINITY;
+              e[T][r] = 0.f;
+            }
       } else {
         const KeyRange rr = visible_keys(P.m, rw + off, lk);
         const uint32_t len = (uint32_t)max(0, rr.hi - rr.lo);
-        const int a0 = s0 + 32 * mt + 4 * h - rr.lo, b0 = rr.s_end - s0 - 32 * mt - 4 * h;
+        const int a0 = s0 + 4 * gr - rr.lo, b0 = rr.s_end - s0 - 4 * gr;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int x = 8 * (r >> 2) + (r & 3);
-          if (!((uint32_t)(a0 + x) < len || x < b0)) {
-            s[mt][r] = -INFINITY;
-            e[mt][r] = 0.f;
+        for (int T = T0; T < T0 + RT / 2; ++T)
+#pragma unroll
+          for (int r = 0; r < M::N; ++r) {
+            const int x = W * T + 8 * (r >> 2) + (r & 3);
+            if (!((uint32_t)(a0 + x) < len || x < b0)) {
+              s[T][r] = -INFINITY;
+              e[T][r] = 0.f;
+            }
           }
-        }
       }
     };
-    constexpr int SR = KK / 2, SC = DT / 2;  // steps of a row tile's logits, of an operand's products
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-    load_rows(0, 0, 0);
-    begin(0);
+    load_rows(0);
+#pragma unroll
+    for (int T = 0; T < RT / 2; ++T) begin(T);
     fence();
 #pragma unroll
-    for (int st = 0; st < SR; ++st) {
-      if (st + 1 < SR)
-        load_rows((st + 1) & 1, 0, st + 1);
-      else
-        load_rows((st + 1) & 1, 1, 0);
+    for (int n = 0; n < RT * SR / 2; ++n) {
+      load_rows(n + 1);
       fence();
-      logits(st & 1, 0, st);
+      logits(n);
       fence();
     }
     if (c == 1) mask(0);
-    begin(1);
 #pragma unroll
-    for (int st = 0; st < SR; ++st) {
-      if (st + 1 < SR)
-        load_rows((st + 1) & 1, 1, st + 1);
+    for (int T = RT / 2; T < RT; ++T) begin(T);
+#pragma unroll
+    for (int n = RT * SR / 2; n < RT * SR; ++n) {
+      if (n + 1 < RT * SR)
+        load_rows(n + 1);
       else
-        load_cols(0, 0, 0, 0);
+        load_cols(0);
       fence();
-      logits(st & 1, 1, st);
-      if (st < 2) probs(0, st);
+      logits(n);
+      if (n - RT * SR / 2 < NO / 2) probs(n - RT * SR / 2);
       fence();
     }
-    if (c == 1) mask(1);
+    if (c == 1) mask(RT / 2);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int st = 0; st < SC; ++st) {
-        const int n = u * SC + st;  // of 2 SC steps
-        if (st + 1 < SC)
-          load_cols((n + 1) & 1, 0, u, st + 1);
-        else
-          load_cols((n + 1) & 1, u ? 1 : 0, u ? 0 : 1, 0);
-        fence();
-        products(n & 1, u, st);
-        fence();
-      }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      probs(1, u);
-#pragma unroll
-      for (int st = 0; st < SC; ++st) {
-        const int n = u * SC + st;
-        if (st + 1 < SC)
-          load_cols((n + 1) & 1, 1, u, st + 1);
-        else if (u == 0)
-          load_cols((n + 1) & 1, 1, 1, 0);
-        fence();
-        products(n & 1, u, st);
-        fence();
-      }
+    for (int n = 0; n < NO * SC; ++n) {
+      if (n + 1 < NO * SC) load_cols(n + 1);
+      fence();
+      products(n);
+      if (n < NO / 2) probs(NO / 2 + n);
+      fence();
     }
   };
   // One barrier a tile: behind it tile t's copies have landed and every
@@ -444,26 +467,29 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
     }
   }
 
-  const int rout = w0 + l32;  // accumulators: row l % 32, dims 32 dt + 8 x + 4 h + r
-  if (!KEYS) rsum += wave_xor32(rsum);
-  auto dims = [&](int dt, int x) { return 32 * dt + 8 * x + 4 * h; };
+  const int rout = w0 + lw;
+  if (!KEYS) {
+    if (W == 16) rsum += __shfl_xor(rsum, 16, 64);
+    rsum += __shfl_xor(rsum, 32, 64);
+  }
+  auto dims = [&](int dt, int x) { return W * dt + 8 * x + 4 * gr; };
   if (parts > 1) {
-    const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + 32 * w + l32;
+    const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + W * w + lw;
     float* p = g.part + slot * 2 * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        f32x4 a, c;
+      for (int x = 0; x < M::N / 4; ++x) {
+        f32x4 a, b4;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           a[r] = acc0[dt][4 * x + r];
-          c[r] = acc1[dt][4 * x + r];
+          b4[r] = acc1[dt][4 * x + r];
         }
         *(f32x4*)(p + dims(dt, x)) = a;
-        *(f32x4*)(p + D + dims(dt, x)) = c;
+        *(f32x4*)(p + D + dims(dt, x)) = b4;
       }
-    if (!KEYS && h == 0) {
+    if (!KEYS && gr == 0) {
       g.rpart[slot] = rsum;
       if (part == 0) {
         g.lse2[(size_t)hx * nqp + rout] = mylse;
@@ -472,17 +498,17 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
     }
     return;
   }
-  if (!KEYS && h == 0) {
+  if (!KEYS && gr == 0) {
     g.lse2[(size_t)hx * nqp + rout] = mylse;
     g.delta[(size_t)hx * nqp + rout] = mydel + rsum;
   }
   if (rout >= nmax) return;
-  const bool on = l32 < wreal;
+  const bool on = lw < wreal;
   bf16* o0 = g.g0 + row_off(hx, rout, g.lg0);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int x = 0; x < M::N / 4; ++x) {
       bf16x4 y;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -496,7 +522,7 @@ __global__ __launch_bounds__(64 * NW, (D == 64 ? 2 : 1)) void window_grad_kernel
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+      for (int x = 0; x < M::N / 4; ++x) {
         bf16x4 y;
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][4 * x + r] : 0.f);
@@ -605,7 +631,7 @@ template <int D, bool KEYS>
 hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
   const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
   hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
-                     dim3(64 * NW), 0, st, P, g);
+                     dim3(64 * kRows / grad_rows<D>()), 0, st, P, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts.places() == 0) return e;
   const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
