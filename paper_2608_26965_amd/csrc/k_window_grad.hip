@@ -575,37 +575,63 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
   }
 }
 
-int clamp_parts(int64_t want, int64_t room) {
-  int64_t p = want < room ? want : room;
-  p = p < 64 ? p : 64;
-  return (int)(p < 1 ? 1 : p);
+// The cut of a launch of `heads` heads with nb row blocks, nsink of them with `all` tiles
+// to walk and the others with `seen` (up to that many where `uneven`: causal attention
+// without a window). Of the cuts below the one with the least time by this estimate, in
+// tiles: a workgroup costs three tiles beside its own; equal workgroups run in rounds of
+// as many as the chip holds, others fill it and leave half the longest over; partial sums
+// (128 x 2 d floats written and read) cost 0.015 each and a launch 3. 8,192 tokens on 2 key
+// heads take one round of 24 tiles (three parts, 159 us with the forward pass) instead of
+// two of 18 (166).
+Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int d, bool uneven) {
+  static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  const int64_t slots = d == 64 ? 512 : 256;
+  if (nsink > nb) nsink = nb;
+  Parts best{nb, nsink, 1, 1};
+  double least = -1;
+  for (int p : kCuts) {
+    if (p > 1 && seen / p < 4) break;
+    for (int ps : kCuts) {
+      if (ps > 1 && (nsink == 0 || all / ps < 4)) break;
+      const Parts x{nb, nsink, ps, p};
+      const int64_t wgs = heads * x.items(), other = nb - nsink;
+      const double each = (double)((seen + p - 1) / p) + 3;
+      const double sink = nsink ? (double)((all + ps - 1) / ps) + 3 : 0;
+      const double longest = each > sink ? each : sink;
+      double work = (double)heads * (nsink * ps * sink + other * p * each);
+      if (uneven) work *= 0.5;
+      double cost;
+      if (wgs <= slots)
+        cost = longest;
+      else if (!uneven && sink <= 1.25 * each)
+        cost = (double)((wgs + slots - 1) / slots) * longest;
+      else
+        cost = work / slots + 0.5 * longest;
+      if (x.places()) cost += 0.015 * (double)(heads * x.places()) + 3;
+      if (least < 0 || cost < least) {
+        least = cost;
+        best = x;
+      }
+    }
+  }
+  return best;
 }
-
-// Parts of both kernels. A launch of fewer than 384 workgroups (256 compute
-// units, one or two workgroups each) is cut into about 512, of eight tiles at least;
-// blocks that hold sinks, whose tiles go with all queries, into parts of about
-// the other blocks' tiles, but no more than balance needs (a part costs its
-// partial sums' way through memory).
 Parts query_parts(const WinProb& P) {
   const int nb = (P.nq + kRows - 1) / kRows;
-  const int64_t wgs = (int64_t)nb * P.B * P.H;
-  int64_t keys = (int64_t)P.m.left + P.m.right + kRows + P.m.sinks;
+  int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
-  return Parts{nb, 0, 1, wgs >= 384 ? 1 : clamp_parts((512 + wgs - 1) / wgs, keys / (8 * KT))};
+  const int64_t tiles = (keys + KT - 1) / KT;
+  return cut(nb, 0, tiles, tiles, (int64_t)P.B * P.H, P.d, P.m.causal && P.m.left >= P.nk);
 }
+// keys kept: the blocks that hold sinks are seen by all queries
 Parts key_parts(const WinProb& P) {
   const int nb = (P.nk + kRows - 1) / kRows;
-  const int64_t wgs = (int64_t)nb * P.B * P.Hk, all = (int64_t)(P.nq + KT - 1) / KT * P.G;
-  int64_t seen = ((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1;
-  seen *= P.G;
+  const int64_t all = (int64_t)(P.nq + KT - 1) / KT * P.G;
+  int64_t seen = (((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1) * P.G;
   if (seen > all) seen = all;
-  const int p = wgs >= 384 ? 1 : clamp_parts((512 + wgs - 1) / wgs, seen / 8);
   const int nsink = P.m.sinks < P.nk ? (P.m.sinks + kRows - 1) / kRows : nb;
-  const int64_t total = (nsink * all + (nb - nsink) * seen) * P.B * P.Hk;
-  int64_t each = (seen + p - 1) / p;
-  if (each < total / 2048) each = total / 2048;  // enough to balance the compute units
-  if (each < 16) each = 16;
-  return Parts{nb, nsink, clamp_parts((all + each - 1) / each, all), p};
+  return cut(nb, seen < all ? nsink : 0, all, seen, (int64_t)P.B * P.Hk, P.d,
+             P.m.causal && P.m.left >= P.nk);
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
