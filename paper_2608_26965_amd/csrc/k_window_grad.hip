@@ -116,7 +116,7 @@ struct GradArgs {
   Lay lx, ly, la, lb;
   const bf16* out;            // queries kept: the attention's output, for D
   const float* lse;
-  float *lse2, *delta;        // [B H][nq padded to kRows]: lse log2(e), D (inf and 0 past the lengths)
+  float *lse2, *delta;        // [B H][nq padded to kRows]: lse log2(e), -D (inf and 0 past the lengths)
   bf16 *g0, *g1;
   Lay lg0, lg1;
   float* part;                // [heads][places][kRows][2][d]
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
   };
 
   bf16x8 af[KK], bf[KK];
-  float mylse = INFINITY, mydel = 0.f;
+  float mylse = INFINITY, negdel = 0.f;
   {
     const bf16* ar = g.a + row_off(hx, row, g.la);
     const bf16* br = g.b + row_off(hx, row, g.lb);
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
       const float ls = g.lse[(size_t)hx * P.nq + row];
       if (lw < wreal && ls != -INFINITY) {
         mylse = ls * kLog2e;
-        mydel = d;
+        negdel = -d;
       }
     }
   }
@@ -326,25 +326,27 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
         if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt][0], yo + coff[dt][1]);
       }
     };
+    // keys kept: E starts from the rows' -D
     auto begin = [&](int T) __attribute__((always_inline)) {
+      if constexpr (KEYS) {
 #pragma unroll
-      for (int x = 0; x < M::N / 4; ++x) {
-        f32x4 d = {mydel, mydel, mydel, mydel};
-        if constexpr (KEYS) d = *(const f32x4*)&rows[BUF][1][W * T + 8 * x + 4 * gr];
+        for (int x = 0; x < M::N / 4; ++x) {
+          const f32x4 d = *(const f32x4*)&rows[BUF][1][W * T + 8 * x + 4 * gr];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[T][4 * x + r] = 0.f;
-          e[T][4 * x + r] = -d[r];
+          for (int r = 0; r < 4; ++r) e[T][4 * x + r] = d[r];
         }
       }
     };
     auto logits = [&](int n) __attribute__((always_inline)) {
       const int T = n / SR;
+      Acc zero;
+#pragma unroll
+      for (int r = 0; r < M::N; ++r) zero[r] = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int kk = 2 * (n % SR) + i;
-        s[T] = M::mma(xr[n & 1][i], af[kk], s[T]);
-        e[T] = M::mma(yr[n & 1][i], bf[kk], e[T]);
+        s[T] = M::mma(xr[n & 1][i], af[kk], kk == 0 ? zero : s[T]);
+        e[T] = M::mma(yr[n & 1][i], bf[kk], kk == 0 && !KEYS ? zero : e[T]);
       }
     };
     auto probs = [&](int o) __attribute__((always_inline)) {
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r0 + r], g.sl2, -ls[r]));
-          ds[4 * x + r] = p[4 * x + r] * e[T][r0 + r];
+          ds[4 * x + r] = p[4 * x + r] * (KEYS ? e[T][r0 + r] : e[T][r0 + r] + negdel);
         }
       }
       pp[o] = pack8(p);
@@ -493,14 +495,14 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
       g.rpart[slot] = rsum;
       if (part == 0) {
         g.lse2[(size_t)hx * nqp + rout] = mylse;
-        g.delta[(size_t)hx * nqp + rout] = mydel;
+        g.delta[(size_t)hx * nqp + rout] = negdel;
       }
     }
     return;
   }
   if (!KEYS && gr == 0) {
     g.lse2[(size_t)hx * nqp + rout] = mylse;
-    g.delta[(size_t)hx * nqp + rout] = mydel + rsum;
+    g.delta[(size_t)hx * nqp + rout] = negdel - rsum;
   }
   if (rout >= nmax) return;
   const bool on = lw < wreal;
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
   const bool on = r < (KEYS ? P.klen(b) : P.qlen(b));
   if (!KEYS && lane == 0) {
     const int nqp = (P.nq + kRows - 1) / kRows * kRows;
-    if (on) g.delta[(size_t)hx * nqp + r] += rs;
+    if (on) g.delta[(size_t)hx * nqp + r] -= rs;
   }
   if (r >= nmax) return;
 #pragma unroll
