@@ -338,22 +338,22 @@ __global__ __launch_bounds__(64 * NW, (DP == 128 ? 1 : kF32Waves)) void window_d
   });
 }
 
-// Adds up the parts of the blocks that were cut, in order: a workgroup a block. `sets`
+// Adds up the parts of the blocks that were cut, in order: a thread an element. `sets`
 // is 1 (dq) or 2 (dk, dv).
 __global__ __launch_bounds__(256) void window_sum_f32_kernel(const float* __restrict__ partial,
                                                              const Cut cut, int n, int d, int sets,
                                                              float* __restrict__ a, Lay la,
                                                              float* __restrict__ b, Lay lb) {
-  const int blk = blockIdx.x, hx = blockIdx.y, rows = min(16, n - 16 * blk);
-  const int parts = blk < cut.nsink ? cut.psink : cut.p;
-  if (parts == 1) return;
+  const int blk = blockIdx.x + (cut.psink > 1 ? 0 : cut.nsink), hx = blockIdx.y;
+  const int rows = min(16, n - 16 * blk), parts = blk < cut.nsink ? cut.psink : cut.p;
   const float* p = partial + ((size_t)hx * cut.items() + cut.item(blk)) * 16 * sets * d;
-  for (int e = threadIdx.x; e < sets * rows * d; e += 256) {
-    const int set = e / (rows * d), x = e - set * rows * d, r = x / d, t = x - r * d;
-    float sum = 0.f;
-    for (int i = 0; i < parts; ++i) sum += p[((size_t)i * sets + set) * 16 * d + x];
-    (set ? b : a)[row_off(hx, 16 * blk + r, set ? lb : la) + t] = sum;
-  }
+  const int e = blockIdx.z * 256 + threadIdx.x, set = e / (16 * d), x = e - set * 16 * d;
+  const int r = x / d, t = x - r * d;
+  if (set >= sets || r >= rows) return;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) sum += p[((size_t)i * sets + set) * 16 * d + x];
+  (set ? b : a)[row_off(hx, 16 * blk + r, set ? lb : la) + t] = sum;
 }
 
 // Wavefronts of a workgroup: eight, four where eight leave too little LDS or registers
@@ -382,7 +382,7 @@ Cut query_cut(const WinProb& P) {
   return Cut{(P.nq + 15) / 16, 0, 1, parts_of(P, 1)};
 }
 // dk and dv: blocks that hold sinks are seen by all queries of the group and cut into
-// parts of about the other blocks' tiles, eight steps at least
+// parts of about the other blocks' tiles, two steps at least
 Cut key_cut(const WinProb& P) {
   const int nw = waves_of(P);
   const int64_t all = (int64_t)(P.nq + 15) / 16 * P.G;
@@ -393,7 +393,7 @@ Cut key_cut(const WinProb& P) {
   if (wgs < 512) c.p = clamp((1024 + wgs - 1) / wgs, seen / nw / 2 < 64 ? seen / nw / 2 : 64);
   if (seen < all && P.m.sinks > 0) {
     c.nsink = P.m.sinks < P.nk ? (P.m.sinks + 15) / 16 : c.nb;
-    const int64_t each = seen / c.p > 8 * nw ? seen / c.p : 8 * nw;
+    const int64_t each = seen / c.p > 2 * nw ? seen / c.p : 2 * nw;
     c.psink = clamp((all + each - 1) / each, 64);
   }
   return c;
@@ -427,8 +427,9 @@ hipError_t run_backward_f32(const WinProb& P, const float* q, const float* k, co
                  const Lay& lb) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !c.cut()) return e;
-    hipLaunchKernelGGL(window_sum_f32_kernel, dim3(c.nb, heads), dim3(256), 0, st, partial, c, n,
-                       P.d, sets, a, la, b, lb);
+    const int blocks = (c.p > 1 ? c.nb : c.nsink) - (c.psink > 1 ? 0 : c.nsink);
+    hipLaunchKernelGGL(window_sum_f32_kernel, dim3(blocks, heads, (16 * sets * P.d + 255) / 256),
+                       dim3(256), 0, st, partial, c, n, P.d, sets, a, la, b, lb);
     return hipGetLastError();
   };
   const Cut cq = query_cut(P), ck = key_cut(P);
