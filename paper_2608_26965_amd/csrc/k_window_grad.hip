@@ -21,8 +21,10 @@
 // bf16, leave a sum r of their own, and r times the mean key of an error. So the
 // first kernel sums the dS as rounded and takes it out, dq = scale (sum dS k -
 // r kbar), and D + r goes to the second. Without it dq is off by 0.0037 of its
-// size (keys of one mixture, 8,192 tokens) where rounding the result alone
-// is 0.0017.
+// size (keys of one mixture, 8,192 tokens), with it 0.0023, where rounding the
+// result alone is 0.0017. dk has no such sum; its dS go in as two bf16 parts (a fifth
+// product), with one it was off by 0.0024 to 0.0027, so by 0.0017 to 0.0020, for 3 to
+// 6% of the time.
 #include <math.h>
 
 #include "row_tile.h"
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
     const char* ys = smem + (2 + BUF) * TILE;
     constexpr int RT = KT / W, NO = KT / M::K;  // row tiles, and operands of 8 accumulators
     Acc s[RT], e[RT];
-    bf16x8 pp[NO], dd[NO];
+    bf16x8 pp[NO], dd[NO], dl[KEYS ? NO : 1];  // P, dS, what dS lost in rounding
 
     // Steps, a fence apart each: the operands of the next step are read before the
     // products of this one, which run beside some of the exponentials. (Left to
@@ -364,7 +366,14 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
       }
       pp[o] = pack8(p);
       dd[o] = pack8(ds);
-      if constexpr (!KEYS) rsum = sum8(dd[o], rsum);
+      if constexpr (KEYS) {
+        float lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lo[j] = ds[j] - bf2f(dd[o][j]);
+        dl[o] = pack8(lo);
+      } else {
+        rsum = sum8(dd[o], rsum);
+      }
     };
     auto products = [&](int n) __attribute__((always_inline)) {
       const int o = n / SC;
@@ -372,6 +381,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
       for (int i = 0; i < 2; ++i) {
         const int dt = 2 * (n % SC) + i;
         acc0[dt] = M::mma(xc[n & 1][i], dd[o], acc0[dt]);
+        if constexpr (KEYS) acc0[dt] = M::mma(xc[n & 1][i], dl[o], acc0[dt]);
         acc1[dt] = M::mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
       }
     };
