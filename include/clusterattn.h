@@ -427,7 +427,7 @@ typedef struct {
   int32_t grid[4], start[4];     /* positions NULL only */
   int64_t pos_stride[3];         /* {batch, axis, token}, positions given */
   int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3]; /* {batch, head, token} */
-  double freq[64];               /* radians per position */
+  double freq[64];               /* radians per position, at most 2^20 */
 } ca_rope_desc;
 
 /* q_out and k_out may be q and k themselves (with the same strides): the rows
@@ -445,7 +445,11 @@ CA_API int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const in
  *   out = sum_j e^{s_j - lse} v_j, lse = ln sum_j e^{s_j}, s_j = scale q . k_j
  * over the keys it sees (scale <= 0 selects 1/sqrt(d)). A query that sees no
  * key, and every row at or past len_q, has out = 0 and lse = -inf. Rows of k
- * and v at or past len_k are never read. */
+ * and v at or past len_k are never read, and what a key or value that a query
+ * does not see holds (infinities and NaN too) does not reach its output; a query
+ * that sees a value that is not finite has an output that is not. (The backward
+ * pass promises this for rows past the lengths only: a NaN or an infinity
+ * in a token reaches the gradients of its neighbours, up to 127 tokens away.) */
 typedef struct {
   int32_t batch, heads, heads_k;
   int32_t nq, nk, d, dtype;      /* 1..2^22 queries and keys */
@@ -456,7 +460,9 @@ typedef struct {
   int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
 } ca_window;
 
-/* out: strides out_stride; lse: optional dense fp32 [batch][heads][nq]. ws:
+/* bf16: token strides of at most 2^23 elements (also of dout in the backward
+ * pass), and batch * heads * (blocks of 128 tokens) below 2^22.
+ * out: strides out_stride; lse: optional dense fp32 [batch][heads][nq]. ws:
  * workspace (long keys for few queries are cut into parts and joined). */
 CA_API int ca_window_attn(const ca_window* p, const void* q, const void* k, const void* v,
                           const int32_t* len_q, const int32_t* len_k, void* out, float* lse,

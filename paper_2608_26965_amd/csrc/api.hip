@@ -710,7 +710,8 @@ int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const int32_t* 
   if (!positions && cells < p->n)
     return fail(CA_E_INVALID, "the grid holds %lld tokens, fewer than n = %d", (long long)cells, p->n);
   for (int i = 0; i < P.npairs; ++i) {
-    if (!isfinite(p->freq[i])) return fail(CA_E_INVALID, "freq[%d] is not finite", i);
+    if (!(fabs(p->freq[i]) <= 1048576.0))
+      return fail(CA_E_INVALID, "freq[%d] must be a number of at most 2^20", i);
     P.freq[i] = p->freq[i];
   }
   for (int i = P.npairs; i < ca::kMaxD / 2; ++i) P.freq[i] = 0.0;
@@ -792,6 +793,8 @@ int ca_window_attn_backward(const ca_window* p, const void* q, const void* k, co
       (s = check_written(p->dk_stride, p->batch, p->heads_k, p->nk, "dk")) ||
       (s = check_written(p->dv_stride, p->batch, p->heads_k, p->nk, "dv")))
     return s;
+  if (p->dtype == CA_BF16 && p->dout_stride[2] > (1 << 23))
+    return fail(CA_E_UNSUPPORTED, "bf16 window attention needs token strides of at most 2^23");
   if ((s = check_bytes(ca::window_backward_bytes(P), ws, ws_bytes))) return s;
   P.len_q = len_q;
   P.len_k = len_k;

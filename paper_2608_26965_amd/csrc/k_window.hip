@@ -65,7 +65,34 @@ struct WindowKeys {
   __device__ __forceinline__ void vals(int t, f32x4 (&f)[DP / 16]) const {
     load_cols<DP>(v, v_sn, key(t), lk, d, lane, f);
   }
-  __device__ __forceinline__ void mask_vals(int, f32x4 (&)[DP / 16]) const {}
+  // Values that are infinite or NaN and that one of the tile's queries does not see are
+  // set to zero (zero times them is NaN); a query that does see one is marked.
+  mutable bool poison;
+  __device__ __forceinline__ void mask_vals(int t, f32x4 (&f)[DP / 16]) const {
+    const int g = lane >> 4, j0 = key(t) + 4 * g;
+    bool all = true, fine = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all &= sees(r, j0 + i);
+    if (__builtin_amdgcn_ballot_w64(!all) == 0) return;
+#pragma unroll
+    for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fine &= fabsf(f[x][i]) <= 3.402823466e38f;
+    if (__builtin_amdgcn_ballot_w64(!fine) == 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bool bad = false;
+#pragma unroll
+      for (int x = 0; x < DP / 16; ++x) {
+        const bool b = !(fabsf(f[x][i]) <= 3.402823466e38f);
+        f[x][i] = b ? 0.f : f[x][i];
+        bad |= b;
+      }
+      // any dim of key j0 + i: held by the 16 lanes of group g
+      const uint64_t m = __builtin_amdgcn_ballot_w64(bad) >> (16 * g);
+      poison |= (m & 0xffffu) != 0 && t < ntile && sees(r, j0 + i);
+    }
+  }
   __device__ __forceinline__ void logits(int t, f32x4& s) const {
     const int j0 = key(t) + 4 * (lane >> 4);
 #pragma unroll
@@ -94,8 +121,13 @@ __global__ __launch_bounds__(64 * NW, kF32Waves) void window_f32_kernel(
   f32_load_rows<DP>(q + row_off(bh, i, P.lq), P.d, lane >> 4, qf);
   const WindowKeys<DP> src{k + row_off(bk, 0, P.lk), v + row_off(bk, 0, P.lv), P.lk.sn, P.lv.sn,
                            list, t0, min(per, list.n - t0), lk, P.d, lane,
-                           visible_keys(P.m, i + off, lk), P.scale};
+                           visible_keys(P.m, i + off, lk), P.scale, false};
   f32_parts<DP, NW, NW>(src, qf, M, w, lane);
+  int poison = src.poison;  // of this wavefront's keys, in the four lanes of a query
+  poison |= __shfl_xor(poison, 16, 64);
+  poison |= __shfl_xor(poison, 32, 64);
+  if (poison)
+    for (int t = lane >> 4; t < DP; t += 4) M.o[w][t][lane & 15] = NAN;
   f32_merge(M, w, lane);
   if (parts > 1) {
     for (int e = threadIdx.x; e < rows * P.d; e += 64 * NW) {
@@ -394,7 +426,8 @@ Cut key_cut(const WinProb& P) {
   if (seen < all && P.m.sinks > 0) {
     c.nsink = P.m.sinks < P.nk ? (P.m.sinks + 15) / 16 : c.nb;
     const int64_t each = seen / c.p > 2 * nw ? seen / c.p : 2 * nw;
-    c.psink = clamp((all + each - 1) / each, 64);
+    const int64_t sinks = (int64_t)c.nsink * P.B * P.Hk;  // 4096 workgroups are enough
+    c.psink = clamp((all + each - 1) / each, (4096 + sinks - 1) / sinks < 64 ? (4096 + sinks - 1) / sinks : 64);
   }
   return c;
 }

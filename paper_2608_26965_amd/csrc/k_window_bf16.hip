@@ -132,7 +132,6 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
   float m, l;       // reference (log2 units) and this lane's part of the sum
   float alpha;      // what a raised reference scales the results so far by
   bool set;         // every row of the wavefront has a reference
-  bool safe = false;
 
   auto logits = [&](const char* ks) __attribute__((always_inline)) {
 #pragma unroll
@@ -181,9 +180,9 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     }
   };
   // The reference of a tile of class c: the rows' own where every row has one and
-  // sees all of the tile, else raised to the tile's maximum. True if raised.
-  auto reference = [&](int c, int k0) __attribute__((always_inline)) {
-    if (c == 2 && set && !safe) return false;
+  // sees all of the tile (`keep`), else raised to the tile's maximum. True if raised.
+  auto reference = [&](int c, int k0, bool keep) __attribute__((always_inline)) {
+    if (keep && c == 2 && set) return false;
     if (c == 1) mask(k0);
     if (c == 0) {
 #pragma unroll
@@ -210,7 +209,6 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     wait_lgkm();
     raw_barrier();
   };
-
   // Tile g's keys sit in key buffer g % 2 and its values in value buffer g % 2
   // (g counted from t0). After iteration g's barrier every wavefront is past
   // iteration g - 1 and the copies that it issued have landed: the keys of tile
@@ -225,31 +223,34 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     if (t + 1 < t1) issue_k(t + 1, PAR ^ 1);
     issue_v(t, PAR);
   };
+  auto groups = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) f(mt, s2);
+  };
+  auto rescale = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+  };
   auto step = [&](auto par_tag, int t) __attribute__((always_inline)) {
     constexpr int PAR = decltype(par_tag)::value;
     copies(par_tag, t);
     const int k0 = KT * list.tile(t), c = tile_class(ra, rz, k0);
     logits(smem + PAR * TILE);
-    const bool raised = reference(c, k0);
+    const bool raised = reference(c, k0, true);
     const float ref = m == -INFINITY ? 0.f : m;  // no key yet
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        pv_group(smem + (2 + (PAR ^ 1)) * TILE, mt, s2);
-        exp_group(mt, s2, ref);
-      }
-    if (raised) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-    }
+    groups([&](int mt, int s2) {
+      pv_group(smem + (2 + (PAR ^ 1)) * TILE, mt, s2);
+      exp_group(mt, s2, ref);
+    });
+    if (raised) rescale();
   };
   const std::integral_constant<int, 0> even;
   const std::integral_constant<int, 1> odd;
-  float l_tot;
-  for (;;) {
+  auto reset = [&]() __attribute__((always_inline)) {
     m = -INFINITY;
     l = 0.f;
     set = false;
@@ -257,49 +258,103 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
-    if (t0 < t1) {
-      issue_k(t0, 0);
-      copies(even, t0);
-      if (wreal == 0) {  // no rows: copies only
-        for (int t = t0 + 1; t < t1; t += 2) {
-          copies(odd, t);
-          if (t + 1 < t1) copies(even, t + 1);
-        }
-        sync_stage();
-      } else {
-        const int k0 = KT * list.tile(t0);
-        logits(smem);
-        reference(tile_class(ra, rz, k0), k0);
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) exp_group(mt, s2, ref);
-        for (int t = t0 + 1; t < t1; t += 2) {
-          step(odd, t);
-          if (t + 1 < t1) step(even, t + 1);
-        }
-        sync_stage();
-        const char* vs = smem + (2 + ((t1 - 1 - t0) & 1)) * TILE;
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) pv_group(vs, mt, s2);
+  };
+  reset();
+  if (t0 < t1) {
+    issue_k(t0, 0);
+    copies(even, t0);
+    if (wreal == 0) {  // no rows: copies only
+      for (int t = t0 + 1; t < t1; t += 2) {
+        copies(odd, t);
+        if (t + 1 < t1) copies(even, t + 1);
       }
+      sync_stage();
+    } else {
+      const int k0 = KT * list.tile(t0);
+      logits(smem);
+      reference(tile_class(ra, rz, k0), k0, true);
+      const float ref = m == -INFINITY ? 0.f : m;
+      groups([&](int mt, int s2) { exp_group(mt, s2, ref); });
+      for (int t = t0 + 1; t < t1; t += 2) {
+        step(odd, t);
+        if (t + 1 < t1) step(even, t + 1);
+      }
+      sync_stage();
+      const char* vs = smem + (2 + ((t1 - 1 - t0) & 1)) * TILE;
+      groups([&](int mt, int s2) { pv_group(vs, mt, s2); });
     }
-    l_tot = l + wave_xor32(l);
-    if (safe) break;
+  }
+  float l_tot = l + wave_xor32(l);
+  bool poison = false;
+  {
     bool fine = l_tot <= 0x1p126f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) fine &= fabsf(oacc[dt][r]) <= 0x1p127f;
     if (__builtin_amdgcn_ballot_w64(!fine) && lane == 0) redo = 1;
-    __syncthreads();
-    if (!redo) break;
-    safe = true;
   }
+  __syncthreads();
+  if (redo) {
+    // The workgroup starts over, one tile after the other, each against its own
+    // maximum. Where the reason was a value that is infinite or NaN and that some row of
+    // the block does not see (zero times it is NaN), `guard` sets the rows of the tile that
+    // hold one to zero, and queries that do see one get NaN at the end. Every wavefront
+    // looks through all of the tile, so all agree on whether there is anything to do.
+    auto guard = [&](char* vs, int k0) __attribute__((always_inline)) {
+      if (tile_class(visible_keys(P.m, q0 + off, lk), visible_keys(P.m, q0 + real - 1 + off, lk),
+                     k0) == 2)
+        return;
+      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      constexpr int NCH = RB / 16;
+      u16x2 most = {0, 0};
+#pragma unroll 2
+      for (int c = 0; c < NCH; ++c) {
+        const u32x4 x = *(const u32x4*)(vs + lane * RB + ((c + lane) % NCH) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu));
+      }
+      uint64_t bad = __builtin_amdgcn_ballot_w64(most.x >= 0x7f80 || most.y >= 0x7f80);
+      if (__builtin_expect(bad == 0, 1)) return;
+      __syncthreads();
+      if (w == 0 && ((bad >> lane) & 1)) {
+#pragma unroll 1
+        for (int c = 0; c < NCH; ++c) *(f32x4*)(vs + lane * RB + c * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      __syncthreads();
+      const KeyRange rr = visible_keys(P.m, i + off, lk);
+      for (; bad; bad &= bad - 1) poison |= sees(rr, k0 + __builtin_ctzll(bad));
+    };
 
+    reset();
+    for (int t = t0; t < t1; ++t) {
+      const int k0 = KT * list.tile(t);
+      issue_k(t, 0);
+      issue_v(t, 0);
+      sync_stage();
+      guard(smem + 2 * TILE, k0);
+      if (wreal) {
+        logits(smem);
+        const bool raised = reference(tile_class(ra, rz, k0), k0, false);
+        const float ref = m == -INFINITY ? 0.f : m;
+        if (raised) rescale();
+        groups([&](int mt, int s2) {
+          exp_group(mt, s2, ref);
+          pv_group(smem + 2 * TILE, mt, s2);
+        });
+      }
+      __syncthreads();  // every wavefront is past the tile
+    }
+    l_tot = l + wave_xor32(l);
+  }
+  if (poison) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[dt][r] = NAN;
+  }
   if constexpr (SPLIT) {
     float* row = part + ((((size_t)bh * order.nb + a) * kRows + 32 * w + l32) * order.splits + sp) *
                             (D + 4);
@@ -375,7 +430,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(const WinProb P,
 int window_splits(const WinProb& P) {
   const int64_t wgs = (int64_t)((P.nq + kRows - 1) / kRows) * P.B * P.H;
   if (wgs >= 384) return 1;
-  int64_t keys = (int64_t)P.m.left + P.m.right + kRows + P.m.sinks;
+  int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
   const int64_t want = (512 + wgs - 1) / wgs, room = keys / (8 * KT);
   const int64_t s = want < room ? want : room;

@@ -607,6 +607,7 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int d, bo
       if (ps > 1 && (nsink == 0 || all / ps < 4)) break;
       const Parts x{nb, nsink, ps, p};
       const int64_t wgs = heads * x.items(), other = nb - nsink;
+      if (p * ps > 1 && wgs > 1 << 16) break;  // enough workgroups, and bytes of partial sums
       const double each = (double)((seen + p - 1) / p) + 3;
       const double sink = nsink ? (double)((all + ps - 1) / ps) + 3 : 0;
       const double longest = each > sink ? each : sink;

@@ -9,7 +9,9 @@ include/clusterattn.h for their definitions).
 
 As in the rest of the binding, every step runs in the HIP library: these
 functions read shapes and strides, allocate outputs and workspaces with torch
-and call on the current stream of the tensors' device.
+and call on the current stream of the tensors' device. They are not recorded by
+autograd: a training program calls window_attn_backward, and rope with
+inverse=True, for the gradients.
 """
 from __future__ import annotations
 
@@ -86,6 +88,22 @@ def _new(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+_MOST = 2 ** 31 - 1
+
+
+def _int(x, name, least=-_MOST - 1, most=_MOST):
+    """x as the C int32 that it has to fit in."""
+    x = int(x)
+    if not least <= x <= most:
+        raise ValueError(f"{name} = {x} is out of range")
+    return x
+
+
+def _side(x):
+    # a window wider than any sequence is no limit; so is a negative one
+    return -1 if x < 0 or x > _MOST else int(x)
+
+
 def _expect(t, shape, name):
     if t.shape != shape:  # (a torch.Size compares with a tuple)
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -151,7 +169,7 @@ class Rope:
         if not 1 <= len(self.freqs) <= 64:
             raise ValueError("1 to 64 pairs")
         f = (ctypes.c_double * 64)(*self.freqs)
-        s = _I32x4(*self.sections)
+        s = _I32x4(*(_int(x, "sections", 0, 64) for x in self.sections))
         object.__setattr__(self, "_c", (len(self.sections), s, f))
 
 
@@ -209,9 +227,9 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     if grid is not None:
         if len(grid) != axes or (start is not None and len(start) != axes):
             raise ValueError(f"grid and start need {axes} entries")
-        g = _I32x4(*grid)
+        g = _I32x4(*(_int(x, "grid") for x in grid))
         if start is not None:
-            s = _I32x4(*start)
+            s = _I32x4(*(_int(x, "start") for x in start))
     else:
         if start is not None:
             raise ValueError("start goes with grid")
@@ -261,7 +279,8 @@ def _window(w, q, k, v, out, scale, len_q, len_k, layout, grads=()):
     _same(out, q, "out")
     _rows(out, "out", 4)
     _expect(out, q.shape, "out")
-    return _lib.CaWindow(B, H, Hk, nq, nk, d, dt, w.left, w.right, w.sinks, int(w.causal),
+    return _lib.CaWindow(B, H, Hk, nq, nk, d, dt, _side(w.left), _side(w.right),
+                         min(w.sinks, _MOST), int(w.causal),
                          0.0 if scale is None else float(scale), _strides(q, layout),
                          _strides(k, layout), _strides(v, layout), _strides(out, layout),
                          *(_strides(t, layout) for t in grads))
@@ -331,7 +350,7 @@ def _paged(q, heads, k_pages, v_pages, table, lens, left, sinks, scale, q_st=Non
     _int32(table, (B, table.shape[1]), k_pages, "page_table")
     _int32(lens, (B,), k_pages, "lens")
     z3, z2 = _I64x3(), _I64x2()
-    return _lib.CaPaged(B, heads, Hk, d, dt, page, P, table.shape[1], left, sinks,
+    return _lib.CaPaged(B, heads, Hk, d, dt, page, P, table.shape[1], _side(left), min(sinks, _MOST),
                         0.0 if scale is None else float(scale),
                         table.stride(0) if B > 1 else 0, _lead(k_pages),
                         _lead(v_pages), q_st or z2, o_st or z2, n_new, kn or z3, vn or z3)

@@ -35,7 +35,7 @@ def _rope(**kw):
     (dict(axes=5), 1, "axes"), (dict(section=I4(-1, 4)), 1, "section"), (dict(section=I4(0, 0)), 1, "section"),
     (dict(section=I4(16, 17)), 1, "section"), (dict(section=I4(2, 2), halves=1), 2, "halves"),
     (dict(grid=I4(2, 3)), 1, "grid"), (dict(grid=I4(0, 9)), 1, "grid"), (dict(start=I4(2**31 - 1)), 1, "start"),
-    (dict(freq=(ctypes.c_double * 64)(float("nan"))), 1, "freq"), (dict(q_stride=I3(64, 64, 4)), 1, "q_stride[2]"),
+    (dict(freq=(ctypes.c_double * 64)(float("nan"))), 1, "freq"), (dict(freq=(ctypes.c_double * 64)(1e9)), 1, "freq"), (dict(q_stride=I3(64, 64, 4)), 1, "q_stride[2]"),
     (dict(q_stride=I3(-64, 64, 64)), 1, "q_stride[0]"), (dict(k_stride=I3(64, 4, 64)), 1, "k_stride[1]"),
     (dict(q_out_stride=I3(2048, 0, 64)), 1, "q_out_stride[1]"), (dict(k_out_stride=I3(2048, 512, 0)), 1, "k_out_stride"),
 ])
@@ -85,7 +85,7 @@ def test_window_refusals(kw, status, word):
 
 
 @pytest.mark.parametrize("kw,status,word", _BAD_WINDOW + [
-    (dict(dout_stride=I3(64, 64, 4)), 1, "dout_stride"), (dict(dq_stride=I3(64, 64, 0)), 1, "dq_stride[2]"),
+    (dict(dout_stride=I3(64, 64, 4)), 1, "dout_stride"), (dict(dout_stride=I3(64, 64, 1 << 24)), 2, "2^23"), (dict(dq_stride=I3(64, 64, 0)), 1, "dq_stride[2]"),
     (dict(dk_stride=I3(0, 64, 64)), 1, "dk_stride[0]"), (dict(dv_stride=I3(64, 0, 64)), 1, "dv_stride[1]"),
 ])
 def test_window_backward_refusals(kw, status, word):
@@ -190,3 +190,5 @@ def test_binding_refuses_cpu_tensors_and_shapes():
         ca.Rope((2, 2), (1.0, 2.0, 3.0))
     with pytest.raises(ValueError):
         ca.Rope((2,), (1.0, 2.0), "pairs")
+    with pytest.raises(ValueError, match="sections"):
+        ca.Rope((2 ** 32 + 2, -2 ** 32), (1.0, 2.0))

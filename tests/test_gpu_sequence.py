@@ -305,6 +305,31 @@ def test_window_rising_maximum(dt):
 
 
 @pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kw", [dict(causal=True), dict(left=30, causal=True, sinks=3), dict(left=20, right=10),
+                                dict(left=0, right=0, sinks=40)])
+@pytest.mark.parametrize("where,value", [("v", float("nan")), ("v", float("inf")), ("k", float("nan"))])
+def test_window_hidden_values_may_be_anything(dt, d, kw, where, value):
+    """A NaN or an infinity in some tokens reaches the queries that see them and no
+    others."""
+    ca = _ca()
+    g = _gen(21)
+    n, at = 260, [45, 100, 101, 190]  # none of them a sink, which all queries see
+    q, k, v = (_rand(g, (1, 2, n, d), dt) for _ in range(3))
+    see = seq.visible(n, n, kw.get("left", -1), kw.get("right", -1), kw.get("sinks", 0), kw.get("causal", False))
+    want = [_bounds(*(_np(x)[0, h] for x in (q, k, v)), None, see, 1 / math.sqrt(d), dt) for h in range(2)]
+    (v if where == "v" else k)[0, :, at, d - 1] = value
+    out, lse = ca.window_attn(ca.Window(**kw), *(x.cuda() for x in (q, k, v)), want_lse=True)
+    sick = see[:, at].any(1)
+    assert sick.any() and not sick.all()
+    for h in range(2):
+        o, e = _np(out)[0, h], _np(lse)[0, h]
+        _close(o[~sick], *(x[~sick] for x in want[h]["out"]), "out of the others")
+        _close(e[~sick], *(x[~sick] for x in want[h]["lse"]), "lse of the others")
+        assert not np.isfinite(o[sick]).all(1).any()
+
+
+@pytest.mark.parametrize("dt", DT)
 def test_window_repeated_inputs(dt):
     """Strides of 0: keys and values shared by the batch, the gradient of a sum."""
     import torch
