@@ -133,18 +133,32 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
   float alpha;      // what a raised reference scales the results so far by
   bool set;         // every row of the wavefront has a reference
 
+  // Operands are read a step ahead of their products, a fence between (left to itself
+  // the compiler reads each right before its product and waits).
   auto logits = [&](const char* ks) __attribute__((always_inline)) {
+    constexpr int ST = KS / 2;  // steps of a row tile
+    bf16x8 av[2][2];
+    auto load = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      f32x16 z;
+      for (int x = 0; x < 2; ++x)
+        av[n & 1][x] = *(const bf16x8*)(ks + 32 * (n / ST) * RB + koff[2 * (n % ST) + x]);
+    };
+    f32x16 z;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    load(0);
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        const bf16x8 av = *(const bf16x8*)(ks + 32 * mt * RB + koff[kk]);
-        sacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qreg[kk], kk == 0 ? z : sacc[mt],
-                                                           0, 0, 0);
+    for (int n = 0; n < 2 * ST; ++n) {
+      const int mt = n / ST;
+      if (n + 1 < 2 * ST) load(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int kk = 2 * (n % ST) + x;
+        sacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[n & 1][x], qreg[kk],
+                                                           kk == 0 ? z : sacc[mt], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   // accumulator r of row tile mt is key k0 + 32 mt + 8 (r / 4) + 4 h + r % 4
@@ -242,10 +256,37 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     logits(smem + PAR * TILE);
     const bool raised = reference(c, k0, true);
     const float ref = m == -INFINITY ? 0.f : m;  // no key yet
-    groups([&](int mt, int s2) {
-      pv_group(smem + (2 + (PAR ^ 1)) * TILE, mt, s2);
-      exp_group(mt, s2, ref);
-    });
+    const char* vs = smem + (2 + (PAR ^ 1)) * TILE;
+    constexpr int SV = DT / 2;  // steps of a group: two products and some of its exponentials
+    bf16x8 av[2][2];
+    auto load = [&](int n) __attribute__((always_inline)) {
+      const char* at = vs + 16 * (n / SV) * RB;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int dt = 2 * (n % SV) + x;
+        av[n & 1][x] = read_cols(at + voff[dt][0], at + voff[dt][1]);
+      }
+    };
+    load(0);
+    float p[8];
+#pragma unroll
+    for (int n = 0; n < 4 * SV; ++n) {
+      const int mt = n / SV / 2, s2 = n / SV % 2, st = n % SV;
+      if (n + 1 < 4 * SV) load(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        oacc[2 * st + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[n & 1][x], pb[mt][s2],
+                                                                   oacc[2 * st + x], 0, 0, 0);
+#pragma unroll
+      for (int j = 8 / SV * st; j < 8 / SV * (st + 1); ++j)
+        p[j] = __builtin_amdgcn_exp2f(fmaf(sacc[mt][8 * s2 + j], sl2, -ref));
+      if (st == SV - 1) {
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        pb[mt][s2] = pack8(p);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     if (raised) rescale();
   };
   const std::integral_constant<int, 0> even;
