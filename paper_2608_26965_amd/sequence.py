@@ -16,6 +16,7 @@ inverse=True, for the gradients.
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 import torch
@@ -33,54 +34,75 @@ _I32x4 = ctypes.c_int32 * 4
 
 
 # ---- what every call checks -----------------------------------------------------
+#
+# A call's descriptor (sizes, strides, type, options) takes longer to make than the
+# launch of a small kernel, and a program makes the same few calls again and again:
+# descriptors are kept by what they are made from. They hold no address, and no
+# value of a tensor.
+_kept = functools.lru_cache(maxsize=1024)
 
-def _dtype(t):
-    dt = _DT.get(t.dtype)
-    if dt is None:
-        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    if not t.is_cuda:
+
+def _geo(t):
+    """What a descriptor says of a tensor."""
+    return t.shape, t.stride(), t.dtype
+
+
+def _on(like, *tensors):
+    """Of a type that the library has, and all on one GPU."""
+    _dtype(like.dtype)
+    if not like.is_cuda:
         raise ValueError("expected tensors on the GPU")
+    for t in tensors:
+        if t is not None and t.device != like.device:
+            raise ValueError(f"expected all tensors on {like.device}, got one on {t.device}")
+
+
+def _dtype(dtype):
+    dt = _DT.get(dtype)
+    if dt is None:
+        raise ValueError(f"expected float32 or bfloat16, got {dtype}")
     return dt
 
 
-def _same(t, like, name):
-    if t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name}: expected {like.dtype} on {like.device}, got {t.dtype} on "
-                         f"{t.device}")
-
-
-def _rows(t, name, dims):
-    if t.dim() != dims or (t.stride(-1) != 1 and t.size(-1) > 1):
+def _rows(geo, name, dims, dtype, shape=None):
+    """(shape, strides) of rows that are contiguous; a stride of a dimension of one
+    element, which is never used, as 0."""
+    size, stride, dt = geo
+    if len(size) != dims or (stride[-1] != 1 and size[-1] > 1):
         raise ValueError(f"{name}: expected {dims} dimensions, the last one contiguous")
+    if dt != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {dt}")
+    if shape is not None and tuple(size) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(size)}")
+    return tuple(size), tuple(b if a > 1 else 0 for a, b in zip(size, stride))
 
 
-def _sizes(t, layout, name):
-    """(batch, heads, tokens, d) of a [B,H,N,d] or ("bnhd") [B,N,H,d] tensor."""
-    _rows(t, name, 4)
-    s = t.shape
+def _heads(geo, layout, name, dtype, shape=None):
+    """((batch, heads, tokens, d), {batch, head, token} strides) of a [B,H,N,d] or
+    ("bnhd") [B,N,H,d] tensor."""
+    (a, b, c, d), (x, y, z, _) = _rows(geo, name, 4, dtype, shape)
     if layout == "bnhd":
-        return s[0], s[2], s[1], s[3]
+        return (a, c, b, d), _I64x3(x, z, y)
     if layout not in ("bhnd", "strided"):
         raise ValueError(layout)
-    return tuple(s)
+    return (a, b, c, d), _I64x3(x, y, z)
 
 
-def _strides(t, layout):
-    """(batch, head, token) element strides (0 where there is one: never used)."""
-    a, b, c, _ = t.stride()
-    x, y, z, _ = t.shape
-    if layout == "bnhd":
-        b, c, y, z = c, b, z, y
-    return _I64x3(a if x > 1 else 0, b if y > 1 else 0, c if z > 1 else 0)
+def _int32(geo, name, *shapes):
+    if geo[2] != torch.int32:
+        raise ValueError(f"{name}: expected int32, got {geo[2]}")
+    if tuple(geo[0]) not in shapes:
+        raise ValueError(f"{name}: expected {' or '.join(map(str, map(list, shapes)))}, got "
+                         f"{list(geo[0])}")
 
 
-def _lead(t):
-    """The strides of a tensor's first three (four dimensions) or two (three)."""
-    if t.dim() == 4:
-        return _strides(t, "bhnd")
-    a, b, _ = t.stride()
-    x, y, _ = t.shape
-    return _I64x2(a if x > 1 else 0, b if y > 1 else 0)
+def _dense(geo):
+    """The geometry of a dense tensor of the same shape."""
+    size, stride, n = geo[0], [], 1
+    for x in reversed(size):
+        stride.insert(0, n)
+        n *= max(1, x)
+    return size, tuple(stride), geo[2]
 
 
 def _new(t):
@@ -104,26 +126,13 @@ def _side(x):
     return -1 if x < 0 or x > _MOST else int(x)
 
 
-def _expect(t, shape, name):
-    if t.shape != shape:  # (a torch.Size compares with a tuple)
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-
-
-def _int32(t, shape, like, name):
-    if t.dtype != torch.int32 or t.device != like.device:
-        raise ValueError(f"{name}: expected int32 on {like.device}, got {t.dtype} on {t.device}")
-    _expect(t, shape, name)
-    if t.dim() and t.stride(-1) != 1 and t.size(-1) > 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-
-
 def _call(name, device, *args):
     """The library's call on the current stream of `device`, made the current
     device for the launch."""
     f = getattr(_lib.load(), name)
     i = device.index
     if i == torch.cuda.current_device():
-        # the handle alone: a torch.cuda.Stream object costs 2 us of a small call's 12
+        # the handle alone: a torch.cuda.Stream object costs 2 us of a small call's 9
         st = f(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(i):
@@ -132,17 +141,20 @@ def _call(name, device, *args):
         _lib.check(st, name)
 
 
-def _workspace(size, *args, device, ws):
-    """The caller's workspace, or a new one of the bytes that the library asks for."""
-    if ws is not None:
-        if ws.device != device or not ws.is_contiguous():
-            raise ValueError(f"ws: expected a contiguous tensor on {device}")
-        return ws
+def _bytes(size, *args):
+    """Bytes of workspace that the library asks for."""
     n = ctypes.c_size_t(0)
-    st = getattr(_lib.load(), size)(*args, n)
-    if st:
-        _lib.check(st, size)
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    _lib.check(getattr(_lib.load(), size)(*args, n), size)
+    return n.value
+
+
+def _workspace(nbytes, like, ws):
+    """The caller's workspace, or a new one."""
+    if ws is None:
+        return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    if ws.device != like.device or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on {like.device}")
+    return ws
 
 
 def _ptr(t):
@@ -162,6 +174,8 @@ class Rope:
     pairing: str = "interleaved"
 
     def __post_init__(self):
+        object.__setattr__(self, "sections", tuple(self.sections))
+        object.__setattr__(self, "freqs", tuple(self.freqs))
         if self.pairing not in ("interleaved", "halves"):
             raise ValueError(self.pairing)
         if not 1 <= len(self.sections) <= 4 or sum(self.sections) != len(self.freqs):
@@ -171,6 +185,10 @@ class Rope:
         f = (ctypes.c_double * 64)(*self.freqs)
         s = _I32x4(*(_int(x, "sections", 0, 64) for x in self.sections))
         object.__setattr__(self, "_c", (len(self.sections), s, f))
+        object.__setattr__(self, "_hash", hash((self.sections, self.freqs, self.pairing)))
+
+    def __hash__(self):
+        return self._hash
 
 
 def rope_axes(dims, base=10000.0, pairing="interleaved", shared=False) -> Rope:
@@ -189,41 +207,20 @@ def rope_axes(dims, base=10000.0, pairing="interleaved", shared=False) -> Rope:
     return Rope(tuple(n // 2 for n in dims), f, pairing)
 
 
-def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=False,
-         layout="bhnd", q_out=None, k_out=None):
-    """Turns q and k (optional) by their tokens' positions. q: [B,H,n,d]
-    ("bhnd", "strided") or [B,n,H,d] ("bnhd"), any strides, k the same with its own head count.
-    Positions: `positions` int32 [axes,n] or [B,axes,n], or `grid` (axis
-    sizes; token i is element i in row-major order), shifted by `start`.
-    inverse=True turns back (also: the gradients of the turned rows to those
-    of the rows). q_out, k_out: outputs, by default new dense tensors of the same shape; passing q and k
-    themselves turns them in place. Returns q_out, or (q_out, k_out) with k."""
-    dt = _dtype(q)
-    B, H, n, d = _sizes(q, layout, "q")
-    axes, section, freq = r._c
-    if q_out is None:
-        q_out = _new(q)
-    else:
-        _same(q_out, q, "q_out")
-        _rows(q_out, "q_out", 4)
-        _expect(q_out, q.shape, "q_out")
-    Hk, zero = 0, _I64x3()
-    ks = kos = zero
+@_kept
+def _rope(r, q, k, q_out, k_out, positions, grid, start, inverse, layout):
+    dtype = q[2]
+    dt = _dtype(dtype)
+    (B, H, n, d), qs = _heads(q, layout, "q", dtype)
+    qos = _heads(q_out or _dense(q), layout, "q_out", dtype, q[0])[1]
+    Hk, ks, kos = 0, _I64x3(), _I64x3()
     if k is not None:
-        _same(k, q, "k")
-        Bk, Hk, nk, dk = _sizes(k, layout, "k")
+        (Bk, Hk, nk, dk), ks = _heads(k, layout, "k", dtype)
         if (Bk, nk, dk) != (B, n, d):
             raise ValueError("q and k must have the same batch, tokens and head dimension")
-        if k_out is None:
-            k_out = _new(k)
-        else:
-            _same(k_out, q, "k_out")
-            _rows(k_out, "k_out", 4)
-            _expect(k_out, k.shape, "k_out")
-        ks, kos = _strides(k, layout), _strides(k_out, layout)
-    if (grid is None) == (positions is None):
-        raise ValueError("give either grid or positions")
-    g, s, ps = _I32x4(), _I32x4(), zero
+        kos = _heads(k_out or _dense(k), layout, "k_out", dtype, k[0])[1]
+    axes, section, freq = r._c
+    g, s, ps = _I32x4(), _I32x4(), _I64x3()
     if grid is not None:
         if len(grid) != axes or (start is not None and len(start) != axes):
             raise ValueError(f"grid and start need {axes} entries")
@@ -233,21 +230,41 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     else:
         if start is not None:
             raise ValueError("start goes with grid")
-        if positions.dtype != torch.int32 or positions.device != q.device:
-            raise ValueError(f"positions: expected int32 on {q.device}")
-        z, t = tuple(positions.shape), positions.stride()
-        if z == (axes, n):
-            ps = _I64x3(0, t[0], t[1])
-        elif z in ((B, axes, n), (1, axes, n)):
-            ps = _I64x3(t[0] if z[0] > 1 else 0, t[1], t[2])
-        else:
-            raise ValueError(f"positions: expected [{axes}, {n}] or [{B}, {axes}, {n}], got "
-                             f"{list(z)}")
-    c = _lib.CaRope(B, H, Hk, n, d, dt, axes, section, int(r.pairing == "halves"), int(inverse),
-                    g, s, ps, _strides(q, layout), ks, _strides(q_out, layout), kos, freq)
-    _call("ca_rope", q.device, c, q.data_ptr(), _ptr(k), _ptr(positions), q_out.data_ptr(),
-          _ptr(k_out) if k is not None else None)
-    return q_out if k is None else (q_out, k_out)
+        _int32(positions, "positions", (axes, n), (B, axes, n), (1, axes, n))
+        t = positions[1]
+        ps = _I64x3(0 if len(t) == 2 or positions[0][0] == 1 else t[0], t[-2], t[-1])
+    return _lib.CaRope(B, H, Hk, n, d, dt, axes, section, int(r.pairing == "halves"), int(inverse),
+                       g, s, ps, qs, ks, qos, kos, freq)
+
+
+def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=False,
+         layout="bhnd", q_out=None, k_out=None):
+    """Turns q and k (optional) by their tokens' positions. q: [B,H,n,d]
+    ("bhnd", "strided") or [B,n,H,d] ("bnhd"), any strides, k the same with its
+    own head count. Positions: `positions` int32 [axes,n] or [B,axes,n], or
+    `grid` (axis sizes; token i is element i in row-major order), shifted by
+    `start`. inverse=True turns back (also: the gradients of the turned rows to
+    those of the rows). q_out, k_out: outputs, by default new dense tensors of
+    the same shape; passing q and k themselves turns them in place. Returns
+    q_out, or (q_out, k_out) with k."""
+    if (grid is None) == (positions is None):
+        raise ValueError("give either grid or positions")
+    _on(q, k, positions, q_out, k_out)
+    c = _rope(r, _geo(q), None if k is None else _geo(k), None if q_out is None else _geo(q_out),
+              None if k_out is None else _geo(k_out),
+              None if positions is None else _geo(positions),
+              None if grid is None else tuple(grid), None if start is None else tuple(start),
+              inverse, layout)
+    if q_out is None:
+        q_out = _new(q)
+    if k is None:
+        _call("ca_rope", q.device, c, q.data_ptr(), None, _ptr(positions), q_out.data_ptr(), None)
+        return q_out
+    if k_out is None:
+        k_out = _new(k)
+    _call("ca_rope", q.device, c, q.data_ptr(), k.data_ptr(), _ptr(positions), q_out.data_ptr(),
+          k_out.data_ptr())
+    return q_out, k_out
 
 
 # ---- window attention ----------------------------------------------------------------
@@ -263,33 +280,37 @@ class Window:
     causal: bool = False
 
 
-def _window(w, q, k, v, out, scale, len_q, len_k, layout, grads=()):
-    dt = _dtype(q)
-    B, H, nq, d = _sizes(q, layout, "q")
-    Bk, Hk, nk, dk = _sizes(k, layout, "k")
-    _same(k, q, "k")
-    _same(v, q, "v")
-    _rows(v, "v", 4)
-    _expect(v, k.shape, "v")
+@_kept
+def _window(w, q, k, v, out, scale, len_q, len_k, layout, grads):
+    """(descriptor, bytes of workspace); grads: of the backward pass, dout and the three
+    gradients."""
+    dtype = q[2]
+    dt = _dtype(dtype)
+    (B, H, nq, d), qs = _heads(q, layout, "q", dtype)
+    (Bk, Hk, nk, dk), ks = _heads(k, layout, "k", dtype)
     if (Bk, dk) != (B, d):
         raise ValueError("q and k must have the same batch and head dimension")
+    vs = _heads(v, layout, "v", dtype, k[0])[1]
+    os = _heads(out or _dense(q), layout, "out", dtype, q[0])[1]
     for t, name in ((len_q, "len_q"), (len_k, "len_k")):
         if t is not None:
-            _int32(t, (B,), q, name)
-    _same(out, q, "out")
-    _rows(out, "out", 4)
-    _expect(out, q.shape, "out")
-    return _lib.CaWindow(B, H, Hk, nq, nk, d, dt, _side(w.left), _side(w.right),
-                         min(w.sinks, _MOST), int(w.causal),
-                         0.0 if scale is None else float(scale), _strides(q, layout),
-                         _strides(k, layout), _strides(v, layout), _strides(out, layout),
-                         *(_strides(t, layout) for t in grads))
+            _int32(t, name, (B,))
+            if t[1][0] != 1 and B > 1:
+                raise ValueError(f"{name} must be contiguous")
+    gs = ()
+    if grads is not None:
+        like = (("dout", q), ("dq", q), ("dk", k), ("dv", v))
+        gs = tuple(_heads(t or _dense(x), layout, name, dtype, x[0])[1]
+                   for t, (name, x) in zip(grads, like))
+    c = _lib.CaWindow(B, H, Hk, nq, nk, d, dt, _side(w.left), _side(w.right),
+                      _int(min(w.sinks, _MOST), "sinks"), int(w.causal),
+                      0.0 if scale is None else float(scale), qs, ks, vs, os, *gs)
+    return c, _bytes("ca_window_workspace_size", c, int(grads is not None))
 
 
-def _lse(q, layout):
+def _lse_shape(q, layout):
     z = q.shape
-    H, n = (z[2], z[1]) if layout == "bnhd" else (z[1], z[2])
-    return q.new_empty((z[0], H, n), dtype=torch.float32)
+    return (z[0], z[2], z[1]) if layout == "bnhd" else (z[0], z[1], z[2])
 
 
 def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layout="bhnd",
@@ -299,11 +320,14 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
     tokens and heads_k heads (a divisor of H). len_q, len_k: int32 [B], the
     lengths in a padded batch. Returns (out, lse [B,H,nq] fp32 or None); rows
     that see no key, and rows past len_q, are 0 with lse -inf."""
+    _on(q, k, v, out, len_q, len_k)
+    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), None if out is None else _geo(out), scale,
+                        None if len_q is None else _geo(len_q),
+                        None if len_k is None else _geo(len_k), layout, None)
     if out is None:
         out = _new(q)
-    c = _window(w, q, k, v, out, scale, len_q, len_k, layout)
-    lse = _lse(q, layout) if want_lse else None
-    ws = _workspace("ca_window_workspace_size", c, 0, device=q.device, ws=ws)
+    lse = q.new_empty(_lse_shape(q, layout), dtype=torch.float32) if want_lse else None
+    ws = _workspace(nbytes, q, ws)
     _call("ca_window_attn", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(len_q),
           _ptr(len_k), out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes)
     return out, lse
@@ -315,16 +339,16 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     dout, from out and lse as window_attn gave them for the same arguments.
     dq, dk, dv: outputs of the inputs' shapes (any strides, for example slices
     of a fused projection's gradient), new dense tensors by default."""
+    _on(q, k, v, out, lse, dout, len_q, len_k, dq, dk, dv)
+    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), _geo(out), scale,
+                        None if len_q is None else _geo(len_q),
+                        None if len_k is None else _geo(len_k), layout,
+                        (_geo(dout), *(None if t is None else _geo(t) for t in (dq, dk, dv))))
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or \
+            tuple(lse.shape) != _lse_shape(q, layout):
+        raise ValueError("lse: expected a contiguous fp32 tensor of [B, H, nq]")
     dq, dk, dv = (_new(t) if g is None else g for t, g in ((q, dq), (k, dk), (v, dv)))
-    for t, like, name in ((dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        _same(t, q, name)
-        _rows(t, name, 4)
-        _expect(t, like.shape, name)
-    c = _window(w, q, k, v, out, scale, len_q, len_k, layout, (dout, dq, dk, dv))
-    if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous():
-        raise ValueError("lse: expected a contiguous fp32 tensor on the same device")
-    _expect(lse, (c.batch, c.heads, c.nq), "lse")
-    ws = _workspace("ca_window_workspace_size", c, 1, device=q.device, ws=ws)
+    ws = _workspace(nbytes, q, ws)
     _call("ca_window_attn_backward", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           out.data_ptr(), lse.data_ptr(), dout.data_ptr(), _ptr(len_q), _ptr(len_k),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes)
@@ -333,27 +357,33 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
 
 # ---- paged cache -----------------------------------------------------------------------
 
-def _paged(q, heads, k_pages, v_pages, table, lens, left, sinks, scale, q_st=None, o_st=None,
-           n_new=0, kn=None, vn=None):
-    dt = _dtype(k_pages)
-    _rows(k_pages, "k_pages", 4)
-    _rows(v_pages, "v_pages", 4)
-    _same(v_pages, k_pages, "v_pages")
-    _expect(v_pages, k_pages.shape, "v_pages")
-    _same(q, k_pages, "queries or new keys")
-    P, page, Hk, d = k_pages.shape
-    B = q.shape[0]
-    if q.shape[-1] != d:
-        raise ValueError(f"expected rows of {d}, got {q.shape[-1]}")
-    if table.dim() != 2:
+@_kept
+def _paged(k_pages, v_pages, table, lens, batch, heads, left, sinks, scale, q, out, k, v):
+    """(descriptor, bytes of workspace) of an append (k, v given) or an attention (q
+    given)."""
+    dtype = k_pages[2]
+    dt = _dtype(dtype)
+    (P, page, Hk, d), ks = _rows(k_pages, "k_pages", 4, dtype)
+    vs = _rows(v_pages, "v_pages", 4, dtype, k_pages[0])[1]
+    if len(table[0]) != 2:
         raise ValueError("page_table: expected [B, max_pages]")
-    _int32(table, (B, table.shape[1]), k_pages, "page_table")
-    _int32(lens, (B,), k_pages, "lens")
+    _int32(table, "page_table", (batch, table[0][1]))
+    _int32(lens, "lens", (batch,))
+    if (table[1][1] != 1 and table[0][1] > 1) or (lens[1][0] != 1 and batch > 1):
+        raise ValueError("lens and the rows of page_table must be contiguous")
     z3, z2 = _I64x3(), _I64x2()
-    return _lib.CaPaged(B, heads, Hk, d, dt, page, P, table.shape[1], _side(left), min(sinks, _MOST),
-                        0.0 if scale is None else float(scale),
-                        table.stride(0) if B > 1 else 0, _lead(k_pages),
-                        _lead(v_pages), q_st or z2, o_st or z2, n_new, kn or z3, vn or z3)
+    qs, os, kn, vn, n = z2, z2, z3, z3, 0
+    if q is not None:
+        size, st = _rows(q, "q", 3, dtype, (batch, heads, d))
+        qs, os = _I64x2(*st[:2]), _I64x2(*_rows(out or _dense(q), "out", 3, dtype, q[0])[1][:2])
+    else:
+        size, st = _rows(k, "k", 4, dtype, (batch, k[0][1], Hk, d))
+        n, kn, vn = size[1], _I64x3(*st[:3]), _I64x3(*_rows(v, "v", 4, dtype, k[0])[1][:3])
+    c = _lib.CaPaged(batch, heads, Hk, d, dt, page, P, table[0][1], _side(left),
+                     _int(min(sinks, _MOST), "sinks"), 0.0 if scale is None else float(scale),
+                     table[1][0] if batch > 1 else 0, _I64x3(*ks[:3]), _I64x3(*vs[:3]), qs, os,
+                     n, kn, vn)
+    return c, _bytes("ca_paged_workspace_size", c) if q is not None else 0
 
 
 def cache_append(k, v, k_pages, v_pages, page_table, lens):
@@ -361,14 +391,11 @@ def cache_append(k, v, k_pages, v_pages, page_table, lens):
     pages: the last n of the lens[b] tokens of sequence b (lens counts them
     already). k_pages, v_pages: [pages, page, Hk, d], any strides;
     page_table: int32 [B, max_pages]; lens: int32 [B]. Returns nothing."""
-    _rows(k, "k", 4)
-    _rows(v, "v", 4)
-    _same(v, k, "v")
-    _expect(v, k.shape, "v")
-    if k_pages.dim() == 4 and k.shape[2] != k_pages.shape[2]:
-        raise ValueError(f"expected {k_pages.shape[2]} key heads, got {k.shape[2]}")
-    c = _paged(k, k.shape[2], k_pages, v_pages, page_table, lens, -1, 0, None, n_new=k.shape[1],
-               kn=_lead(k), vn=_lead(v))
+    _on(k, v, k_pages, v_pages, page_table, lens)
+    if k.dim() != 4:
+        raise ValueError("k: expected [B, n, Hk, d]")
+    c, _ = _paged(_geo(k_pages), _geo(v_pages), _geo(page_table), _geo(lens), k.shape[0],
+                  k.shape[2], -1, 0, None, None, None, _geo(k), _geo(v))
     _call("ca_cache_append", k.device, c, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
           v_pages.data_ptr(), page_table.data_ptr(), lens.data_ptr())
 
@@ -381,18 +408,16 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     any strides, Hk a divisor of H; page_table: int32 [B, max_pages]; lens:
     int32 [B], the new token included. Returns (out [B,H,d], lse [B,H] fp32 or
     None); a sequence of no tokens gives 0 and -inf."""
-    _rows(q, "q", 3)
+    _on(q, k_pages, v_pages, page_table, lens, out)
+    if q.dim() != 3:
+        raise ValueError("q: expected [B, H, d]")
+    B, H, _ = q.shape
+    c, nbytes = _paged(_geo(k_pages), _geo(v_pages), _geo(page_table), _geo(lens), B, H, left,
+                       sinks, scale, _geo(q), None if out is None else _geo(out), None, None)
     if out is None:
         out = _new(q)
-    else:
-        _same(out, q, "out")
-        _rows(out, "out", 3)
-        _expect(out, q.shape, "out")
-    B, H = q.shape[0], q.shape[1]
-    c = _paged(q, H, k_pages, v_pages, page_table, lens, left, sinks, scale, _lead(q),
-               _lead(out))
     lse = q.new_empty((B, H), dtype=torch.float32) if want_lse else None
-    ws = _workspace("ca_paged_workspace_size", c, device=q.device, ws=ws)
+    ws = _workspace(nbytes, q, ws)
     _call("ca_paged_attn", q.device, c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
           page_table.data_ptr(), lens.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(ws),
           0 if ws is None else ws.nbytes)
