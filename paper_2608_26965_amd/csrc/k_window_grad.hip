@@ -36,7 +36,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
-constexpr int kRows = 128;       // kept rows of a workgroup
+constexpr int kPad = 128;        // lse2 and delta are padded to this
 constexpr int KT = 64;           // streamed rows of a tile
 
 // Kept rows of a wavefront: 32 at d = 64, 16 at d = 128, where the operands and sums of
@@ -48,6 +48,10 @@ template <int D>
 constexpr int grad_rows() {
   return D == 64 ? 32 : 16;
 }
+// ... and of a workgroup: two of them share a compute unit and are not at the same point of a
+// tile at the same time (d = 128: one workgroup of 128 rows took 775 us where two of 64
+// take 761, and 487 where they take 447)
+constexpr int grad_block(int d) { return d == 64 ? 128 : 64; }
 // A product of W kept rows: W x W x K, accumulator r of a lane being row 8 (r / 4) + 4 g
 // + r % 4 (g = lane / W) of kept row lane % W
 template <int W>
@@ -118,7 +122,7 @@ struct GradArgs {
   Lay lx, ly, la, lb;
   const bf16* out;            // queries kept: the attention's output, for D
   const float* lse;
-  float *lse2, *delta;        // [B H][nq padded to kRows]: lse log2(e), -D (inf and 0 past the lengths)
+  float *lse2, *delta;        // [B H][nq padded to kPad]: lse log2(e), -D (inf and 0 past the lengths)
   bf16 *g0, *g1;
   Lay lg0, lg1;
   float* part;                // [heads][places][kRows][2][d]
@@ -129,8 +133,8 @@ struct GradArgs {
 };
 
 template <int D, bool KEYS>
-__global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
-  constexpr int W = grad_rows<D>(), NW = kRows / W;
+__global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
+  constexpr int W = grad_rows<D>(), kRows = grad_block(D), NW = kRows / W;
   typedef Mma<W> M;
   constexpr int KK = D / M::K, DT = D / W, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
   const int b = hx / HX, lq = P.qlen(b), lk = P.klen(b), off = lk - lq;
   const int n = KEYS ? lk : lq, nmax = KEYS ? P.nk : P.nq, r0 = blk * kRows;
   const int real = max(0, min(kRows, n - r0));
-  const int nqp = (P.nq + kRows - 1) / kRows * kRows;
+  const int nqp = (P.nq + kPad - 1) / kPad * kPad;
 
   // the tiles that one of the block's rows sees
   TileList list{0, 0, 0};
@@ -547,7 +551,7 @@ __global__ __launch_bounds__(64 * kRows / grad_rows<D>(), 2) void window_grad_ke
 template <int D, bool KEYS>
 __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, const GradArgs g,
                                                                int ncut, int first_cut) {
-  constexpr int E = D / 32;  // elements of a lane
+  constexpr int E = D / 32, kRows = grad_block(D);  // elements of a lane, rows of a block
   const int HX = KEYS ? P.Hk : P.H, nmax = KEYS ? P.nk : P.nq;
   const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -575,7 +579,7 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
   }
   const bool on = r < (KEYS ? P.klen(b) : P.qlen(b));
   if (!KEYS && lane == 0) {
-    const int nqp = (P.nq + kRows - 1) / kRows * kRows;
+    const int nqp = (P.nq + kPad - 1) / kPad * kPad;
     if (on) g.delta[(size_t)hx * nqp + r] -= rs;
   }
   if (r >= nmax) return;
@@ -597,7 +601,7 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
 // two of 18 (166).
 Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int d, bool uneven) {
   static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-  const int64_t slots = d == 64 ? 512 : 256;
+  const int64_t slots = 512;  // two workgroups a compute unit
   if (nsink > nb) nsink = nb;
   Parts best{nb, nsink, 1, 1};
   double least = -1;
@@ -630,7 +634,7 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int d, bo
   return best;
 }
 Parts query_parts(const WinProb& P) {
-  const int nb = (P.nq + kRows - 1) / kRows;
+  const int kRows = grad_block(P.d), nb = (P.nq + kRows - 1) / kRows;
   int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
   const int64_t tiles = (keys + KT - 1) / KT;
@@ -638,7 +642,7 @@ Parts query_parts(const WinProb& P) {
 }
 // keys kept: the blocks that hold sinks are seen by all queries
 Parts key_parts(const WinProb& P) {
-  const int nb = (P.nk + kRows - 1) / kRows;
+  const int kRows = grad_block(P.d), nb = (P.nk + kRows - 1) / kRows;
   const int64_t all = (int64_t)(P.nq + KT - 1) / KT * P.G;
   int64_t seen = (((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1) * P.G;
   if (seen > all) seen = all;
@@ -653,7 +657,8 @@ struct GradPlan {
   size_t lse2, delta, part, rpart, total;
 };
 GradPlan plan(const WinProb& P) {
-  const size_t nqp = (size_t)(P.nq + kRows - 1) / kRows * kRows, rows = (size_t)P.B * P.H * nqp;
+  const int kRows = grad_block(P.d);
+  const size_t nqp = (size_t)(P.nq + kPad - 1) / kPad * kPad, rows = (size_t)P.B * P.H * nqp;
   // the two kernels' partial sums follow one another in the same place
   const size_t pq = (size_t)P.B * P.H * query_parts(P).places() * kRows;
   const size_t pk = (size_t)P.B * P.Hk * key_parts(P).places() * kRows;
@@ -670,13 +675,13 @@ template <int D, bool KEYS>
 hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
   const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
   hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
-                     dim3(64 * kRows / grad_rows<D>()), 0, st, P, g);
+                     dim3(64 * grad_block(D) / grad_rows<D>()), 0, st, P, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts.places() == 0) return e;
   const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
   const int ncut = (g.parts.p > 1 ? g.parts.nb : g.parts.nsink) - first;
   hipLaunchKernelGGL((window_grad_join_kernel<D, KEYS>),
-                     dim3((unsigned)(((int64_t)heads * ncut * kRows + 7) / 8)), dim3(256), 0, st, P, g,
+                     dim3((unsigned)(((int64_t)heads * ncut * grad_block(D) + 7) / 8)), dim3(256), 0, st, P, g,
                      ncut, first);
   return hipGetLastError();
 }
