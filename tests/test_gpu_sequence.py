@@ -635,3 +635,107 @@ def test_other_stream_and_graph_replays():
         want = step() + serve()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+
+
+# ---- places, streams, workspaces ----------------------------------------------------------------
+
+def test_offsets_past_32_bits():
+    """Heads and pages whose elements lie past 2^32: every call on such views gives what it
+    gives on dense copies."""
+    import torch
+    ca = _ca()
+    g = _gen(30)
+    far = 2 ** 32 + 2 ** 20  # elements; 8.6 GB in bf16
+    pool = torch.empty(far + 2 ** 20, dtype=torch.bfloat16, device="cuda")
+
+    n, d = 300, 64
+    near = [_rand(g, (1, 2, n, d), "bf16").cuda() for _ in range(4)]
+    q, k, v, do = (pool.as_strided((1, 2, n, d), (0, far, d, 1), 32768 * i) for i in range(4))
+    for t, x in zip((q, k, v, do), near):
+        t.copy_(x)
+    w = ca.Window(left=100, sinks=70, causal=True)
+    a, b = ca.window_attn(w, q, k, v, want_lse=True), ca.window_attn(w, *near[:3], want_lse=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    ga = ca.window_attn_backward(w, do, q, k, v, *a)
+    gb = ca.window_attn_backward(w, near[3], *near[:3], *b)
+    assert all(torch.equal(x, y) for x, y in zip(ga, gb))
+    r = ca.rope_axes((32, 32))
+    y = ca.rope(r, near[0], near[1], grid=(15, 20))
+    ca.rope(r, q, k, grid=(15, 20), q_out=q, k_out=k)
+    assert torch.equal(q, y[0]) and torch.equal(k, y[1])
+    # pages: two of 64 tokens, the second one past 2^32
+    kp, vp = (pool.as_strided((2, 64, 2, 64), (far, 128, 64, 1), 8192 * (40 + i)) for i in range(2))
+    kn, vn = (_rand(g, (1, 100, 2, 64), "bf16").cuda() for _ in range(2))
+    table, lens = torch.tensor([[1, 0]], dtype=torch.int32).cuda(), torch.tensor([100], dtype=torch.int32).cuda()
+    ca.cache_append(kn, vn, kp, vp, table, lens)
+    assert torch.equal(kp[1], kn[0, :64]) and torch.equal(vp[0, :36], vn[0, 64:])
+    qq = _rand(g, (1, 4, 64), "bf16").cuda()
+    a = ca.paged_attn(qq, kp, vp, table, lens, want_lse=True)
+    b = ca.paged_attn(qq, kp.clone(), vp.clone(), table, lens, want_lse=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_two_streams_at_once(dt):
+    """The same calls on two streams at the same time, each with its own tensors."""
+    import torch
+    ca = _ca()
+    r, w = ca.rope_axes((32, 32)), ca.Window(left=60, right=9, sinks=70)
+    g = _gen(31)
+    sets = [[_rand(g, (2, h, 400, 64), dt).cuda() for h in (4, 2, 2, 4)] for _ in range(2)]
+
+    def step(q, k, v, do):
+        qr, kr = ca.rope(r, q, k, grid=(20, 20))
+        out, lse = ca.window_attn(w, qr, kr, v, want_lse=True)
+        return (out, lse) + ca.window_attn_backward(w, do, qr, kr, v, out, lse)
+
+    want = [step(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for _ in range(3):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i] = step(*sets[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_given_outputs_and_workspaces(dt):
+    """Outputs of other strides, workspaces of the caller's (too small ones are refused),
+    no lse."""
+    import torch
+    ca = _ca()
+    g = _gen(32)
+    q, k, v = (_rand(g, (1, 9, 2, 64), dt).cuda(), *(_rand(g, (1, 5000, 2, 64), dt).cuda() for _ in range(2)))
+    w = ca.Window()
+    a, lse = ca.window_attn(w, q, k, v, layout="bnhd", want_lse=True)
+    big = torch.zeros(1, 9, 4, 128, dtype=_torch(dt), device="cuda")
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    b, none = ca.window_attn(w, q, k, v, layout="bnhd", out=big[:, :, 1:3, 64:], ws=ws)
+    assert none is None and torch.equal(a, b) and not big[:, :, 0].any() and not big[..., :64].any()
+    with pytest.raises(ca.CAError, match="workspace"):
+        ca.window_attn(w, q, k, v, layout="bnhd", ws=ws[:256])
+    with pytest.raises(ca.CAError, match="workspace"):
+        ca.window_attn_backward(w, a, q, k, v, a, lse, layout="bnhd", ws=ws[:256])
+    x = ca.window_attn_backward(w, a, q, k, v, a, lse, layout="bnhd", ws=ws)
+    y = ca.window_attn_backward(w, a, q, k, v, a, lse, layout="bnhd")
+    assert all(torch.equal(s, t) for s, t in zip(x, y))
+    table, lens = torch.arange(5000, dtype=torch.int32, device="cuda")[None], torch.tensor([5000], dtype=torch.int32).cuda()
+    kp, vp = k[0][:, None], v[0][:, None]
+    out = torch.zeros(1, 4, 64, dtype=_torch(dt), device="cuda")
+    a, _ = ca.paged_attn(q[:, 0], kp, vp, table, lens)
+    b, _ = ca.paged_attn(q[:, 0], kp, vp, table, lens, out=out[:, ::2], ws=ws)
+    assert torch.equal(a, b) and not out[:, 1::2].any()
+    with pytest.raises(ca.CAError, match="workspace"):
+        ca.paged_attn(q[:, 0], kp, vp, table, lens, ws=ws[:256])
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,nk,kw", [(1, 40000, dict(causal=True)), (20, 9000, dict()), (5000, 3, dict(sinks=2, left=1)),
+                                      (700, 700, dict(sinks=650, left=5, causal=True))])
+def test_window_cut_into_parts(dt, d, nq, nk, kw):
+    """Few queries on many keys, few keys under many queries, blocks of sinks: launches that
+    are cut into parts and joined."""
+    _window_case(dt, 1, 2, 1, nq, nk, d, seed=nk, **kw)
