@@ -487,6 +487,12 @@ PagedPlan paged_plan(const PagedProb& P) {
   // the window: 114 and 119).
   const int parts = P.B >= 8 ? 4096 : 2048;
   int64_t tiles = (all * wgs + parts - 1) / parts;
+  // A table can hold far more than the sequences have: 64 tiles at most keep short
+  // sequences in wide tables parallel (20 parts of 40,000 keys in a table for a million),
+  // up to 65,536 workgroups. (Parts sized on the device by the sum of the lengths, for
+  // which every workgroup reads them, were slower: 32 ragged sequences 256 to 299 us.)
+  if (tiles > 64) tiles = 64;
+  if (tiles < (all * wgs) >> 16) tiles = (all * wgs) >> 16;
   if (tiles < kPartTiles) tiles = kPartTiles;
   if (all <= tiles + 2) return PagedPlan{1, (int)all};
   return PagedPlan{(int)((all + tiles - 1) / tiles), (int)tiles};

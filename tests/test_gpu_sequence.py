@@ -739,3 +739,23 @@ def test_window_cut_into_parts(dt, d, nq, nk, kw):
     """Few queries on many keys, few keys under many queries, blocks of sinks: launches that
     are cut into parts and joined."""
     _window_case(dt, 1, 2, 1, nq, nk, d, seed=nk, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_paged_wide_tables_and_many_lengths(dt):
+    """Seventy sequences of 0 to 3,000 tokens in tables that could hold 64,000: parts go by
+    the lengths, and a sequence's result does not depend on the others beyond rounding."""
+    import torch
+    ca = _ca()
+    g = _gen(33)
+    lens = [int(x) for x in np.random.default_rng(1).integers(0, 400, 70)]
+    lens[3], lens[40], lens[69] = 3000, 0, 1111
+    kp, vp, table, rows = _pages(g, dt, lens, 16, 1, 64)
+    wide = torch.full((70, 4000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    q = _rand(g, (70, 2, 64), dt).cuda()
+    n = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, wide, n, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, -1, 0, dt)
+    out, lse = ca.paged_attn(q, kp, vp, wide, n, left=500, sinks=50, want_lse=True)
+    _paged_check(q, out, lse, lens, rows, 500, 50, dt)
