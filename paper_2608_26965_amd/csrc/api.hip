@@ -703,6 +703,13 @@ int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const int32_t* 
       if (cells < p->n) cells *= p->grid[a];
     }
   }
+  // A grid may be larger than n and its products than 32 bits: past every token the place
+  // on the axis is 0, whatever the product
+  int64_t inner = 1;
+  for (int a = ca::kMaxAxes - 1; a >= 0; --a) {
+    P.inner[a] = (int)inner;
+    inner = std::min<int64_t>(inner * P.grid[a], INT32_MAX);
+  }
   if (P.npairs < 1 || 2 * P.npairs > p->d)
     return fail(CA_E_INVALID, "2 * (sum of section) = %d must be in [2, d = %d]", 2 * P.npairs, p->d);
   if (p->halves && P.npairs % unit != 0)

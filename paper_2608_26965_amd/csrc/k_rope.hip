@@ -49,10 +49,7 @@ __device__ __forceinline__ void sincos_of(int pos, double freq, float* s, float*
 
 __device__ __forceinline__ int axis_position(const RopeProb& P, int b, int a, int i) {
   if (P.pos) return P.pos[b * P.pos_sb + a * P.pos_sa + i * P.pos_sn];
-  int inner = 1;
-  for (int x = kMaxAxes - 1; x > 0; --x)
-    if (x > a && x < P.axes) inner *= P.grid[x];
-  return (i / inner) % P.grid[a] + P.start[a];
+  return (i / P.inner[a]) % P.grid[a] + P.start[a];
 }
 
 template <typename T>

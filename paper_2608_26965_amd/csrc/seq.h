@@ -102,6 +102,7 @@ struct RopeProb {
   int axes, npairs, halves;
   int end[kMaxAxes];   // pairs [end[a - 1], end[a]) turn with axis a
   int grid[kMaxAxes], start[kMaxAxes];
+  int inner[kMaxAxes]; // tokens between neighbours on the axis; INT32_MAX from n on
   float sign;          // of the angle: -1 for the transposed rotation
   const int32_t* pos;  // NULL: from the grid
   int64_t pos_sb, pos_sa, pos_sn;

@@ -161,6 +161,17 @@ def test_rope_in_place_strided_and_back():
     assert torch.equal(ca.rope(r, q, grid=(2, 3, 5), start=(7, -2, 100)), ca.rope(r, q, positions=p))
 
 
+@pytest.mark.parametrize("grid", [(2, 1 << 16, 1 << 16), (3, 5, 1 << 16, 1 << 15), (7, 3, (1 << 31) - 8)])
+def test_rope_grid_beyond_32_bits(grid):
+    """The grid may hold more tokens than the call and than 32 bits count."""
+    import torch
+    ca = _ca()
+    x = _rand(_gen(11), (1, 2, 70, 64), "f32").cuda()
+    r = ca.rope_axes((16,) * len(grid))
+    p = torch.from_numpy(seq.grid_positions(70, grid).astype(np.int32)).cuda()
+    assert torch.equal(ca.rope(r, x, grid=grid), ca.rope(r, x, positions=p))
+
+
 def test_rope_dims_that_do_not_turn_keep_any_value():
     import torch
     ca = _ca()
