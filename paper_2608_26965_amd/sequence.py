@@ -37,8 +37,9 @@ _I32x4 = ctypes.c_int32 * 4
 #
 # A call's descriptor (sizes, strides, type, options) takes longer to make than the
 # launch of a small kernel, and a program makes the same few calls again and again:
-# descriptors are kept by what they are made from. They hold no address, and no
-# value of a tensor.
+# descriptors are kept by what they are made from. They hold no address. Numbers are
+# made Python's own before they become part of a key: a tensor of one element is equal to
+# itself whatever it holds by now.
 _kept = functools.lru_cache(maxsize=1024)
 
 
@@ -121,6 +122,14 @@ def _int(x, name, least=-_MOST - 1, most=_MOST):
     return x
 
 
+def _ints(x):
+    return None if x is None else tuple(int(i) for i in x)
+
+
+def _scale(x):
+    return None if x is None else float(x)
+
+
 def _side(x):
     # a window wider than any sequence is no limit; so is a negative one
     return -1 if x < 0 or x > _MOST else int(x)
@@ -174,8 +183,8 @@ class Rope:
     pairing: str = "interleaved"
 
     def __post_init__(self):
-        object.__setattr__(self, "sections", tuple(self.sections))
-        object.__setattr__(self, "freqs", tuple(self.freqs))
+        object.__setattr__(self, "sections", _ints(self.sections))
+        object.__setattr__(self, "freqs", tuple(float(x) for x in self.freqs))
         if self.pairing not in ("interleaved", "halves"):
             raise ValueError(self.pairing)
         if not 1 <= len(self.sections) <= 4 or sum(self.sections) != len(self.freqs):
@@ -252,9 +261,8 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     _on(q, k, positions, q_out, k_out)
     c = _rope(r, _geo(q), None if k is None else _geo(k), None if q_out is None else _geo(q_out),
               None if k_out is None else _geo(k_out),
-              None if positions is None else _geo(positions),
-              None if grid is None else tuple(grid), None if start is None else tuple(start),
-              inverse, layout)
+              None if positions is None else _geo(positions), _ints(grid), _ints(start),
+              bool(inverse), layout)
     if q_out is None:
         q_out = _new(q)
     if k is None:
@@ -278,6 +286,11 @@ class Window:
     right: int = -1
     sinks: int = 0
     causal: bool = False
+
+    def __post_init__(self):
+        for x in ("left", "right", "sinks"):
+            object.__setattr__(self, x, int(getattr(self, x)))
+        object.__setattr__(self, "causal", bool(self.causal))
 
 
 @_kept
@@ -304,7 +317,7 @@ def _window(w, q, k, v, out, scale, len_q, len_k, layout, grads):
                    for t, (name, x) in zip(grads, like))
     c = _lib.CaWindow(B, H, Hk, nq, nk, d, dt, _side(w.left), _side(w.right),
                       _int(min(w.sinks, _MOST), "sinks"), int(w.causal),
-                      0.0 if scale is None else float(scale), qs, ks, vs, os, *gs)
+                      0.0 if scale is None else scale, qs, ks, vs, os, *gs)
     return c, _bytes("ca_window_workspace_size", c, int(grads is not None))
 
 
@@ -321,7 +334,7 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
     lengths in a padded batch. Returns (out, lse [B,H,nq] fp32 or None); rows
     that see no key, and rows past len_q, are 0 with lse -inf."""
     _on(q, k, v, out, len_q, len_k)
-    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), None if out is None else _geo(out), scale,
+    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), None if out is None else _geo(out), _scale(scale),
                         None if len_q is None else _geo(len_q),
                         None if len_k is None else _geo(len_k), layout, None)
     if out is None:
@@ -340,7 +353,7 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     dq, dk, dv: outputs of the inputs' shapes (any strides, for example slices
     of a fused projection's gradient), new dense tensors by default."""
     _on(q, k, v, out, lse, dout, len_q, len_k, dq, dk, dv)
-    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), _geo(out), scale,
+    c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), _geo(out), _scale(scale),
                         None if len_q is None else _geo(len_q),
                         None if len_k is None else _geo(len_k), layout,
                         (_geo(dout), *(None if t is None else _geo(t) for t in (dq, dk, dv))))
@@ -380,7 +393,7 @@ def _paged(k_pages, v_pages, table, lens, batch, heads, left, sinks, scale, q, o
         size, st = _rows(k, "k", 4, dtype, (batch, k[0][1], Hk, d))
         n, kn, vn = size[1], _I64x3(*st[:3]), _I64x3(*_rows(v, "v", 4, dtype, k[0])[1][:3])
     c = _lib.CaPaged(batch, heads, Hk, d, dt, page, P, table[0][1], _side(left),
-                     _int(min(sinks, _MOST), "sinks"), 0.0 if scale is None else float(scale),
+                     _int(min(sinks, _MOST), "sinks"), 0.0 if scale is None else scale,
                      table[1][0] if batch > 1 else 0, _I64x3(*ks[:3]), _I64x3(*vs[:3]), qs, os,
                      n, kn, vn)
     return c, _bytes("ca_paged_workspace_size", c) if q is not None else 0
@@ -412,8 +425,8 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     if q.dim() != 3:
         raise ValueError("q: expected [B, H, d]")
     B, H, _ = q.shape
-    c, nbytes = _paged(_geo(k_pages), _geo(v_pages), _geo(page_table), _geo(lens), B, H, left,
-                       sinks, scale, _geo(q), None if out is None else _geo(out), None, None)
+    c, nbytes = _paged(_geo(k_pages), _geo(v_pages), _geo(page_table), _geo(lens), B, H, int(left),
+                       int(sinks), _scale(scale), _geo(q), None if out is None else _geo(out), None, None)
     if out is None:
         out = _new(q)
     lse = q.new_empty((B, H), dtype=torch.float32) if want_lse else None

@@ -192,3 +192,13 @@ def test_binding_refuses_cpu_tensors_and_shapes():
         ca.Rope((2,), (1.0, 2.0), "pairs")
     with pytest.raises(ValueError, match="sections"):
         ca.Rope((2 ** 32 + 2, -2 ** 32), (1.0, 2.0))
+
+
+def test_numbers_given_as_tensors_become_numbers():
+    import torch
+    import paper_2608_26965_amd as ca
+    t = torch.tensor(3)
+    w, r = ca.Window(left=t, sinks=t, causal=t), ca.Rope(torch.tensor([2, 1]), torch.tensor([1.0, 0.5, 0.25]))
+    t.fill_(7)
+    assert w == ca.Window(left=3, sinks=3, causal=True) and hash(w) == hash(ca.Window(3, -1, 3, True))
+    assert r == ca.Rope((2, 1), (1.0, 0.5, 0.25)) and hash(r) == hash(ca.Rope((2, 1), (1.0, 0.5, 0.25)))

@@ -393,6 +393,32 @@ def test_window_same_bits_twice(dt):
     assert all(torch.equal(a, b) for a, b in zip(*runs))
 
 
+def test_numbers_given_as_tensors_are_read_anew():
+    """A scale, a window or a grid held in a tensor of one element counts as it is at the call."""
+    import torch
+    ca = _ca()
+    g = _gen(21)
+    q, k, v = (_rand(g, (1, 2, 40, 64), "bf16").cuda() for _ in range(3))
+    kp, vp = (_rand(g, (4, 16, 2, 64), "bf16").cuda() for _ in range(2))
+    table = torch.arange(4, dtype=torch.int32).reshape(1, 4).cuda()
+    lens = torch.tensor([50], dtype=torch.int32).cuda()
+    r = ca.rope_axes((32, 32))
+    scale, left, rows = torch.tensor(0.25), torch.tensor(3), torch.tensor(10)
+    for s, n, h in ((0.25, 3, 10), (0.5, 9, 20)):
+        scale.fill_(s)
+        left.fill_(n)
+        rows.fill_(h)
+        a, lse = ca.window_attn(ca.Window(left=left), q, k, v, scale=scale, want_lse=True)
+        b, lse2 = ca.window_attn(ca.Window(left=n), q, k, v, scale=s, want_lse=True)
+        assert torch.equal(a, b) and torch.equal(lse, lse2)
+        for x, y in zip(ca.window_attn_backward(ca.Window(left=left), q, q, k, v, a, lse, scale=scale),
+                        ca.window_attn_backward(ca.Window(left=n), q, q, k, v, a, lse, scale=s)):
+            assert torch.equal(x, y)
+        assert torch.equal(ca.paged_attn(q[:, :, 0], kp, vp, table, lens, left=left, scale=scale)[0],
+                           ca.paged_attn(q[:, :, 0], kp, vp, table, lens, left=n, scale=s)[0])
+        assert torch.equal(ca.rope(r, q, grid=(4, rows)), ca.rope(r, q, grid=(4, h)))
+
+
 # ---- paged cache -----------------------------------------------------------------------------
 
 def _pages(g, dt, lens, page, Hk, d, heads_first=False, extra=2):
