@@ -323,6 +323,8 @@ def forward(q, k, v, cq=128, ck=None, keep=None, keep_k=None, transform="metric"
     frames, rows, columns) or by rope_positions, as in rope(); queries and keys
     then have as many tokens each."""
     ck = cq if ck is None else ck
+    if rotary is None and (rope_grid is not None or rope_positions is not None):
+        raise ValueError("rope_grid and rope_positions go with rotary")
     if rotary is not None:
         q, k = rope(rotary, q, k, grid=rope_grid, positions=rope_positions, layout=layout)
     if layout in ("bhnd", "strided"):

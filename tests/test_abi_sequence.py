@@ -202,3 +202,12 @@ def test_numbers_given_as_tensors_become_numbers():
     t.fill_(7)
     assert w == ca.Window(left=3, sinks=3, causal=True) and hash(w) == hash(ca.Window(3, -1, 3, True))
     assert r == ca.Rope((2, 1), (1.0, 0.5, 0.25)) and hash(r) == hash(ca.Rope((2, 1), (1.0, 0.5, 0.25)))
+
+
+@pytest.mark.parametrize("kw", [{"rope_grid": (2, 2)}, {"rope_positions": 1}])
+def test_forward_refuses_positions_without_rotary(kw):
+    import torch
+    import paper_2608_26965_amd as ca
+    x = torch.zeros(1, 2, 4, 64)
+    with pytest.raises(ValueError, match="go with rotary"):
+        ca.forward(x, x, x, keep=0.5, **kw)
