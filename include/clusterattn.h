@@ -391,7 +391,8 @@ CA_API int ca_attn_compensated_noalloc(const ca_problem* p, const void* qp, cons
  * - Tensors of rows of d are given by element strides (the last dimension is
  *   contiguous): each >= 0 and a multiple of 16 bytes' worth of elements, bases
  *   16-byte aligned. A stride of 0 repeats an input; rows of an output must not
- *   overlap (outputs with a stride of 0 over more than one row are refused).
+ *   overlap (outputs with a stride of 0 over more than one row are refused),
+ *   nor an output another tensor of the call, but for ca_rope in place.
  * - Query head h of `heads` reads key head h / (heads / heads_k); heads_k
  *   divides heads.
  * - Head dimensions: bf16 64 or 128, fp32 any multiple of 4 up to 128 (rotary:

@@ -1,8 +1,8 @@
 // Gradients of attention with a sliding window and sinks, bf16, on the matrix
 // cores.
 //
-// Two kernels of one form. Each keeps 128 rows a workgroup of two tensors in
-// registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
+// Two kernels of one form. Each keeps the rows of a block (grad_block) of two tensors
+// in registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
 // per tile, with P = e^{s - lse},
 //     S = X A^T,  E = Y B^T - D,  dS = P E,
 // whose accumulators (a lane holds one kept row and several streamed ones) are the
@@ -126,7 +126,7 @@ struct GradArgs {
   bf16 *g0, *g1;
   Lay lg0, lg1;
   float* part;                // [heads][places][kRows][2][d]
-  float* rpart;               // queries kept: [heads][places][kRows], then D as it starts
+  float* rpart;               // queries kept: [heads][places][kRows], sums of dS as rounded
   Parts parts;
   int contiguous;
   float sl2;
@@ -596,10 +596,10 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
 // without a window). Of the cuts below the one with the least time by this estimate, in
 // tiles: a workgroup costs three tiles beside its own; equal workgroups run in rounds of
 // as many as the chip holds, others fill it and leave half the longest over; partial sums
-// (128 x 2 d floats written and read) cost 0.015 each and a launch 3. 8,192 tokens on 2 key
+// (a block of 2 d floats a row, written and read) cost 0.015 each and a launch 3. 8,192 tokens on 2 key
 // heads take one round of 24 tiles (three parts, 159 us with the forward pass) instead of
 // two of 18 (166).
-Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int d, bool uneven) {
+Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool uneven) {
   static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   const int64_t slots = 512;  // two workgroups a compute unit
   if (nsink > nb) nsink = nb;
@@ -638,7 +638,7 @@ Parts query_parts(const WinProb& P) {
   int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
   const int64_t tiles = (keys + KT - 1) / KT;
-  return cut(nb, 0, tiles, tiles, (int64_t)P.B * P.H, P.d, P.m.causal && P.m.left >= P.nk);
+  return cut(nb, 0, tiles, tiles, (int64_t)P.B * P.H, P.m.causal && P.m.left >= P.nk);
 }
 // keys kept: the blocks that hold sinks are seen by all queries
 Parts key_parts(const WinProb& P) {
@@ -647,7 +647,7 @@ Parts key_parts(const WinProb& P) {
   int64_t seen = (((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1) * P.G;
   if (seen > all) seen = all;
   const int nsink = P.m.sinks < P.nk ? (P.m.sinks + kRows - 1) / kRows : nb;
-  return cut(nb, seen < all ? nsink : 0, all, seen, (int64_t)P.B * P.Hk, P.d,
+  return cut(nb, seen < all ? nsink : 0, all, seen, (int64_t)P.B * P.Hk,
              P.m.causal && P.m.left >= P.nk);
 }
 
