@@ -7,7 +7,10 @@
 // b1 b0 the key makes both reads free of bank conflicts: sixteen consecutive
 // rows at one lc fall on sixteen different chunks of 256 bytes, and the four
 // rows x 64 bytes that a half wavefront's transposing read takes fall on
-// different 32-byte pairs of chunks.
+// different 32-byte pairs of chunks. Where a product has sixteen rows, the lanes that
+// are served together hold rows 0-3 and 12-15 at one chunk and rows 4-11 at its
+// neighbour, lc ^ 1: the bit b2 ^ b3 keeps these two sets on chunks of their own (with
+// b2 in its place every such read took twice the time).
 #pragma once
 
 #include "attn_tile.h"
@@ -18,7 +21,8 @@ template <int RB>
 __device__ __forceinline__ int row_key(int r) {
   static_assert(RB == 128 || RB == 256, "row width");
   const int b0 = r & 1, b1 = (r >> 1) & 1, b2 = (r >> 2) & 1, b3 = (r >> 3) & 1;
-  return RB == 256 ? (b1 << 3) | (b0 << 2) | (b2 << 1) | b3 : (b1 << 2) | (b2 << 1) | b3;
+  const int m = b2 ^ b3;
+  return RB == 256 ? (b1 << 3) | (b0 << 2) | (m << 1) | b3 : (b1 << 2) | (m << 1) | b3;
 }
 
 // Copies ROWS rows of RB bytes, `stride` bytes apart, into an LDS tile, NW
