@@ -1,7 +1,7 @@
 // Gradients of attention with a sliding window and sinks, bf16, on the matrix
 // cores.
 //
-// Two kernels of one form. Each keeps the rows of a block (grad_block) of two tensors
+// Two kernels of one form. Each keeps a block of 64 rows of two tensors
 // in registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
 // per tile, with P = e^{s - lse},
 //     S = X A^T,  E = Y B^T - D,  dS = P E,
@@ -39,39 +39,24 @@ constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
 constexpr int kPad = 128;        // lse2 and delta are padded to this
 constexpr int KT = 64;           // streamed rows of a tile
 
-// Kept rows of a wavefront: 32 at d = 64, 16 at d = 128, where the operands and sums of
-// 32 take more than the 256 registers that two waves a SIMD have (one wave with 512,
-// half of them accumulation registers that its operands are copied through, took 793 us
-// for the padded batch of three, 16 rows 726; at d = 64 16 rows took 187 us for 8,192
-// tokens, 32 rows 168).
-template <int D>
-constexpr int grad_rows() {
-  return D == 64 ? 32 : 16;
+// Kept rows of a wavefront: sixteen, so that its operands and sums leave two waves a SIMD
+// at d = 128 and three at d = 64 (32 rows at d = 128, one wave with half the registers
+// accumulation registers that operands are copied through: 793 us for the padded batch
+// of three where 16 took 726; 32 rows at d = 64: 335 us where 16 take 307 (2 x 8 heads, 4,230
+// tokens), 175 and 150 (8,733 tokens, a short window), 184 and 190 (14,567, 3 heads)).
+constexpr int W = 16;
+// ... and of a workgroup: several share a compute unit and are not at the same point of a
+// tile at the same time (d = 128: workgroups of 128 rows take 713 to 720 us where those of 64
+// take 703 to 710, 468 and 430, 342 and 322, but 436 and 504 where 64 make 357 blocks;
+// d = 64: 336 and 307, 189 and 155)
+constexpr int kRows = 64, NW = kRows / W;
+// A product of 16 kept rows, 16 x 16 x 32: accumulator r of a lane is row 4 g + r
+// (g = lane / 16) of kept row lane % 16
+typedef f32x4 Acc;
+constexpr int MK = 32, MN = 4;
+__device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-// ... and of a workgroup: two of them share a compute unit and are not at the same point of a
-// tile at the same time (d = 128: one workgroup of 128 rows took 775 us where two of 64
-// take 761, and 487 where they take 447)
-constexpr int grad_block(int d) { return d == 64 ? 128 : 64; }
-// A product of W kept rows: W x W x K, accumulator r of a lane being row 8 (r / 4) + 4 g
-// + r % 4 (g = lane / W) of kept row lane % W
-template <int W>
-struct Mma;
-template <>
-struct Mma<32> {
-  typedef f32x16 Acc;
-  static constexpr int K = 16, N = 16;
-  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-  }
-};
-template <>
-struct Mma<16> {
-  typedef f32x4 Acc;
-  static constexpr int K = 32, N = 4;
-  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  }
-};
 
 // Row blocks and the parts that their streamed tiles are cut into. Blocks 0 ..
 // nsink - 1 are cut into `psink` parts (keys kept: the blocks that hold sinks,
@@ -133,10 +118,9 @@ struct GradArgs {
 };
 
 template <int D, bool KEYS>
-__global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
-  constexpr int W = grad_rows<D>(), kRows = grad_block(D), NW = kRows / W;
-  typedef Mma<W> M;
-  constexpr int KK = D / M::K, DT = D / W, RB = 2 * D, TILE = KT * RB;
+__global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
+    const WinProb P, const GradArgs g) {
+  constexpr int KK = D / MK, DT = D / W, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
   __shared__ __attribute__((aligned(16))) float rows[KEYS ? 2 : 1][2][KEYS ? KT : 4];
   const int nitem = g.parts.items();
@@ -208,19 +192,19 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
     const bf16* br = g.b + row_off(hx, row, g.lb);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      af[kk] = *(const bf16x8*)(ar + M::K * kk + 8 * gr);
-      bf[kk] = *(const bf16x8*)(br + M::K * kk + 8 * gr);
+      af[kk] = *(const bf16x8*)(ar + MK * kk + 8 * gr);
+      bf[kk] = *(const bf16x8*)(br + MK * kk + 8 * gr);
     }
     if constexpr (!KEYS) {
       const bf16* orow = g.out + row_off(hx, row, P.lo);
       float d = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 o = *(const bf16x8*)(orow + M::K * kk + 8 * gr);
+        const bf16x8 o = *(const bf16x8*)(orow + MK * kk + 8 * gr);
 #pragma unroll
         for (int j = 0; j < 8; ++j) d = fmaf(bf2f(o[j]), bf2f(bf[kk][j]), d);
       }
-      if (W == 16) d += __shfl_xor(d, 16, 64);
+      d += __shfl_xor(d, 16, 64);
       d += __shfl_xor(d, 32, 64);
       const float ls = g.lse[(size_t)hx * P.nq + row];
       if (lw < wreal && ls != -INFINITY) {
@@ -271,32 +255,25 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
       if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
     }
   };
-  // Operand offsets. Rows: this lane's chunk of row l % W of a row tile. Columns: its
-  // pieces in the two transposing reads that make an operand of M::K streamed rows
-  // whose other operand is 8 accumulators: W = 32, accumulators 8 u .. 8 u + 7 of a row
-  // tile (col_operand); W = 16, two row tiles, element j being row 16 (j / 4) + 4 g + j % 4.
-  int xoff[KK], coff[DT][2];
+  // Operand offsets. Rows: this lane's chunk of row l % 16 of a row tile. Columns: its
+  // piece in the two transposing reads (the second 16 rows on) that make an operand of 32
+  // streamed rows whose other operand is the 8 accumulators of two row tiles: element j is
+  // row 16 (j / 4) + 4 g + j % 4.
+  int xoff[KK], coff[DT];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk)
-    xoff[kk] = lw * RB + (((M::K / 8 * kk + gr) ^ row_key<RB>(lw)) << 4);
+    xoff[kk] = lw * RB + (((MK / 8 * kk + gr) ^ row_key<RB>(lw)) << 4);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    if constexpr (W == 32) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) coff[dt][t] = col_operand<RB>(lane, dt, t);
-    } else {
-      const int r = 4 * gr + (lw >> 2), lc = 2 * dt + ((lw & 3) >> 1);
-      coff[dt][0] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (lw & 1);
-      coff[dt][1] = coff[dt][0] + 16 * RB;
-    }
+    const int r = 4 * gr + (lw >> 2), lc = 2 * dt + ((lw & 3) >> 1);
+    coff[dt] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (lw & 1);
   }
 
-  typedef typename M::Acc Acc;
   Acc acc0[DT], acc1[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < M::N; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
+    for (int r = 0; r < MN; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
   float rsum = 0.f;
 
   auto compute = [&](auto buf_tag, int s0) __attribute__((always_inline)) {
@@ -305,7 +282,7 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
     if (c == 0) return;
     const char* xs = smem + BUF * TILE;
     const char* ys = smem + (2 + BUF) * TILE;
-    constexpr int RT = KT / W, NO = KT / M::K;  // row tiles, and operands of 8 accumulators
+    constexpr int RT = KT / W, NO = KT / MK;  // row tiles, and operands of 8 accumulators
     Acc s[RT], e[RT];
     bf16x8 pp[NO], dd[NO], dl[KEYS ? NO : 1];  // P, dS, what dS lost in rounding
 
@@ -324,48 +301,41 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
       }
     };
     auto load_cols = [&](int n) __attribute__((always_inline)) {  // step n: operand n / SC
-      const char *xo = xs + M::K * (n / SC) * RB, *yo = ys + M::K * (n / SC) * RB;
+      const char *xo = xs + MK * (n / SC) * RB, *yo = ys + MK * (n / SC) * RB;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int dt = 2 * (n % SC) + i;
-        xc[n & 1][i] = read_cols(xo + coff[dt][0], xo + coff[dt][1]);
-        if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt][0], yo + coff[dt][1]);
+        xc[n & 1][i] = read_cols(xo + coff[dt], xo + coff[dt] + 16 * RB);
+        if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt], yo + coff[dt] + 16 * RB);
       }
     };
     // keys kept: E starts from the rows' -D
     auto begin = [&](int T) __attribute__((always_inline)) {
       if constexpr (KEYS) {
-#pragma unroll
-        for (int x = 0; x < M::N / 4; ++x) {
-          const f32x4 d = *(const f32x4*)&rows[BUF][1][W * T + 8 * x + 4 * gr];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) e[T][4 * x + r] = d[r];
-        }
+        e[T] = *(const f32x4*)&rows[BUF][1][W * T + 4 * gr];
       }
     };
     auto logits = [&](int n) __attribute__((always_inline)) {
       const int T = n / SR;
-      Acc zero;
-#pragma unroll
-      for (int r = 0; r < M::N; ++r) zero[r] = 0.f;
+      const Acc zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int kk = 2 * (n % SR) + i;
-        s[T] = M::mma(xr[n & 1][i], af[kk], kk == 0 ? zero : s[T]);
-        e[T] = M::mma(yr[n & 1][i], bf[kk], kk == 0 && !KEYS ? zero : e[T]);
+        s[T] = mma(xr[n & 1][i], af[kk], kk == 0 ? zero : s[T]);
+        e[T] = mma(yr[n & 1][i], bf[kk], kk == 0 && !KEYS ? zero : e[T]);
       }
     };
     auto probs = [&](int o) __attribute__((always_inline)) {
       float p[8], ds[8];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {  // four accumulators from r on of row tile T
-        const int T = W == 32 ? o / 2 : 2 * o + x, r0 = W == 32 ? 8 * (o % 2) + 4 * x : 0;
+      for (int x = 0; x < 2; ++x) {  // row tile T
+        const int T = 2 * o + x;
         f32x4 ls = {mylse, mylse, mylse, mylse};
-        if constexpr (KEYS) ls = *(const f32x4*)&rows[BUF][0][W * T + 2 * r0 + 4 * gr];
+        if constexpr (KEYS) ls = *(const f32x4*)&rows[BUF][0][W * T + 4 * gr];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r0 + r], g.sl2, -ls[r]));
-          ds[4 * x + r] = p[4 * x + r] * (KEYS ? e[T][r0 + r] : e[T][r0 + r] + negdel);
+          p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r], g.sl2, -ls[r]));
+          ds[4 * x + r] = p[4 * x + r] * (KEYS ? e[T][r] : e[T][r] + negdel);
         }
       }
       pp[o] = pack8(p);
@@ -384,9 +354,9 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int dt = 2 * (n % SC) + i;
-        acc0[dt] = M::mma(xc[n & 1][i], dd[o], acc0[dt]);
-        if constexpr (KEYS) acc0[dt] = M::mma(xc[n & 1][i], dl[o], acc0[dt]);
-        acc1[dt] = M::mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
+        acc0[dt] = mma(xc[n & 1][i], dd[o], acc0[dt]);
+        if constexpr (KEYS) acc0[dt] = mma(xc[n & 1][i], dl[o], acc0[dt]);
+        acc1[dt] = mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
       }
     };
     // row tiles T0 .. T0 + RT / 2 - 1
@@ -400,8 +370,8 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
 #pragma unroll
         for (int T = T0; T < T0 + RT / 2; ++T)
 #pragma unroll
-          for (int r = 0; r < M::N; ++r)
-            if ((uint32_t)(p0 + W * T + 8 * (r >> 2) + (r & 3)) >= len) {
+          for (int r = 0; r < MN; ++r)
+            if ((uint32_t)(p0 + W * T + r) >= len) {
               s[T][r] = -INFINITY;
               e[T][r] = 0.f;
             }
@@ -412,8 +382,8 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
 #pragma unroll
         for (int T = T0; T < T0 + RT / 2; ++T)
 #pragma unroll
-          for (int r = 0; r < M::N; ++r) {
-            const int x = W * T + 8 * (r >> 2) + (r & 3);
+          for (int r = 0; r < MN; ++r) {
+            const int x = W * T + r;
             if (!((uint32_t)(a0 + x) < len || x < b0)) {
               s[T][r] = -INFINITY;
               e[T][r] = 0.f;
@@ -485,26 +455,18 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
 
   const int rout = w0 + lw;
   if (!KEYS) {
-    if (W == 16) rsum += __shfl_xor(rsum, 16, 64);
+    rsum += __shfl_xor(rsum, 16, 64);
     rsum += __shfl_xor(rsum, 32, 64);
   }
-  auto dims = [&](int dt, int x) { return W * dt + 8 * x + 4 * gr; };
+  auto dims = [&](int dt) { return W * dt + 4 * gr; };
   if (parts > 1) {
     const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + W * w + lw;
     float* p = g.part + slot * 2 * D;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int x = 0; x < M::N / 4; ++x) {
-        f32x4 a, b4;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          a[r] = acc0[dt][4 * x + r];
-          b4[r] = acc1[dt][4 * x + r];
-        }
-        *(f32x4*)(p + dims(dt, x)) = a;
-        *(f32x4*)(p + D + dims(dt, x)) = b4;
-      }
+    for (int dt = 0; dt < DT; ++dt) {
+      *(f32x4*)(p + dims(dt)) = acc0[dt];
+      *(f32x4*)(p + D + dims(dt)) = acc1[dt];
+    }
     if (!KEYS && gr == 0) {
       g.rpart[slot] = rsum;
       if (part == 0) {
@@ -522,28 +484,24 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
   const bool on = lw < wreal;
   bf16* o0 = g.g0 + row_off(hx, rout, g.lg0);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt) {
+    bf16x4 y;
 #pragma unroll
-    for (int x = 0; x < M::N / 4; ++x) {
-      bf16x4 y;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float a = acc0[dt][4 * x + r], d = KEYS ? a : a - rsum * acc1[dt][4 * x + r];
-        y[r] = f2bf(on ? d * P.scale : 0.f);
-      }
-      *(bf16x4*)(o0 + dims(dt, x)) = y;
+    for (int r = 0; r < 4; ++r) {
+      const float a = acc0[dt][r], d = KEYS ? a : a - rsum * acc1[dt][r];
+      y[r] = f2bf(on ? d * P.scale : 0.f);
     }
+    *(bf16x4*)(o0 + dims(dt)) = y;
+  }
   if constexpr (KEYS) {
     bf16* o1 = g.g1 + row_off(hx, rout, g.lg1);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt) {
+      bf16x4 y;
 #pragma unroll
-      for (int x = 0; x < M::N / 4; ++x) {
-        bf16x4 y;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][4 * x + r] : 0.f);
-        *(bf16x4*)(o1 + dims(dt, x)) = y;
-      }
+      for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][r] : 0.f);
+      *(bf16x4*)(o1 + dims(dt)) = y;
+    }
   }
 }
 
@@ -551,7 +509,7 @@ __global__ __launch_bounds__(64 * grad_block(D) / grad_rows<D>(), 2) void window
 template <int D, bool KEYS>
 __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, const GradArgs g,
                                                                int ncut, int first_cut) {
-  constexpr int E = D / 32, kRows = grad_block(D);  // elements of a lane, rows of a block
+  constexpr int E = D / 32;  // elements of a lane
   const int HX = KEYS ? P.Hk : P.H, nmax = KEYS ? P.nk : P.nq;
   const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -634,7 +592,7 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool unev
   return best;
 }
 Parts query_parts(const WinProb& P) {
-  const int kRows = grad_block(P.d), nb = (P.nq + kRows - 1) / kRows;
+  const int nb = (P.nq + kRows - 1) / kRows;
   int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
   const int64_t tiles = (keys + KT - 1) / KT;
@@ -642,7 +600,7 @@ Parts query_parts(const WinProb& P) {
 }
 // keys kept: the blocks that hold sinks are seen by all queries
 Parts key_parts(const WinProb& P) {
-  const int kRows = grad_block(P.d), nb = (P.nk + kRows - 1) / kRows;
+  const int nb = (P.nk + kRows - 1) / kRows;
   const int64_t all = (int64_t)(P.nq + KT - 1) / KT * P.G;
   int64_t seen = (((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1) * P.G;
   if (seen > all) seen = all;
@@ -657,7 +615,6 @@ struct GradPlan {
   size_t lse2, delta, part, rpart, total;
 };
 GradPlan plan(const WinProb& P) {
-  const int kRows = grad_block(P.d);
   const size_t nqp = (size_t)(P.nq + kPad - 1) / kPad * kPad, rows = (size_t)P.B * P.H * nqp;
   // the two kernels' partial sums follow one another in the same place
   const size_t pq = (size_t)P.B * P.H * query_parts(P).places() * kRows;
@@ -675,13 +632,13 @@ template <int D, bool KEYS>
 hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
   const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
   hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
-                     dim3(64 * grad_block(D) / grad_rows<D>()), 0, st, P, g);
+                     dim3(64 * NW), 0, st, P, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts.places() == 0) return e;
   const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
   const int ncut = (g.parts.p > 1 ? g.parts.nb : g.parts.nsink) - first;
   hipLaunchKernelGGL((window_grad_join_kernel<D, KEYS>),
-                     dim3((unsigned)(((int64_t)heads * ncut * grad_block(D) + 7) / 8)), dim3(256), 0, st, P, g,
+                     dim3((unsigned)(((int64_t)heads * ncut * kRows + 7) / 8)), dim3(256), 0, st, P, g,
                      ncut, first);
   return hipGetLastError();
 }
