@@ -554,12 +554,15 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
 // without a window). Of the cuts below the one with the least time by this estimate, in
 // tiles: a workgroup costs three tiles beside its own; equal workgroups run in rounds of
 // as many as the chip holds, others fill it and leave half the longest over; partial sums
-// (a block of 2 d floats a row, written and read) cost 0.015 each and a launch 3. 8,192 tokens on 2 key
-// heads take one round of 24 tiles (three parts, 159 us with the forward pass) instead of
-// two of 18 (166).
+// (64 rows of 2 d floats, written and read) cost 0.0075 each and a launch 3. Twice that
+// for the sums took 502 us instead of 387 for 3 heads of 7,553 tokens (d = 128, 357 blocks
+// on 512 places), 170 instead of 167 for 8,192 tokens on 2 key heads, but 252 instead of 270
+// for 10 heads of 3,186 and 306 instead of 316 for 2 x 8 of 4,230.
 Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool uneven) {
   static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-  const int64_t slots = 512;  // two workgroups a compute unit
+  // two workgroups a compute unit; at d = 64 three fit, but 768 here took 196 us instead of
+  // 185, 321 instead of 316 and 288 instead of 302 on three shapes, others the same
+  const int64_t slots = 512;
   if (nsink > nb) nsink = nb;
   Parts best{nb, nsink, 1, 1};
   double least = -1;
@@ -582,7 +585,7 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool unev
         cost = (double)((wgs + slots - 1) / slots) * longest;
       else
         cost = work / slots + 0.5 * longest;
-      if (x.places()) cost += 0.015 * (double)(heads * x.places()) + 3;
+      if (x.places()) cost += 0.0075 * (double)(heads * x.places()) + 3;
       if (least < 0 || cost < least) {
         least = cost;
         best = x;
