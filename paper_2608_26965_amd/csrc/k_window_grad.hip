@@ -1,8 +1,8 @@
 // Gradients of attention with a sliding window and sinks, bf16, on the matrix
 // cores.
 //
-// Two kernels of one form. Each keeps a block of 64 rows of two tensors
-// in registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
+// Two kernels of one form. Each keeps a block of 64 or 128 rows (key_rows) of two
+// tensors in registers, streams 64-row tiles of two others through LDS (row_tile.h) and forms
 // per tile, with P = e^{s - lse},
 //     S = X A^T,  E = Y B^T - D,  dS = P E,
 // whose accumulators (a lane holds one kept row and several streamed ones) are the
@@ -39,24 +39,43 @@ constexpr int kVmcnt0 = 0x0F70;  // s_waitcnt immediate: vmcnt = 0 only
 constexpr int kPad = 128;        // lse2 and delta are padded to this
 constexpr int KT = 64;           // streamed rows of a tile
 
-// Kept rows of a wavefront: sixteen, so that its operands and sums leave two waves a SIMD
-// at d = 128 and three at d = 64 (32 rows at d = 128, one wave with half the registers
-// accumulation registers that operands are copied through: 793 us for the padded batch
-// of three where 16 took 726; 32 rows at d = 64: 335 us where 16 take 307 (2 x 8 heads, 4,230
-// tokens), 175 and 150 (8,733 tokens, a short window), 184 and 190 (14,567, 3 heads)).
-constexpr int W = 16;
-// ... and of a workgroup: several share a compute unit and are not at the same point of a
-// tile at the same time (d = 128: workgroups of 128 rows take 713 to 720 us where those of 64
-// take 703 to 710, 468 and 430, 342 and 322, but 436 and 504 where 64 make 357 blocks;
-// d = 64: 336 and 307, 189 and 155)
-constexpr int kRows = 64, NW = kRows / W;
-// A product of 16 kept rows, 16 x 16 x 32: accumulator r of a lane is row 4 g + r
-// (g = lane / 16) of kept row lane % 16
-typedef f32x4 Acc;
-constexpr int MK = 32, MN = 4;
-__device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+constexpr int NW = 4;            // wavefronts of a workgroup, W kept rows each
+
+// Kept rows of a wavefront: 16, or 32 where keys are kept at d = 64 and the window is long.
+// 16 rows leave three waves a SIMD at d = 64 and two at d = 128 (32 there, one wave with
+// half the registers accumulation registers that operands are copied through: 793 us
+// for the padded batch of three where 16 took 726), and four wavefronts of them make
+// blocks of 64, of which several share a compute unit, not at the same point of a tile at the
+// same time (d = 128, workgroups of 128 rows: 468 us where 64 take 430, 342 and 322, 713 to
+// 720 and 703 to 710). dq takes 52 us with 32 rows and 49 with 16 (8,192 tokens, d = 64),
+// 116 and 102, 68 and 57, 25 and 20. dk and dv: blocks of 128 keys waste more of a short
+// window's tiles (2 x 8 heads of 6,013 tokens, 48 keys: 25 us and 21; 8,733 tokens, 295
+// keys: 76 and 64), blocks of 64 read every streamed row twice as often (1,024 keys: 70
+// and 74; 2,437: 68 and 93; no limit, 3,984 tokens: 121 and 145).
+int key_rows(const WinProb& P) {
+  return P.d == 64 && (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) >= 512 ? 32 : 16;
 }
+constexpr int kQueryRows = 16;
+// A product of W kept rows: W x W x K, accumulator r of a lane being row 8 (r / 4) + 4 g
+// + r % 4 (g = lane / W) of kept row lane % W
+template <int W>
+struct Mma;
+template <>
+struct Mma<32> {
+  typedef f32x16 Acc;
+  static constexpr int K = 16, N = 16;
+  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<16> {
+  typedef f32x4 Acc;
+  static constexpr int K = 32, N = 4;
+  static __device__ __forceinline__ Acc mma(bf16x8 a, bf16x8 b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
 
 // Row blocks and the parts that their streamed tiles are cut into. Blocks 0 ..
 // nsink - 1 are cut into `psink` parts (keys kept: the blocks that hold sinks,
@@ -117,10 +136,11 @@ struct GradArgs {
   float sl2;
 };
 
-template <int D, bool KEYS>
-__global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
-    const WinProb P, const GradArgs g) {
-  constexpr int KK = D / MK, DT = D / W, RB = 2 * D, TILE = KT * RB;
+template <int D, bool KEYS, int W>
+__global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(const WinProb P, const GradArgs g) {
+  constexpr int kRows = NW * W;
+  typedef Mma<W> M;
+  constexpr int KK = D / M::K, DT = D / W, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // X, X, Y, Y
   __shared__ __attribute__((aligned(16))) float rows[KEYS ? 2 : 1][2][KEYS ? KT : 4];
   const int nitem = g.parts.items();
@@ -192,19 +212,19 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
     const bf16* br = g.b + row_off(hx, row, g.lb);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      af[kk] = *(const bf16x8*)(ar + MK * kk + 8 * gr);
-      bf[kk] = *(const bf16x8*)(br + MK * kk + 8 * gr);
+      af[kk] = *(const bf16x8*)(ar + M::K * kk + 8 * gr);
+      bf[kk] = *(const bf16x8*)(br + M::K * kk + 8 * gr);
     }
     if constexpr (!KEYS) {
       const bf16* orow = g.out + row_off(hx, row, P.lo);
       float d = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 o = *(const bf16x8*)(orow + MK * kk + 8 * gr);
+        const bf16x8 o = *(const bf16x8*)(orow + M::K * kk + 8 * gr);
 #pragma unroll
         for (int j = 0; j < 8; ++j) d = fmaf(bf2f(o[j]), bf2f(bf[kk][j]), d);
       }
-      d += __shfl_xor(d, 16, 64);
+      if (W == 16) d += __shfl_xor(d, 16, 64);
       d += __shfl_xor(d, 32, 64);
       const float ls = g.lse[(size_t)hx * P.nq + row];
       if (lw < wreal && ls != -INFINITY) {
@@ -255,25 +275,32 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
       if (w < 2 && lane < 16) lds_dma16(w ? g.delta + at : g.lse2 + at, 16 * lane, dst);
     }
   };
-  // Operand offsets. Rows: this lane's chunk of row l % 16 of a row tile. Columns: its
-  // piece in the two transposing reads (the second 16 rows on) that make an operand of 32
-  // streamed rows whose other operand is the 8 accumulators of two row tiles: element j is
-  // row 16 (j / 4) + 4 g + j % 4.
-  int xoff[KK], coff[DT];
+  // Operand offsets. Rows: this lane's chunk of row l % W of a row tile. Columns: its
+  // pieces in the two transposing reads that make an operand of M::K streamed rows
+  // whose other operand is 8 accumulators: W = 32, accumulators 8 u .. 8 u + 7 of a row
+  // tile (col_operand); W = 16, two row tiles, element j being row 16 (j / 4) + 4 g + j % 4.
+  int xoff[KK], coff[DT][2];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk)
-    xoff[kk] = lw * RB + (((MK / 8 * kk + gr) ^ row_key<RB>(lw)) << 4);
+    xoff[kk] = lw * RB + (((M::K / 8 * kk + gr) ^ row_key<RB>(lw)) << 4);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
-    const int r = 4 * gr + (lw >> 2), lc = 2 * dt + ((lw & 3) >> 1);
-    coff[dt] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (lw & 1);
+    if constexpr (W == 32) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) coff[dt][t] = col_operand<RB>(lane, dt, t);
+    } else {
+      const int r = 4 * gr + (lw >> 2), lc = 2 * dt + ((lw & 3) >> 1);
+      coff[dt][0] = r * RB + ((lc ^ row_key<RB>(r)) << 4) + 8 * (lw & 1);
+      coff[dt][1] = coff[dt][0] + 16 * RB;
+    }
   }
 
+  typedef typename M::Acc Acc;
   Acc acc0[DT], acc1[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < MN; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
+    for (int r = 0; r < M::N; ++r) acc0[dt][r] = acc1[dt][r] = 0.f;
   float rsum = 0.f;
 
   auto compute = [&](auto buf_tag, int s0) __attribute__((always_inline)) {
@@ -282,7 +309,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
     if (c == 0) return;
     const char* xs = smem + BUF * TILE;
     const char* ys = smem + (2 + BUF) * TILE;
-    constexpr int RT = KT / W, NO = KT / MK;  // row tiles, and operands of 8 accumulators
+    constexpr int RT = KT / W, NO = KT / M::K;  // row tiles, and operands of 8 accumulators
     Acc s[RT], e[RT];
     bf16x8 pp[NO], dd[NO], dl[KEYS ? NO : 1];  // P, dS, what dS lost in rounding
 
@@ -301,41 +328,48 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
       }
     };
     auto load_cols = [&](int n) __attribute__((always_inline)) {  // step n: operand n / SC
-      const char *xo = xs + MK * (n / SC) * RB, *yo = ys + MK * (n / SC) * RB;
+      const char *xo = xs + M::K * (n / SC) * RB, *yo = ys + M::K * (n / SC) * RB;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int dt = 2 * (n % SC) + i;
-        xc[n & 1][i] = read_cols(xo + coff[dt], xo + coff[dt] + 16 * RB);
-        if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt], yo + coff[dt] + 16 * RB);
+        xc[n & 1][i] = read_cols(xo + coff[dt][0], xo + coff[dt][1]);
+        if constexpr (KEYS) yc[n & 1][i] = read_cols(yo + coff[dt][0], yo + coff[dt][1]);
       }
     };
     // keys kept: E starts from the rows' -D
     auto begin = [&](int T) __attribute__((always_inline)) {
       if constexpr (KEYS) {
-        e[T] = *(const f32x4*)&rows[BUF][1][W * T + 4 * gr];
+#pragma unroll
+        for (int x = 0; x < M::N / 4; ++x) {
+          const f32x4 d = *(const f32x4*)&rows[BUF][1][W * T + 8 * x + 4 * gr];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) e[T][4 * x + r] = d[r];
+        }
       }
     };
     auto logits = [&](int n) __attribute__((always_inline)) {
       const int T = n / SR;
-      const Acc zero = {0.f, 0.f, 0.f, 0.f};
+      Acc zero;
+#pragma unroll
+      for (int r = 0; r < M::N; ++r) zero[r] = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int kk = 2 * (n % SR) + i;
-        s[T] = mma(xr[n & 1][i], af[kk], kk == 0 ? zero : s[T]);
-        e[T] = mma(yr[n & 1][i], bf[kk], kk == 0 && !KEYS ? zero : e[T]);
+        s[T] = M::mma(xr[n & 1][i], af[kk], kk == 0 ? zero : s[T]);
+        e[T] = M::mma(yr[n & 1][i], bf[kk], kk == 0 && !KEYS ? zero : e[T]);
       }
     };
     auto probs = [&](int o) __attribute__((always_inline)) {
       float p[8], ds[8];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {  // row tile T
-        const int T = 2 * o + x;
+      for (int x = 0; x < 2; ++x) {  // four accumulators from r on of row tile T
+        const int T = W == 32 ? o / 2 : 2 * o + x, r0 = W == 32 ? 8 * (o % 2) + 4 * x : 0;
         f32x4 ls = {mylse, mylse, mylse, mylse};
-        if constexpr (KEYS) ls = *(const f32x4*)&rows[BUF][0][W * T + 4 * gr];
+        if constexpr (KEYS) ls = *(const f32x4*)&rows[BUF][0][W * T + 2 * r0 + 4 * gr];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r], g.sl2, -ls[r]));
-          ds[4 * x + r] = p[4 * x + r] * (KEYS ? e[T][r] : e[T][r] + negdel);
+          p[4 * x + r] = __builtin_amdgcn_exp2f(fmaf(s[T][r0 + r], g.sl2, -ls[r]));
+          ds[4 * x + r] = p[4 * x + r] * (KEYS ? e[T][r0 + r] : e[T][r0 + r] + negdel);
         }
       }
       pp[o] = pack8(p);
@@ -354,9 +388,9 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int dt = 2 * (n % SC) + i;
-        acc0[dt] = mma(xc[n & 1][i], dd[o], acc0[dt]);
-        if constexpr (KEYS) acc0[dt] = mma(xc[n & 1][i], dl[o], acc0[dt]);
-        acc1[dt] = mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
+        acc0[dt] = M::mma(xc[n & 1][i], dd[o], acc0[dt]);
+        if constexpr (KEYS) acc0[dt] = M::mma(xc[n & 1][i], dl[o], acc0[dt]);
+        acc1[dt] = M::mma(KEYS ? yc[n & 1][i] : xc[n & 1][i], pp[o], acc1[dt]);
       }
     };
     // row tiles T0 .. T0 + RT / 2 - 1
@@ -370,8 +404,8 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
 #pragma unroll
         for (int T = T0; T < T0 + RT / 2; ++T)
 #pragma unroll
-          for (int r = 0; r < MN; ++r)
-            if ((uint32_t)(p0 + W * T + r) >= len) {
+          for (int r = 0; r < M::N; ++r)
+            if ((uint32_t)(p0 + W * T + 8 * (r >> 2) + (r & 3)) >= len) {
               s[T][r] = -INFINITY;
               e[T][r] = 0.f;
             }
@@ -382,8 +416,8 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
 #pragma unroll
         for (int T = T0; T < T0 + RT / 2; ++T)
 #pragma unroll
-          for (int r = 0; r < MN; ++r) {
-            const int x = W * T + r;
+          for (int r = 0; r < M::N; ++r) {
+            const int x = W * T + 8 * (r >> 2) + (r & 3);
             if (!((uint32_t)(a0 + x) < len || x < b0)) {
               s[T][r] = -INFINITY;
               e[T][r] = 0.f;
@@ -455,18 +489,26 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
 
   const int rout = w0 + lw;
   if (!KEYS) {
-    rsum += __shfl_xor(rsum, 16, 64);
+    if (W == 16) rsum += __shfl_xor(rsum, 16, 64);
     rsum += __shfl_xor(rsum, 32, 64);
   }
-  auto dims = [&](int dt) { return W * dt + 4 * gr; };
+  auto dims = [&](int dt, int x) { return W * dt + 8 * x + 4 * gr; };
   if (parts > 1) {
     const size_t slot = ((size_t)hx * g.parts.places() + place) * kRows + W * w + lw;
     float* p = g.part + slot * 2 * D;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      *(f32x4*)(p + dims(dt)) = acc0[dt];
-      *(f32x4*)(p + D + dims(dt)) = acc1[dt];
-    }
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int x = 0; x < M::N / 4; ++x) {
+        f32x4 a, b4;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          a[r] = acc0[dt][4 * x + r];
+          b4[r] = acc1[dt][4 * x + r];
+        }
+        *(f32x4*)(p + dims(dt, x)) = a;
+        *(f32x4*)(p + D + dims(dt, x)) = b4;
+      }
     if (!KEYS && gr == 0) {
       g.rpart[slot] = rsum;
       if (part == 0) {
@@ -484,32 +526,36 @@ __global__ __launch_bounds__(64 * NW, 2) void window_grad_kernel(
   const bool on = lw < wreal;
   bf16* o0 = g.g0 + row_off(hx, rout, g.lg0);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    bf16x4 y;
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float a = acc0[dt][r], d = KEYS ? a : a - rsum * acc1[dt][r];
-      y[r] = f2bf(on ? d * P.scale : 0.f);
+    for (int x = 0; x < M::N / 4; ++x) {
+      bf16x4 y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float a = acc0[dt][4 * x + r], d = KEYS ? a : a - rsum * acc1[dt][4 * x + r];
+        y[r] = f2bf(on ? d * P.scale : 0.f);
+      }
+      *(bf16x4*)(o0 + dims(dt, x)) = y;
     }
-    *(bf16x4*)(o0 + dims(dt)) = y;
-  }
   if constexpr (KEYS) {
     bf16* o1 = g.g1 + row_off(hx, rout, g.lg1);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      bf16x4 y;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][r] : 0.f);
-      *(bf16x4*)(o1 + dims(dt)) = y;
-    }
+      for (int x = 0; x < M::N / 4; ++x) {
+        bf16x4 y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = f2bf(on ? acc1[dt][4 * x + r] : 0.f);
+        *(bf16x4*)(o1 + dims(dt, x)) = y;
+      }
   }
 }
 
 // Adds up the parts of the blocks that were cut, in order: 32 lanes a row.
-template <int D, bool KEYS>
+template <int D, bool KEYS, int W>
 __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, const GradArgs g,
                                                                int ncut, int first_cut) {
-  constexpr int E = D / 32;  // elements of a lane
+  constexpr int E = D / 32, kRows = NW * W;  // elements of a lane, rows of a block
   const int HX = KEYS ? P.Hk : P.H, nmax = KEYS ? P.nk : P.nq;
   const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
@@ -554,11 +600,12 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
 // without a window). Of the cuts below the one with the least time by this estimate, in
 // tiles: a workgroup costs three tiles beside its own; equal workgroups run in rounds of
 // as many as the chip holds, others fill it and leave half the longest over; partial sums
-// (64 rows of 2 d floats, written and read) cost 0.0075 each and a launch 3. Twice that
-// for the sums took 502 us instead of 387 for 3 heads of 7,553 tokens (d = 128, 357 blocks
-// on 512 places), 170 instead of 167 for 8,192 tokens on 2 key heads, but 252 instead of 270
-// for 10 heads of 3,186 and 306 instead of 316 for 2 x 8 of 4,230.
-Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool uneven) {
+// (2 d floats a row, written and read) cost 0.015 for 128 rows and a launch 3. Twice
+// that for the sums took 502 us instead of 387 for 3 heads of 7,553 tokens (d = 128, 357
+// blocks on 512 places), but 252 instead of 270 for 10 heads of 3,186. 8,192 tokens on 2
+// key heads take one round of 24 tiles (three parts, 159 us with the forward pass) instead
+// of two of 18 (166).
+Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int rows, bool uneven) {
   static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   // two workgroups a compute unit; at d = 64 three fit, but 768 here took 196 us instead of
   // 185, 321 instead of 316 and 288 instead of 302 on three shapes, others the same
@@ -585,7 +632,7 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool unev
         cost = (double)((wgs + slots - 1) / slots) * longest;
       else
         cost = work / slots + 0.5 * longest;
-      if (x.places()) cost += 0.0075 * (double)(heads * x.places()) + 3;
+      if (x.places()) cost += 0.015 / 128 * (double)(heads * x.places() * rows) + 3;
       if (least < 0 || cost < least) {
         least = cost;
         best = x;
@@ -595,20 +642,20 @@ Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, bool unev
   return best;
 }
 Parts query_parts(const WinProb& P) {
-  const int nb = (P.nq + kRows - 1) / kRows;
+  const int kRows = NW * kQueryRows, nb = (P.nq + kRows - 1) / kRows;
   int64_t keys = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows + P.m.sinks;
   if (keys > P.nk) keys = P.nk;
   const int64_t tiles = (keys + KT - 1) / KT;
-  return cut(nb, 0, tiles, tiles, (int64_t)P.B * P.H, P.m.causal && P.m.left >= P.nk);
+  return cut(nb, 0, tiles, tiles, (int64_t)P.B * P.H, kRows, P.m.causal && P.m.left >= P.nk);
 }
 // keys kept: the blocks that hold sinks are seen by all queries
 Parts key_parts(const WinProb& P) {
-  const int nb = (P.nk + kRows - 1) / kRows;
+  const int kRows = NW * key_rows(P), nb = (P.nk + kRows - 1) / kRows;
   const int64_t all = (int64_t)(P.nq + KT - 1) / KT * P.G;
   int64_t seen = (((int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + kRows) / KT + 1) * P.G;
   if (seen > all) seen = all;
   const int nsink = P.m.sinks < P.nk ? (P.m.sinks + kRows - 1) / kRows : nb;
-  return cut(nb, seen < all ? nsink : 0, all, seen, (int64_t)P.B * P.Hk,
+  return cut(nb, seen < all ? nsink : 0, all, seen, (int64_t)P.B * P.Hk, kRows,
              P.m.causal && P.m.left >= P.nk);
 }
 
@@ -620,8 +667,8 @@ struct GradPlan {
 GradPlan plan(const WinProb& P) {
   const size_t nqp = (size_t)(P.nq + kPad - 1) / kPad * kPad, rows = (size_t)P.B * P.H * nqp;
   // the two kernels' partial sums follow one another in the same place
-  const size_t pq = (size_t)P.B * P.H * query_parts(P).places() * kRows;
-  const size_t pk = (size_t)P.B * P.Hk * key_parts(P).places() * kRows;
+  const size_t pq = (size_t)P.B * P.H * query_parts(P).places() * NW * kQueryRows;
+  const size_t pk = (size_t)P.B * P.Hk * key_parts(P).places() * NW * key_rows(P);
   GradPlan g;
   g.lse2 = 0;
   g.delta = align256(rows * 4);
@@ -631,17 +678,17 @@ GradPlan plan(const WinProb& P) {
   return g;
 }
 
-template <int D, bool KEYS>
+template <int D, bool KEYS, int W>
 hipError_t run_grad(const WinProb& P, const GradArgs& g, hipStream_t st) {
   const int heads = P.B * (KEYS ? P.Hk : P.H), n = g.parts.items();
-  hipLaunchKernelGGL((window_grad_kernel<D, KEYS>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
+  hipLaunchKernelGGL((window_grad_kernel<D, KEYS, W>), dim3((unsigned)((int64_t)8 * ((n + 7) / 8) * heads)),
                      dim3(64 * NW), 0, st, P, g);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.parts.places() == 0) return e;
   const int first = g.parts.psink > 1 ? 0 : g.parts.nsink;
   const int ncut = (g.parts.p > 1 ? g.parts.nb : g.parts.nsink) - first;
-  hipLaunchKernelGGL((window_grad_join_kernel<D, KEYS>),
-                     dim3((unsigned)(((int64_t)heads * ncut * kRows + 7) / 8)), dim3(256), 0, st, P, g,
+  hipLaunchKernelGGL((window_grad_join_kernel<D, KEYS, W>),
+                     dim3((unsigned)(((int64_t)heads * ncut * NW * W + 7) / 8)), dim3(256), 0, st, P, g,
                      ncut, first);
   return hipGetLastError();
 }
@@ -654,13 +701,15 @@ hipError_t run_both(const WinProb& P, GradArgs& g, const bf16* q, const bf16* k,
   g.a = q, g.la = P.lq, g.b = dout, g.lb = P.ldo;
   g.g0 = dq, g.lg0 = P.ldq, g.g1 = nullptr, g.lg1 = P.ldq;
   g.parts = query_parts(P);
-  const hipError_t e = run_grad<D, false>(P, g, st);
+  const hipError_t e = run_grad<D, false, kQueryRows>(P, g, st);
   if (e != hipSuccess) return e;
   g.x = q, g.lx = P.lq, g.y = dout, g.ly = P.ldo;
   g.a = k, g.la = P.lk, g.b = v, g.lb = P.lv;
   g.g0 = dk, g.lg0 = P.ldk, g.g1 = dv, g.lg1 = P.ldv;
   g.parts = key_parts(P);
-  return run_grad<D, true>(P, g, st);
+  if constexpr (D == 64)
+    if (key_rows(P) == 32) return run_grad<D, true, 32>(P, g, st);
+  return run_grad<D, true, 16>(P, g, st);
 }
 
 }  // namespace
