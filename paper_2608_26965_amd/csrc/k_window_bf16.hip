@@ -14,10 +14,13 @@
 // product; the result is rounded once.
 //
 // A tile that every row of the wavefront sees runs without a maximum, against
-// the reference that the rows have (probabilities above 1 cost no accuracy while
-// nothing overflows; that is checked once at the end, and the workgroup starts
-// over with a maximum in every tile where it fails). Tiles at the edges of
-// the window, and the first ones, take the maximum and rescale.
+// the reference that the rows have: probabilities above 1 cost no accuracy while
+// nothing overflows. Tiles at the edges of the window, and the first ones, take the
+// maximum and rescale, which loses what is scaled by less than 2^-126 (the
+// exponential of that is 0): no weight to speak of next to a sum of at most the number
+// of keys, but perhaps most of a sum that grew far above its reference. Where a
+// large sum meets such a factor, or one overflows (checked once at the end), the
+// workgroup starts over with a maximum in every tile.
 #include <math.h>
 
 #include "row_tile.h"
@@ -212,7 +215,8 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
     mx = fmaxf(mx, wave_xor32(mx));
     const float m_new = fmaxf(m, mx * sl2);
     alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-    l *= alpha;
+    // (2^22 keys at most: against maxima no sum is larger)
+    l = m_new - m > 126.f && l > 0x1p22f ? INFINITY : l * alpha;
     const bool raised = __builtin_amdgcn_ballot_w64(m_new > m) != 0;
     m = m_new;
     set = __builtin_amdgcn_ballot_w64(m == -INFINITY) == 0;

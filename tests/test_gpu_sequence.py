@@ -796,3 +796,61 @@ def test_paged_wide_tables_and_many_lengths(dt):
     _paged_check(q, out, lse, lens, rows, -1, 0, dt)
     out, lse = ca.paged_attn(q, kp, vp, wide, n, left=500, sinks=50, want_lse=True)
     _paged_check(q, out, lse, lens, rows, 500, 50, dt)
+
+
+# ---- logits far apart ------------------------------------------------------------------------------
+
+def _steep_case(dt, d, bits, v, nq, grads=True, **kw):
+    """Every query's logit of key j is bits[j] (numbers that bf16 holds) in log2 units, exactly
+    before the scale: queries are 2 in one dim and 0 in the others."""
+    import torch
+    ca = _ca()
+    g = _gen(41)
+    n = len(bits)
+    scale = math.log(2.0)
+    q, k = torch.zeros(1, 1, nq, d, dtype=_torch(dt)), _rand(g, (1, 1, n, d), dt)
+    q[..., 0] = 2.0
+    k[0, 0, :, 0] = torch.from_numpy(np.asarray(bits) / 2.0).to(_torch(dt))
+    v, do = v.to(_torch(dt))[None, None], _rand(g, (1, 1, nq, d), dt)
+    w = ca.Window(**kw)
+    dev = [x.cuda() for x in (q, k, v)]
+    out, lse = ca.window_attn(w, *dev, scale=scale, want_lse=True)
+    got = {"out": out, "lse": lse}
+    if grads:
+        got["dq"], got["dk"], got["dv"] = ca.window_attn_backward(w, do.cuda(), *dev, out, lse, scale=scale)
+    see = seq.visible(nq, n, kw.get("left", -1), kw.get("right", -1), kw.get("sinks", 0), kw.get("causal", False))
+    want = _bounds(*(_np(x)[0, 0] for x in (q, k, v, do)), see, scale, dt)
+    for name, x in got.items():
+        _close(_np(x)[0, 0], *want[name], name)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("slope", [0.90, 0.95, 0.97, 1.0])
+@pytest.mark.parametrize("kw", [dict(causal=True), dict(left=190, right=0), dict(left=250, right=30),
+                                dict(left=10, right=0, sinks=200)])
+def test_window_rising_ramps(dt, d, slope, kw):
+    """Tiles that a query sees whole rise to just below the range of fp32 over the first one, and a
+    tile at the edge of what it sees comes after them: none of their share is lost. The values change
+    sign at a tile's edge."""
+    import torch
+    n = 256
+    bits = torch.tensor([slope * j - 100 for j in range(n)]).to(torch.bfloat16).double().numpy()
+    v = torch.randn(n, d, generator=_gen(40))
+    v[:, ::2] = torch.where(torch.arange(n) < 192, 1.0, -1.0)[:, None]
+    _steep_case(dt, d, bits, v, n, **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("last", [0, 200])
+def test_window_last_tile_far_above(dt, d, last):
+    """The rows' last tile is 120 to 250 bits above a first one, with tiles between them whose sum has
+    most or next to nothing of the weight."""
+    import torch
+    n = 320
+    for mid, top in ((117.0, 125.0), (118.0, 128.0), (110.0, 127.0), (118.0, 250.0), (-20.0, 130.0)):
+        bits = np.where(np.arange(n) < 64, 0.0, mid)
+        bits[256:] = -60.0
+        bits[256 + last % 64] = top
+        _steep_case(dt, d, bits, torch.randn(n, d, generator=_gen(42)), 64, left=310, right=0)
