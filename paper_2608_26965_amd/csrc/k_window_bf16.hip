@@ -401,6 +401,15 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void window_bf16_kernel(
       for (int r = 0; r < 16; ++r) oacc[dt][r] = NAN;
   }
   if constexpr (SPLIT) {
+    // A sum far above its reference goes out against a reference at its own size: the
+    // joining compares references, and adds up as many sums as there are parts
+    const int up = l_tot > 0x1p22f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
+    m += (float)up;
+    l_tot = __builtin_amdgcn_ldexpf(l_tot, -up);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[dt][r] = __builtin_amdgcn_ldexpf(oacc[dt][r], -up);
     float* row = part + ((((size_t)bh * order.nb + a) * kRows + 32 * w + l32) * order.splits + sp) *
                             (D + 4);
 #pragma unroll

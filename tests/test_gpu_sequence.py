@@ -854,3 +854,20 @@ def test_window_last_tile_far_above(dt, d, last):
         bits[256:] = -60.0
         bits[256 + last % 64] = top
         _steep_case(dt, d, bits, torch.randn(n, d, generator=_gen(42)), 64, left=310, right=0)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nk,tops", [(1024, (117, 0)), (1024, (0, 117)), (2048, (117, 117, 117, 117)),
+                                     (4096, (117, 60, 117, 0, 116, 117, 90, 117)), (4096, (117,) * 8)])
+@pytest.mark.parametrize("firsts", [0, 127, 240])
+def test_window_parts_far_apart(dt, d, nk, tops, firsts):
+    """Few queries, keys in parts of 512: each part's first tile lies up to 117 bits below the rest of
+    it, and one key of the other parts' first tiles `firsts` bits above (0: at) them."""
+    import torch
+    bits = np.zeros(nk)
+    for i, t in enumerate(tops):
+        bits[512 * i + 64:512 * (i + 1)] = t
+        if i % 2:
+            bits[512 * i + 5] = firsts
+    _steep_case(dt, d, bits, torch.randn(nk, d, generator=_gen(43)), 40)
