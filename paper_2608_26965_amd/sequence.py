@@ -11,12 +11,15 @@ As in the rest of the binding, every step runs in the HIP library: these
 functions read shapes and strides, allocate outputs and workspaces with torch
 and call on the current stream of the tensors' device. They are not recorded by
 autograd: a training program calls window_attn_backward, and rope with
-inverse=True, for the gradients.
+inverse=True, for the gradients (lse has none). Where autograd records, inputs
+that require gradients give a warning, and tensors that require them are
+refused as outputs; outputs that the caller gave count as changed in place.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
+import warnings
 from dataclasses import dataclass
 
 import torch
@@ -53,9 +56,30 @@ def _on(like, *tensors):
     _dtype(like.dtype)
     if not like.is_cuda:
         raise ValueError("expected tensors on the GPU")
+    i = like.get_device()  # (half the time of a torch.device; -1 off the GPU)
     for t in tensors:
-        if t is not None and t.device != like.device:
+        if t is not None and t.get_device() != i:
             raise ValueError(f"expected all tensors on {like.device}, got one on {t.device}")
+
+
+def _unrecorded(read, written):
+    """Where autograd records, tells what the call does not do."""
+    for t in written:
+        if t is not None and t.requires_grad:
+            raise ValueError("the call would write a tensor that requires gradients, unrecorded by "
+                             "autograd: give it detached, or call under torch.no_grad()")
+    for t in read:
+        if t is not None and t.requires_grad:
+            warnings.warn("not recorded by autograd: no gradient reaches the inputs that require one "
+                          "(window_attn_backward and rope with inverse=True form them)", stacklevel=3)
+            return
+
+
+def _wrote(*tensors):
+    """Tensors of the caller's that a call wrote (some may be None): their versions tell
+    autograd, which saw none of it."""
+    # (torch.autograd.graph.increment_version is this and 0.4 us more, of a small call's 9)
+    torch._C._increment_version([t for t in tensors if t is not None])
 
 
 def _dtype(dtype):
@@ -255,24 +279,22 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     `start`. inverse=True turns back (also: the gradients of the turned rows to
     those of the rows). q_out, k_out: outputs, by default new dense tensors of
     the same shape; passing q and k themselves turns them in place. Returns
-    q_out, or (q_out, k_out) with k."""
+    q_out, or (q_out, k_out) with k. Not recorded by autograd."""
     if (grid is None) == (positions is None):
         raise ValueError("give either grid or positions")
+    if torch.is_grad_enabled():
+        _unrecorded((q, k), (q_out, k_out))
     _on(q, k, positions, q_out, k_out)
     c = _rope(r, _geo(q), None if k is None else _geo(k), None if q_out is None else _geo(q_out),
               None if k_out is None else _geo(k_out),
               None if positions is None else _geo(positions), _ints(grid), _ints(start),
               bool(inverse), layout)
-    if q_out is None:
-        q_out = _new(q)
-    if k is None:
-        _call("ca_rope", q.device, c, q.data_ptr(), None, _ptr(positions), q_out.data_ptr(), None)
-        return q_out
-    if k_out is None:
-        k_out = _new(k)
-    _call("ca_rope", q.device, c, q.data_ptr(), k.data_ptr(), _ptr(positions), q_out.data_ptr(),
-          k_out.data_ptr())
-    return q_out, k_out
+    qo = _new(q) if q_out is None else q_out
+    ko = None if k is None else _new(k) if k_out is None else k_out
+    _call("ca_rope", q.device, c, q.data_ptr(), _ptr(k), _ptr(positions), qo.data_ptr(), _ptr(ko))
+    if q_out is not None or k_out is not None:
+        _wrote(q_out, k_out)
+    return qo if k is None else (qo, ko)
 
 
 # ---- window attention ----------------------------------------------------------------
@@ -332,18 +354,22 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
     "strided") or [B,nq,H,d] ("bnhd"), any strides; k, v the same with nk
     tokens and heads_k heads (a divisor of H). len_q, len_k: int32 [B], the
     lengths in a padded batch. Returns (out, lse [B,H,nq] fp32 or None); rows
-    that see no key, and rows past len_q, are 0 with lse -inf."""
+    that see no key, and rows past len_q, are 0 with lse -inf. Not recorded by
+    autograd; window_attn_backward forms the gradients of out (lse has none)."""
+    if torch.is_grad_enabled():
+        _unrecorded((q, k, v), (out,))
     _on(q, k, v, out, len_q, len_k)
     c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), None if out is None else _geo(out), _scale(scale),
                         None if len_q is None else _geo(len_q),
                         None if len_k is None else _geo(len_k), layout, None)
-    if out is None:
-        out = _new(q)
+    o = _new(q) if out is None else out
     lse = q.new_empty(_lse_shape(q, layout), dtype=torch.float32) if want_lse else None
     ws = _workspace(nbytes, q, ws)
     _call("ca_window_attn", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(len_q),
-          _ptr(len_k), out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes)
-    return out, lse
+          _ptr(len_k), o.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.nbytes)
+    if out is not None:
+        _wrote(out)
+    return o, lse
 
 
 def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_q=None,
@@ -352,6 +378,9 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     dout, from out and lse as window_attn gave them for the same arguments.
     dq, dk, dv: outputs of the inputs' shapes (any strides, for example slices
     of a fused projection's gradient), new dense tensors by default."""
+    given = dq, dk, dv
+    if torch.is_grad_enabled():
+        _unrecorded((), given)
     _on(q, k, v, out, lse, dout, len_q, len_k, dq, dk, dv)
     c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), _geo(out), _scale(scale),
                         None if len_q is None else _geo(len_q),
@@ -365,6 +394,7 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     _call("ca_window_attn_backward", q.device, c, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           out.data_ptr(), lse.data_ptr(), dout.data_ptr(), _ptr(len_q), _ptr(len_k),
           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes)
+    _wrote(*given)
     return dq, dk, dv
 
 
@@ -403,7 +433,10 @@ def cache_append(k, v, k_pages, v_pages, page_table, lens):
     """Writes the new keys and values k, v [B,n,Hk,d] of B sequences into their
     pages: the last n of the lens[b] tokens of sequence b (lens counts them
     already). k_pages, v_pages: [pages, page, Hk, d], any strides;
-    page_table: int32 [B, max_pages]; lens: int32 [B]. Returns nothing."""
+    page_table: int32 [B, max_pages]; lens: int32 [B]. Returns nothing. Not
+    recorded by autograd."""
+    if torch.is_grad_enabled():
+        _unrecorded((k, v), (k_pages, v_pages))
     _on(k, v, k_pages, v_pages, page_table, lens)
     if k.dim() != 4:
         raise ValueError("k: expected [B, n, Hk, d]")
@@ -411,6 +444,7 @@ def cache_append(k, v, k_pages, v_pages, page_table, lens):
                   k.shape[2], -1, 0, None, None, None, _geo(k), _geo(v))
     _call("ca_cache_append", k.device, c, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
           v_pages.data_ptr(), page_table.data_ptr(), lens.data_ptr())
+    _wrote(k_pages, v_pages)
 
 
 def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale=None,
@@ -420,18 +454,22 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     and the first `sinks`. q: [B,H,d]; k_pages, v_pages: [pages, page, Hk, d],
     any strides, Hk a divisor of H; page_table: int32 [B, max_pages]; lens:
     int32 [B], the new token included. Returns (out [B,H,d], lse [B,H] fp32 or
-    None); a sequence of no tokens gives 0 and -inf."""
+    None); a sequence of no tokens gives 0 and -inf. Not recorded by autograd,
+    and without a backward pass."""
+    if torch.is_grad_enabled():
+        _unrecorded((q, k_pages, v_pages), (out,))
     _on(q, k_pages, v_pages, page_table, lens, out)
     if q.dim() != 3:
         raise ValueError("q: expected [B, H, d]")
     B, H, _ = q.shape
     c, nbytes = _paged(_geo(k_pages), _geo(v_pages), _geo(page_table), _geo(lens), B, H, int(left),
                        int(sinks), _scale(scale), _geo(q), None if out is None else _geo(out), None, None)
-    if out is None:
-        out = _new(q)
+    o = _new(q) if out is None else out
     lse = q.new_empty((B, H), dtype=torch.float32) if want_lse else None
     ws = _workspace(nbytes, q, ws)
     _call("ca_paged_attn", q.device, c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-          page_table.data_ptr(), lens.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(ws),
+          page_table.data_ptr(), lens.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(ws),
           0 if ws is None else ws.nbytes)
-    return out, lse
+    if out is not None:
+        _wrote(out)
+    return o, lse

@@ -211,3 +211,42 @@ def test_forward_refuses_positions_without_rotary(kw):
     x = torch.zeros(1, 2, 4, 64)
     with pytest.raises(ValueError, match="go with rotary"):
         ca.forward(x, x, x, keep=0.5, **kw)
+
+
+@pytest.mark.parametrize("call", [
+    lambda ca, x: ca.rope(ca.rope_axes((32, 32)), x, grid=(2, 2)),
+    lambda ca, x: ca.window_attn(ca.Window(), x, x, x),
+    lambda ca, x: ca.cache_append(x, x, x.detach(), x.detach(), x.detach(), x.detach()),
+    lambda ca, x: ca.paged_attn(x, x, x, x, x)])
+def test_inputs_that_require_gradients_give_a_warning(call):
+    """And the refusal of tensors off the GPU that the call gets without."""
+    import warnings
+    import torch
+    import paper_2608_26965_amd as ca
+    x = torch.zeros(1, 2, 4, 64, requires_grad=True)
+    with pytest.warns(UserWarning, match="not recorded by autograd"), pytest.raises(ValueError, match="GPU"):
+        call(ca, x)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with pytest.raises(ValueError, match="GPU"):
+            call(ca, x.detach())
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call(ca, x)
+
+
+@pytest.mark.parametrize("call", [
+    lambda ca, x, y: ca.rope(ca.rope_axes((32, 32)), x, grid=(2, 2), q_out=y),
+    lambda ca, x, y: ca.rope(ca.rope_axes((32, 32)), x, x, grid=(2, 2), k_out=y),
+    lambda ca, x, y: ca.window_attn(ca.Window(), x, x, x, out=y),
+    lambda ca, x, y: ca.window_attn_backward(ca.Window(), x, x, x, x, x, x, dk=y),
+    lambda ca, x, y: ca.cache_append(x, x, x, y, x, x),
+    lambda ca, x, y: ca.paged_attn(x, x, x, x, x, out=y)])
+def test_tensors_that_require_gradients_are_not_written(call):
+    import torch
+    import paper_2608_26965_amd as ca
+    x, y = torch.zeros(1, 2, 4, 64), torch.zeros(1, 2, 4, 64, requires_grad=True)
+    for z in (y, y[:]):  # a leaf, and a view of one
+        with pytest.raises(ValueError, match="requires gradients"):
+            call(ca, x, z)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+        call(ca, x, y)

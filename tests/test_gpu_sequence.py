@@ -871,3 +871,53 @@ def test_window_parts_far_apart(dt, d, nk, tops, firsts):
         if i % 2:
             bits[512 * i + 5] = firsts
     _steep_case(dt, d, bits, torch.randn(nk, d, generator=_gen(43)), 40)
+
+
+# ---- autograd ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", DT)
+def test_given_outputs_count_as_changed(dt):
+    """Autograd sees that a tensor it saved was written by a call of these."""
+    import torch
+    ca = _ca()
+    g = _gen(50)
+    x, y, z = (_rand(g, (1, 2, 40, 64), dt).cuda() for _ in range(3))
+    kp, vp = (_rand(g, (3, 16, 2, 64), dt).cuda() for _ in range(2))
+    table = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([40], dtype=torch.int32, device="cuda")
+    r, w = ca.rope_axes((32, 32)), ca.Window(left=9)
+    out, lse = ca.window_attn(w, x, y, z, want_lse=True)
+    new = [torch.zeros_like(x) for _ in range(3)]
+    calls = [(lambda: ca.rope(r, x, y, grid=(5, 8), q_out=x, k_out=y), (x, y)),
+             (lambda: ca.rope(r, x, grid=(5, 8), q_out=z), (z,)),
+             (lambda: ca.window_attn(w, x, y, z, out=out), (out,)),
+             (lambda: ca.window_attn_backward(w, z, x, y, z, out, lse, dq=new[0], dk=new[1], dv=new[2]), new),
+             (lambda: ca.cache_append(y.transpose(1, 2), z.transpose(1, 2), kp, vp, table, lens), (kp, vp)),
+             (lambda: ca.paged_attn(x[:, :, 0], kp, vp, table, lens, out=out[:, :, 1]), (out,))]
+    for call, changed in calls:
+        p = torch.ones_like(changed[0], requires_grad=True)
+        loss = sum((p.view_as(t) * t).sum() for t in changed)
+        call()
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            loss.backward()
+    # what the calls only read stays good for a backward pass
+    p = torch.ones_like(x, requires_grad=True)
+    loss = (p * x).sum() + (p * y).sum()
+    ca.window_attn(w, x, y, z)
+    ca.rope(r, x, y, grid=(5, 8))
+    loss.backward()
+    assert torch.equal(p.grad, x + y)
+
+
+def test_inputs_that_require_gradients_are_detached():
+    """A warning, and the results that the call gives without."""
+    import torch
+    ca = _ca()
+    q, k, v = (_rand(_gen(51), (1, 2, 40, 64), "f32").cuda().requires_grad_() for _ in range(3))
+    with torch.no_grad():
+        want, lse = ca.window_attn(ca.Window(left=5), q, k, v, want_lse=True)
+    with pytest.warns(UserWarning, match="not recorded by autograd"):
+        out, _ = ca.window_attn(ca.Window(left=5), q, k, v)
+    assert torch.equal(out, want) and not out.requires_grad
+    for x in ca.window_attn_backward(ca.Window(left=5), out, q, k, v, out, lse):
+        assert torch.isfinite(x).all()
