@@ -282,6 +282,8 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
     q_out, or (q_out, k_out) with k. Not recorded by autograd."""
     if (grid is None) == (positions is None):
         raise ValueError("give either grid or positions")
+    if k is None and k_out is not None:
+        raise ValueError("k_out goes with k")
     if torch.is_grad_enabled():
         _unrecorded((q, k), (q_out, k_out))
     _on(q, k, positions, q_out, k_out)

@@ -250,3 +250,11 @@ def test_tensors_that_require_gradients_are_not_written(call):
             call(ca, x, z)
     with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
         call(ca, x, y)
+
+
+def test_rope_refuses_an_output_for_keys_that_are_not_given():
+    import torch
+    import paper_2608_26965_amd as ca
+    x = torch.zeros(1, 2, 4, 64)
+    with pytest.raises(ValueError, match="k_out goes with k"):
+        ca.rope(ca.rope_axes((32, 32)), x, grid=(2, 2), k_out=x)
