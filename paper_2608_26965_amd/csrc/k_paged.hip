@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kJoin) void paged_join_kernel(const PagedProb P,
                                                            T* __restrict__ out,
                                                            float* __restrict__ lse) {
   constexpr int NW = kJoin / 64;
-  __shared__ float acc[NW][kMaxD], wmx[NW], wsum[NW];
+  __shared__ float acc[NW][kMaxD], wsum[NW];
   const int bh = blockIdx.x, b = bh / P.H, h = bh - b * P.H;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int n = (seen_keys(P, P.klen(b)).list.n + tiles - 1) / tiles;  // the sequence's parts
