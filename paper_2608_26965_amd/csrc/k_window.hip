@@ -42,10 +42,15 @@ struct Cut {
     *part = (sink ? v : v - s) % *parts;
     *blk = (sink ? 0 : nsink) + (sink ? v : v - s) / *parts;
   }
-  __device__ __forceinline__ int item(int blk) const {  // of its first part
-    return blk < nsink ? blk * psink : nsink * psink + (blk - nsink) * p;
+  // places of partial sums: blocks of one part need none
+  __host__ __device__ int sink_places() const { return psink > 1 ? nsink * psink : 0; }
+  __host__ __device__ int places() const { return sink_places() + (p > 1 ? (nb - nsink) * p : 0); }
+  __device__ __forceinline__ int place(int v) const {  // of a workgroup of a block that is cut
+    return v < nsink * psink ? v : sink_places() + v - nsink * psink;
   }
-  bool cut() const { return p > 1 || (nsink && psink > 1); }
+  __device__ __forceinline__ int first_place(int blk) const {  // of its first part
+    return blk < nsink ? blk * psink : sink_places() + (blk - nsink) * p;
+  }
 };
 
 template <int DP>
@@ -203,7 +208,7 @@ __device__ __forceinline__ void sum_rows(float (*S)[DP][17], const f32x4 (&a)[DP
 }
 
 // dq of 16 queries, and delta = row sums of dout * out. Blocks of one part write dq
-// itself, others their place of the partial sums, [heads][items][16][d].
+// itself, others their place of the partial sums, [heads][places][16][d].
 template <int DP, int NW>
 __global__ __launch_bounds__(64 * NW, kF32Waves) void window_dq_f32_kernel(
     const WinProb P, const float* __restrict__ q, const float* __restrict__ k,
@@ -275,7 +280,7 @@ __global__ __launch_bounds__(64 * NW, kF32Waves) void window_dq_f32_kernel(
   for (int x = 0; x < NJ; ++x)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[x][e] = (lane & 15) < real ? acc[x][e] : 0.f;
-  float* place = partial + ((size_t)bh * cut.items() + blockIdx.x) * 16 * P.d;
+  float* place = partial + ((size_t)bh * cut.places() + cut.place(blockIdx.x)) * 16 * P.d;
   sum_rows<DP, NW>(S, acc, w, lane, rows, P.d, [&](int x) {
     return parts > 1 ? place + x * P.d : dq + row_off(bh, q0 + x, P.ldq);
   });
@@ -361,7 +366,7 @@ __global__ __launch_bounds__(64 * NW, (DP == 128 ? 1 : kF32Waves)) void window_d
       ak[x][e] = (lane & 15) < real ? ak[x][e] : 0.f;
       av[x][e] = (lane & 15) < real ? av[x][e] : 0.f;
     }
-  float* place = partial + ((size_t)bk * cut.items() + blockIdx.x) * 32 * P.d;
+  float* place = partial + ((size_t)bk * cut.places() + cut.place(blockIdx.x)) * 32 * P.d;
   sum_rows<DP, NW>(S, ak, w, lane, rows, P.d, [&](int x) {
     return parts > 1 ? place + x * P.d : dk + row_off(bk, k0 + x, P.ldk);
   });
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(256) void window_sum_f32_kernel(const float* __rest
                                                              float* __restrict__ b, Lay lb) {
   const int blk = blockIdx.x + (cut.psink > 1 ? 0 : cut.nsink), hx = blockIdx.y;
   const int rows = min(16, n - 16 * blk), parts = blk < cut.nsink ? cut.psink : cut.p;
-  const float* p = partial + ((size_t)hx * cut.items() + cut.item(blk)) * 16 * sets * d;
+  const float* p = partial + ((size_t)hx * cut.places() + cut.first_place(blk)) * 16 * sets * d;
   const int e = blockIdx.z * 256 + threadIdx.x, set = e / (16 * d), x = e - set * 16 * d;
   const int r = x / d, t = x - r * d;
   if (set >= sets || r >= rows) return;
@@ -459,7 +464,7 @@ hipError_t run_backward_f32(const WinProb& P, const float* q, const float* k, co
   auto sum = [&](const Cut& c, int heads, int n, int sets, float* a, const Lay& la, float* b,
                  const Lay& lb) {
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !c.cut()) return e;
+    if (e != hipSuccess || c.places() == 0) return e;
     const int blocks = (c.p > 1 ? c.nb : c.nsink) - (c.psink > 1 ? 0 : c.nsink);
     hipLaunchKernelGGL(window_sum_f32_kernel, dim3(blocks, heads, (16 * sets * P.d + 255) / 256),
                        dim3(256), 0, st, partial, c, n, P.d, sets, a, la, b, lb);
@@ -499,8 +504,8 @@ size_t window_backward_bytes(const WinProb& P) {
   if (P.dtype == CA_BF16) return window_grad_bf16_bytes(P);
   // the partial sums of dq, and after them those of dk and dv, in the same place
   const Cut cq = query_cut(P), ck = key_cut(P);
-  const size_t a = cq.cut() ? (size_t)P.B * P.H * cq.items() * 16 * P.d * 4 : 0;
-  const size_t b = ck.cut() ? (size_t)P.B * P.Hk * ck.items() * 32 * P.d * 4 : 0;
+  const size_t a = (size_t)P.B * P.H * cq.places() * 16 * P.d * 4;
+  const size_t b = (size_t)P.B * P.Hk * ck.places() * 32 * P.d * 4;
   return delta_bytes(P) + align256(a > b ? a : b);
 }
 

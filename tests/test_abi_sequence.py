@@ -258,3 +258,20 @@ def test_rope_refuses_an_output_for_keys_that_are_not_given():
     x = torch.zeros(1, 2, 4, 64)
     with pytest.raises(ValueError, match="k_out goes with k"):
         ca.rope(ca.rope_axes((32, 32)), x, grid=(2, 2), k_out=x)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_window_backward_workspace_holds_cut_blocks_only(dt):
+    """Two dense rows of 2^16 tokens a head, 16 sinks: partial sums of the keys' block that holds
+    the sinks (of one block of 16 to 128 keys, at most 64 parts), not of every block."""
+    L, lib = _lib()
+    n = ctypes.c_size_t(0)
+    N, H = 1 << 16, 4
+    st = I3(H * N * 64, N * 64, 64)
+    w = _window(dtype=L.CA_F32 if dt == "f32" else L.CA_BF16, batch=1, heads=H, heads_k=H, nq=N, nk=N, left=100, causal=1,
+                sinks=16, **{x + "_stride": st for x in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")})
+    assert lib.ca_window_workspace_size(w, 1, n) == L.CA_OK
+    rows = 2 * H * N * 4  # at most two numbers a query
+    assert n.value <= rows + H * 64 * 128 * 2 * 64 * 4 + 4096
+    w.sinks = 0
+    assert lib.ca_window_workspace_size(w, 1, n) == L.CA_OK and n.value <= rows + 4096

@@ -921,3 +921,10 @@ def test_inputs_that_require_gradients_are_detached():
     assert torch.equal(out, want) and not out.requires_grad
     for x in ca.window_attn_backward(ca.Window(left=5), out, q, k, v, out, lse):
         assert torch.isfinite(x).all()
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", [64, 128])
+def test_window_only_the_sinks_blocks_cut(dt, d):
+    """Launches of many blocks: those that hold sinks are cut, the others are not."""
+    _window_case(dt, 8, 4, 2, 1030, 1030, d, left=50, sinks=20, causal=True, seed=60)
