@@ -525,6 +525,17 @@ __global__ __launch_bounds__((64 * attn_waves<D, CQ, CK, SPLIT>()),
     // key half 0 through the stage buffers; the merged state takes the larger
     // reference of the halves that hold any key.
     static_assert(KSPL == 2, "two key halves");
+    // A sum far above its reference (the fast pass) takes one at its own size first: the
+    // merge compares references, and the exponential of a difference below -126 is 0.
+    if (l_tot > 0x1p60f) {
+      const int up = __builtin_amdgcn_frexp_expf(l_tot);
+      m_ref += (float)up;
+      l_tot = __builtin_amdgcn_ldexpf(l_tot, -up);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dt][r] = __builtin_amdgcn_ldexpf(oacc[dt][r], -up);
+    }
     constexpr int NV = 2 + 16 * DT;  // floats per lane
     // query tiles per round: as many as the stage buffers hold
     constexpr int QR = (2 * STAGE) / (NV * 64 * 4) < QW ? (2 * STAGE) / (NV * 64 * 4) : QW;

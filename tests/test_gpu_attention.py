@@ -459,3 +459,44 @@ def test_scheduled_launch_matches_index_order(pattern):
     torch.cuda.synchronize()
     assert torch.equal(op1, op0) and torch.equal(lse1, lse0)
     assert torch.isfinite(lse1[:, :n]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ck", [64, 128])
+@pytest.mark.parametrize("low,top", [(119.0, 127.0), (110.0, 118.0), (118.0, 126.0), (-40.0, 200.0)])
+@pytest.mark.parametrize("swap", [False, True])
+def test_key_halves_far_apart(d, ck, low, top, swap):
+    """Query clusters of 64 take a stage's 64 keys in two halves. The first half starts at 0 and goes
+    on at `low`, the second holds one key at `top` in its first stage and zeros else (all in log2 units;
+    with swap the halves are exchanged): their sums have weight both, against references up to 127 apart.
+    Products are exact (queries 2 in one dim; 2 scale log2(e) is 2 in bf16), so the output is off by
+    rounded probabilities and its own rounding, 2^-8 each, and the row sums by as much at most."""
+    import torch
+    import paper_2608_26965_amd as ca
+    from tests import gpu_util as G
+    from synth import bf16_round
+    n, cq, k, tau = 4 * ck, 64, 3, math.log(2.0)
+    G.flush(f"key halves d={d} ck={ck} low={low} top={top} swap={swap}")
+    rng = np.random.default_rng(5)
+    V, K, Q = (bf16_round(rng.standard_normal((1, n, d)).astype(np.float32)).astype(np.float64) for _ in range(3))
+    Q[:] = 0.0
+    Q[..., 0] = 2.0
+    half = (np.arange(n) % 64 >= 32) != swap
+    bits = np.where(half | (np.arange(n) < 64), 0.0, low)
+    bits[3 if swap else 40] = top
+    K[0, :, 0] = bits / 2.0
+    perm = np.arange(n, dtype=np.int32)[None]
+    lists = np.tile(np.arange(k, dtype=np.int32), (1, n // cq, 1))
+    p = ca.Problem(1, 1, n, n, d, cq, ck, torch.bfloat16)
+    op, lse = ca.block_sparse_attn(p, G.permuted_rows(Q, perm, cq, torch.bfloat16),
+                                   G.permuted_rows(K, perm, ck, torch.bfloat16),
+                                   G.value_tiles(V, perm, ck, torch.bfloat16), G.dev(G.counts(n, ck)[None], torch.int32),
+                                   G.dev(lists, torch.int32), k, scale=tau)
+    torch.cuda.synchronize()
+    op, lse = G.host(op)[0], G.host(lse)[0]
+    b = bits[:k * ck]
+    P = np.exp2(b - b.max())
+    want_lse, P = math.log(P.sum()) + math.log(2.0) * b.max(), P / P.sum()
+    want, size = P @ V[0, :k * ck], P @ np.abs(V[0, :k * ck])
+    assert (np.abs(op - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12) * size).all()
+    assert (np.abs(lse - want_lse) <= 2.0 ** -8 + 2.0 ** -12).all()
