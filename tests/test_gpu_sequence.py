@@ -928,3 +928,100 @@ def test_inputs_that_require_gradients_are_detached():
 def test_window_only_the_sinks_blocks_cut(dt, d):
     """Launches of many blocks: those that hold sinks are cut, the others are not."""
     _window_case(dt, 8, 4, 2, 1030, 1030, d, left=50, sinks=20, causal=True, seed=60)
+
+
+# ---- calls that the documentation allows ---------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("H,Hk", [(17, 1), (40, 1), (66, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_many_heads_cut_into_parts(dt, H, Hk, d):
+    """More than 16 query heads to a key head, with keys cut into parts and joined."""
+    import torch
+    ca = _ca()
+    g = _gen(70)
+    lens = [2100, 0, 700]
+    kp, vp, table, rows = _pages(g, dt, lens, 16, Hk, d)
+    q = _rand(g, (3, H, d), dt).cuda()
+    out, lse = ca.paged_attn(q, kp, vp, table, torch.tensor(lens, dtype=torch.int32).cuda(), want_lse=True)
+    _paged_check(q, out, lse, lens, rows, -1, 0, dt)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_pools_that_lie_in_one_tensor(dt):
+    """Keys and values of a page side by side, and of a token side by side."""
+    import torch
+    ca = _ca()
+    g = _gen(71)
+    lens = [37, 100]
+    n = torch.tensor(lens, dtype=torch.int32).cuda()
+    kp, vp, table, rows = _pages(g, dt, lens, 16, 2, 64)
+    q, k, v = (_rand(g, s, dt).cuda() for s in ((2, 4, 64), (2, 3, 2, 64), (2, 3, 2, 64)))
+    want = ca.paged_attn(q, kp, vp, table, n, want_lse=True)
+    for dim in (1, 2, 3):
+        both = torch.stack((kp, vp), dim)
+        a, b = both.unbind(dim)
+        got = ca.paged_attn(q, a, b, table, n, want_lse=True)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        wk, wv = kp.clone(), vp.clone()
+        ca.cache_append(k, v, a, b, table, n)
+        ca.cache_append(k, v, wk, wv, table, n)
+        for x, y in ((a, wk), (b, wv)):
+            assert torch.equal(torch.nan_to_num(x), torch.nan_to_num(y))
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd", "strided"])
+@pytest.mark.parametrize("pairing", ["interleaved", "halves"])
+def test_forward_turns_first_in_every_layout(dt, layout, pairing):
+    """forward(rotary=...) by a grid and by positions of each batch entry."""
+    import torch
+    ca = _ca()
+    B, H, n, d = 2, 2, 300, 64
+    qkv = _rand(_gen(72), (B, n, 3, H, d), dt).cuda()
+    q, k, v = (qkv[:, :, i] for i in range(3))
+    if layout != "bnhd":
+        q, k, v = (x.transpose(1, 2) for x in (q, k, v))
+    if layout != "strided":
+        q, k, v = (x.contiguous() for x in (q, k, v))
+    r = ca.rope_axes((24, 24, 16), pairing=pairing)
+    grid = torch.from_numpy(seq.grid_positions(n, (5, 6, 10)).astype(np.int32)).cuda()
+    far = torch.stack((grid, grid + 1000))
+    kw = dict(cq=64, keep=0.5, layout=layout)
+    for where, place in ((dict(rope_grid=(5, 6, 10)), dict(grid=(5, 6, 10))),
+                         (dict(rope_positions=grid), dict(positions=grid)), (dict(rope_positions=far), dict(positions=far))):
+        a = ca.forward(q, k, v, rotary=r, **where, **kw)
+        qr, kr = ca.rope(r, q, k, layout=layout, **place)
+        assert torch.equal(a, ca.forward(qr, kr, v, **kw))
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_two_graphs_with_one_workspace(dt):
+    """Steps captured apart that were given the same workspace, replayed by turns."""
+    import torch
+    ca = _ca()
+    w = ca.Window(left=300, sinks=70, causal=True)
+    sets = [[_rand(_gen(73 + i), (1, h, n, 64), dt).cuda() for h, n in ((4, 200), (2, 1500), (2, 1500), (4, 200))]
+            for i in range(2)]
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+
+    def step(q, k, v, do):
+        out, lse = ca.window_attn(w, q, k, v, want_lse=True, ws=ws)
+        return (out, lse) + ca.window_attn_backward(w, do, q, k, v, out, lse, ws=ws)
+
+    want = [[t.clone() for t in step(*s)] for s in sets]
+    graphs, held = [], []
+    for s in sets:
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            held.append(step(*s))
+    for _ in range(3):
+        for i in (0, 1, 1, 0):
+            graphs[i].replay()
+        step(*sets[1])
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+            for x in a:
+                x.zero_()
