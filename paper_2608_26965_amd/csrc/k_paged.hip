@@ -480,12 +480,13 @@ PagedPlan paged_plan(const PagedProb& P) {
   if (P.left < kNoWindow && (int64_t)P.left + 1 + P.sinks < most) seen = (int64_t)P.left + 1 + P.sinks;
   const int64_t all = (seen + kTile - 1) / kTile + 2;  // a window may begin and end inside a tile
   const int64_t wgs = (int64_t)P.B * P.Hk * ((P.G + 15) / 16);
-  // Workgroups of the launch if all sequences are as long as can be. Many
-  // sequences often have different lengths and balance in smaller parts (32 of 512 to
-  // 32,768: 276 us with 2,048, 239 with 4,096), few pay more for their joining
-  // (one of 262,144 with 16 heads: 203 and 210; four with 40 heads and 6,240 keys in
-  // the window: 114 and 119).
-  const int parts = P.B >= 8 ? 4096 : 2048;
+  // Workgroups of the launch if all sequences are as long as can be. Many sequences often
+  // have different lengths and balance in smaller parts, fewer pay more for their joining
+  // (lengths of 512 to 32,768 at 8 key heads of 128, us with 2,048 and 4,096: 4 sequences 73
+  // and 83, 6 71 and 81, 8 114 and 125, 12 152 and 144, 16 194 and 180, 32 175 and 173; equal
+  // lengths 2 to 5% more with 4,096; one of 262,144 with 16 heads 203 and 210; at 16 heads of
+  // 64 and one of 128 the two are within 3% from 8 sequences on).
+  const int parts = P.B >= 12 ? 4096 : 2048;
   int64_t tiles = (all * wgs + parts - 1) / parts;
   // A table can hold far more than the sequences have: 64 tiles at most keep short
   // sequences in wide tables parallel (20 parts of 40,000 keys in a table for a million),
