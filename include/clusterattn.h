@@ -397,6 +397,8 @@ CA_API int ca_attn_compensated_noalloc(const ca_problem* p, const void* qp, cons
  *   divides heads.
  * - Head dimensions: bf16 64 or 128, fp32 any multiple of 4 up to 128 (rotary:
  *   any multiple of 16 bytes up to 128).
+ * - Attention adds up probabilities times values in fp32 and divides at the end:
+ *   finite values have to stay below 2^96 in size.
  * - Every call can be captured into a graph: it allocates nothing, keeps
  *   nothing from one call for the next and records kernels only. */
 
@@ -445,9 +447,9 @@ CA_API int ca_rope(const ca_rope_desc* p, const void* q, const void* k, const in
  * [batch], clamped to [0, nq] and [0, nk] (NULL: nq, nk).
  *   out = sum_j e^{s_j - lse} v_j, lse = ln sum_j e^{s_j}, s_j = scale q . k_j
  * over the keys it sees (scale <= 0 selects 1/sqrt(d)). A query that sees no
- * key, and every row at or past len_q, has out = 0 and lse = -inf. Rows of k
- * and v at or past len_k are never read, and what a key or value that a query
- * does not see holds (infinities and NaN too) does not reach its output; a query
+ * key, and every row at or past len_q, has out = 0 and lse = -inf. What rows at
+ * or past the lengths hold, and what a key or value that a query does not see
+ * holds (infinities and NaN too), does not reach its output; a query
  * that sees a value that is not finite has an output that is not. (The backward
  * pass promises this for rows past the lengths only: a NaN or an infinity
  * in a token reaches the gradients of its neighbours, up to 127 tokens away.) */
@@ -508,7 +510,9 @@ typedef struct {
 CA_API int ca_cache_append(const ca_paged* p, const void* k, const void* v, void* k_pages,
                            void* v_pages, const int32_t* table, const int32_t* lens, void* stream);
 
-/* Bytes of workspace of ca_paged_attn (256-byte aligned; may be 0). Host-only. */
+/* Bytes of workspace of ca_paged_attn (256-byte aligned; may be 0). The lengths
+ * are on the device, so it goes with the table's width (partial results of up to
+ * max_pages * page visible keys for every sequence and head). Host-only. */
 CA_API int ca_paged_workspace_size(const ca_paged* p, size_t* bytes);
 
 /* Attention of one query per sequence and head, its last token (position

@@ -42,7 +42,8 @@ constexpr int KT = 64;           // streamed rows of a tile
 constexpr int NW = 4;            // wavefronts of a workgroup, W kept rows each
 
 // Kept rows of a wavefront: 16, or 32 where keys are kept at d = 64 and the window is long.
-// 16 rows leave three waves a SIMD at d = 64 and two at d = 128 (32 there, one wave with
+// 16 rows leave four waves a SIMD at d = 64 with queries kept (128 registers) and three with
+// keys kept (143; two with 32 rows), two at d = 128 (32 there, one wave with
 // half the registers accumulation registers that operands are copied through: 793 us
 // for the padded batch of three where 16 took 726), and four wavefronts of them make
 // blocks of 64, of which several share a compute unit, not at the same point of a tile at the
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(256) void window_grad_join_kernel(const WinProb P, 
 // as many as the chip holds, others fill it and leave half the longest over; partial sums
 // (2 d floats a row, written and read) cost 0.015 for 128 rows and a launch 3. Twice
 // that for the sums took 502 us instead of 387 for 3 heads of 7,553 tokens (d = 128, 357
-// blocks on 512 places), but 252 instead of 270 for 10 heads of 3,186. 8,192 tokens on 2
+// blocks on 512 places), but 252 instead of 270 for 10 heads on 2 of 3,186 (causal). 8,192 tokens on 2
 // key heads take one round of 24 tiles (three parts, 159 us with the forward pass) instead
 // of two of 18 (166).
 Parts cut(int nb, int nsink, int64_t all, int64_t seen, int64_t heads, int rows, bool uneven) {

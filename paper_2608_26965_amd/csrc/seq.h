@@ -87,7 +87,8 @@ size_t window_grad_bf16_bytes(const WinProb& P);
 hipError_t launch_window_grad_bf16(const WinProb& P, const void* q, const void* k, const void* v,
                                    const void* out, const float* lse, const void* dout, void* dq,
                                    void* dk, void* dv, char* ws, hipStream_t st);
-// Workspace of the backward pass (fp32): delta (the row sums of dout * out), fp32 [B H][nq]
+// Workspace of the backward pass (fp32): delta (the row sums of dout * out), fp32 [B H][nq],
+// then the partial sums of the blocks that are cut, those of dq and afterwards of dk and dv
 size_t window_backward_bytes(const WinProb& P);
 hipError_t launch_window_backward(const WinProb& P, const void* q, const void* k, const void* v,
                                   const void* out, const float* lse, const void* dout, void* dq,
@@ -102,7 +103,7 @@ struct RopeProb {
   int axes, npairs, halves;
   int end[kMaxAxes];   // pairs [end[a - 1], end[a]) turn with axis a
   int grid[kMaxAxes], start[kMaxAxes];
-  int inner[kMaxAxes]; // tokens between neighbours on the axis; INT32_MAX from n on
+  int inner[kMaxAxes]; // tokens between neighbours on the axis, INT32_MAX at most
   float sign;          // of the angle: -1 for the transposed rotation
   const int32_t* pos;  // NULL: from the grid
   int64_t pos_sb, pos_sa, pos_sn;

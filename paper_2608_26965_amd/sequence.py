@@ -456,8 +456,9 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     and the first `sinks`. q: [B,H,d]; k_pages, v_pages: [pages, page, Hk, d],
     any strides, Hk a divisor of H; page_table: int32 [B, max_pages]; lens:
     int32 [B], the new token included. Returns (out [B,H,d], lse [B,H] fp32 or
-    None); a sequence of no tokens gives 0 and -inf. Not recorded by autograd,
-    and without a backward pass."""
+    None); a sequence of no tokens gives 0 and -inf. The workspace goes with
+    the table's width, not the lengths. Not recorded by autograd, and without a
+    backward pass."""
     if torch.is_grad_enabled():
         _unrecorded((q, k_pages, v_pages), (out,))
     _on(q, k_pages, v_pages, page_table, lens, out)
