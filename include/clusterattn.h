@@ -525,6 +525,103 @@ CA_API int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages,
                          const void* v_pages, const int32_t* table, const int32_t* lens, void* out,
                          float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Chunks of new tokens over the paged cache --------------------------------
+ *
+ * A step of a serving program takes any number of new tokens of each of its
+ * sequences: one where a sequence goes on, a few where drafted tokens are checked,
+ * a frame of a video, all of a prompt. The new tokens lie packed, one sequence
+ * after the other: those of sequence b are rows starts[b] .. starts[b + 1] - 1 of
+ * arrays of `tokens` rows (starts: device int32 [batch + 1], ascending from 0; the
+ * rows from starts[batch] on are room for more). lens[b] counts the sequence's
+ * tokens, the new ones, its last, included.
+ *
+ * ca_cache_grow finds pages for the new tokens and says where they go,
+ * ca_cache_write puts their keys and values there, ca_paged_chunk_attn attends,
+ * ca_cache_release gives pages back.
+ *
+ * The pages that no sequence holds are free_pages[0 .. state[0] - 1], a stack:
+ * device int32 free_pages[pages], the next page to be taken last. state: device
+ * int32 [3]: the number of free pages; pages that the last ca_cache_grow lacked;
+ * new tokens for which it had no rows. A free page must not stand twice in the
+ * stack, nor in a table. */
+typedef struct {
+  int32_t batch, page, pages, max_pages; /* as in ca_paged; max_pages * page < 2^30 */
+  int32_t tokens;                        /* ca_cache_grow: rows of slots and positions, >= 1 */
+  int32_t left, sinks;                   /* ca_cache_release */
+  int64_t table_stride;                  /* >= max_pages where batch > 1 */
+} ca_pages;
+
+/* Pages for the new tokens of a step, and where they go. n_new: device int32
+ * [batch], how many of the lens[b] tokens are new (clamped to [0, lens[b]]; lens to
+ * [0, max_pages * page]).
+ *
+ * Every entry of the table that a new token lies on (those of places lens[b] -
+ * n_new[b] .. lens[b] - 1) and that holds no page (a value outside [0, pages)) gets
+ * one: the first such entry, by sequence and place, the last of the stack, and so
+ * on. Entries that hold one stay, so a call repeated changes nothing. Where the
+ * stack runs short the later entries stay as they are and state[1] says how
+ * many; it is 0 else.
+ *
+ * starts[b] = the sum of n_new[0 .. b - 1], at most `tokens` (state[2] says how many
+ * tokens are beyond). slots (device int64 [tokens]): the place of a row's token in
+ * the pools, page * (its table entry) + place in the page, -1 where there is no
+ * page and in rows from starts[batch] on. positions (device int32 [tokens]): the
+ * token's place in its sequence (as ca_rope reads it), 0 in rows from
+ * starts[batch] on. */
+CA_API int ca_cache_grow(const ca_pages* p, const int32_t* lens, const int32_t* n_new,
+                         int32_t* table, int32_t* free_pages, int32_t* state, int32_t* starts,
+                         int64_t* slots, int32_t* positions, void* stream);
+
+/* Gives back the pages that hold no token which the next one of its sequence sees:
+ * an entry i of row b keeps its page where a token j of its places (i * page <= j <
+ * (i + 1) * page) has j < lens[b] and, with left >= 0, j < sinks or j >= lens[b] -
+ * left. All others in [0, pages) go to the stack, the first one, by sequence and
+ * place, on top (what ca_cache_grow took goes back as it came), and become -1.
+ * lens[b] = 0 gives back all of a finished sequence, a smaller length than before
+ * the pages of rejected tokens, left and sinks those behind a window. A page that
+ * stands in several rows (a common beginning) must not go back from two of them.
+ * ws: workspace (ca_cache_release_workspace_size, 256-byte aligned). */
+CA_API int ca_cache_release(const ca_pages* p, const int32_t* lens, int32_t* table,
+                            int32_t* free_pages, int32_t* state, void* ws, size_t ws_bytes,
+                            void* stream);
+CA_API int ca_cache_release_workspace_size(const ca_pages* p, size_t* bytes);
+
+/* Attention of the new tokens, and what ca_cache_write writes */
+typedef struct {
+  int32_t batch, heads, heads_k, d, dtype; /* ca_cache_write: heads_k, d and dtype only */
+  int32_t page, pages, max_pages;          /* ca_cache_write: page and pages only */
+  int32_t tokens;                          /* rows of q and out (of k and v), 1..2^24 */
+  int32_t left, right, sinks, causal;      /* as in ca_window */
+  float scale;
+  int64_t table_stride;
+  int64_t k_stride[3], v_stride[3];         /* pools: {page, token, head} */
+  int64_t q_stride[2], out_stride[2];       /* {token, head} */
+  int64_t k_new_stride[2], v_new_stride[2]; /* ca_cache_write: {token, head} */
+} ca_chunk;
+
+/* Writes row t of k and v to place slots[t] (device int64 [tokens]) of the pools:
+ * token slots[t] % page of page slots[t] / page. Rows whose slot lies outside
+ * [0, pages * page) are left out. No two rows may have the same slot. */
+CA_API int ca_cache_write(const ca_chunk* p, const void* k, const void* v, void* k_pages,
+                          void* v_pages, const int64_t* slots, void* stream);
+
+/* Attention of packed queries over the cache of their sequences. Query i of the
+ * lq = starts[b + 1] - starts[b] of sequence b sits at p = i + lens[b] - lq (the last
+ * one beside the last key) and sees the keys that ca_window_attn shows it: j <
+ * lens[b] where (j < sinks or p - left <= j <= p + right) and (not causal or j <= p).
+ * out, lse as there: 0 and -inf where a query sees no key. Keys on entries outside
+ * [0, pages) are not there; what keys and values that a query does not see
+ * hold does not reach it. starts are clamped to [0, tokens], lens to
+ * [0, max_pages * page]. Rows of out and lse (optional, dense fp32 [tokens][heads])
+ * before starts[0] and from starts[batch] on are left as they were. ws: workspace. */
+CA_API int ca_paged_chunk_attn(const ca_chunk* p, const void* q, const void* k_pages,
+                               const void* v_pages, const int32_t* table, const int32_t* lens,
+                               const int32_t* starts, void* out, float* lse, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* Bytes of workspace of ca_paged_chunk_attn (256-byte aligned; may be 0). Host-only. */
+CA_API int ca_paged_chunk_workspace_size(const ca_chunk* p, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -62,3 +62,43 @@ def attend_backward(q, k, v, do, see, scale):
     dP = do @ v.T
     dS = P * (dP - (do * o).sum(1, keepdims=True))
     return scale * (dS @ k), scale * (dS.T @ q), P.T @ do
+
+
+# ---- pages of a cache, entry by entry -----------------------------------------------------------
+
+def cache_grow(table, free, lens, new, page, pages, tokens):
+    """table: rows of entries and free: a list, its end taken first, both changed. Returns
+    (state, starts, slots, positions)."""
+    lacked, starts, slots, positions = 0, [0], [], []
+    for b, row in enumerate(table):
+        n = min(max(int(lens[b]), 0), len(row) * page)
+        m = min(max(int(new[b]), 0), n)
+        for i in range((n - m) // page, -(-n // page) if m else 0):
+            if not 0 <= row[i] < pages:
+                if free:
+                    row[i] = free.pop()
+                else:
+                    lacked += 1
+        for j in range(n - m, n):
+            e = int(row[j // page])
+            slots.append(e * page + j % page if 0 <= e < pages else -1)
+            positions.append(j)
+        starts.append(starts[-1] + m)
+    total = starts[-1]
+    rest = max(0, tokens - total)
+    return ([len(free), lacked, max(0, total - tokens)], [min(x, tokens) for x in starts],
+            slots[:tokens] + [-1] * rest, positions[:tokens] + [0] * rest)
+
+
+def cache_release(table, free, lens, page, pages, left=-1, sinks=0):
+    """Pages without a token that the sequence's next one sees go to free's end, the first of
+    them last; their entries become -1."""
+    gone = []
+    for b, row in enumerate(table):
+        n = min(max(int(lens[b]), 0), len(row) * page)
+        for i, e in enumerate(row):
+            places = range(i * page, min((i + 1) * page, n))
+            if not any(left < 0 or j < sinks or j >= n - left for j in places) and 0 <= e < pages:
+                gone.append(int(e))
+                row[i] = -1
+    free.extend(reversed(gone))

@@ -22,13 +22,16 @@ from . import _lib
 from ._lib import (CA_BF16, CA_F32, CA_LAYOUT_BHND, CA_LAYOUT_BNHD, CA_LAYOUT_STRIDED,
                    CA_SPLIT_BASIC, CA_SPLIT_DIAG, CA_XF_ADAPTIVE, CA_XF_METRIC, CA_XF_NONE,
                    CA_XF_PCA, CA_XF_RANDOM, CAError)
-from .sequence import (Rope, Window, cache_append, paged_attn, rope, rope_axes, window_attn,
-                       window_attn_backward)
+from .sequence import (CacheStep, PagePool, Rope, Window, cache_append, cache_grow, cache_release,
+                       cache_write, page_pool, paged_attn, paged_chunk_attn, rope, rope_axes,
+                       window_attn, window_attn_backward)
 
 __all__ = ["Problem", "bhnd_strides", "workspace_size", "cluster", "select", "select_hist", "block_sparse_attn",
            "compensate", "attn_compensated", "attn_compensated_noalloc", "check_finite",
            "forward", "CAError", "abi_version", "Rope", "rope_axes", "rope", "Window",
-           "window_attn", "window_attn_backward", "cache_append", "paged_attn"]
+           "window_attn", "window_attn_backward", "cache_append", "paged_attn", "PagePool",
+           "page_pool", "CacheStep", "cache_grow", "cache_release", "cache_write",
+           "paged_chunk_attn"]
 
 _XF = {"none": CA_XF_NONE, "pca": CA_XF_PCA, "metric": CA_XF_METRIC, "adaptive": CA_XF_ADAPTIVE,
        "random": CA_XF_RANDOM}

@@ -33,6 +33,12 @@ EXPORTS = (
     "ca_cache_append",
     "ca_paged_workspace_size",
     "ca_paged_attn",
+    "ca_cache_grow",
+    "ca_cache_release",
+    "ca_cache_release_workspace_size",
+    "ca_cache_write",
+    "ca_paged_chunk_attn",
+    "ca_paged_chunk_workspace_size",
 )
 
 _i32 = ctypes.c_int32
@@ -78,6 +84,20 @@ class CaPaged(ctypes.Structure):
                    ("q_stride", ctypes.c_int64 * 2), ("out_stride", ctypes.c_int64 * 2),
                    ("n_new", _i32), ("k_new_stride", ctypes.c_int64 * 3),
                    ("v_new_stride", ctypes.c_int64 * 3)])
+
+
+class CaPages(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("batch", "page", "pages", "max_pages", "tokens", "left", "sinks")]
+                + [("table_stride", ctypes.c_int64)])
+
+
+class CaChunk(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("batch", "heads", "heads_k", "d", "dtype", "page", "pages",
+                                     "max_pages", "tokens", "left", "right", "sinks", "causal")]
+                + [("scale", ctypes.c_float), ("table_stride", ctypes.c_int64),
+                   ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+                + [(n, ctypes.c_int64 * 2) for n in ("q_stride", "out_stride", "k_new_stride",
+                                                     "v_new_stride")])
 
 
 class CAError(RuntimeError):
@@ -141,7 +161,14 @@ def load() -> ctypes.CDLL:
     lib.ca_cache_append.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 7
     lib.ca_paged_workspace_size.argtypes = [ctypes.POINTER(CaPaged), size]
     lib.ca_paged_attn.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
-    for name in EXPORTS[-7:]:
+    pages, chunk = ctypes.POINTER(CaPages), ctypes.POINTER(CaChunk)
+    lib.ca_cache_grow.argtypes = [pages] + [_vp] * 9
+    lib.ca_cache_release.argtypes = [pages] + [_vp] * 5 + [ctypes.c_size_t, _vp]
+    lib.ca_cache_release_workspace_size.argtypes = [pages, size]
+    lib.ca_cache_write.argtypes = [chunk] + [_vp] * 6
+    lib.ca_paged_chunk_attn.argtypes = [chunk] + [_vp] * 9 + [ctypes.c_size_t, _vp]
+    lib.ca_paged_chunk_workspace_size.argtypes = [chunk, size]
+    for name in EXPORTS[EXPORTS.index("ca_rope"):]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

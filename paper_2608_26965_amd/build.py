@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libclusterattn.so")
 SOURCES = ["api.hip", "k_cluster.hip", "k_select.hip", "k_attn.hip", "k_comp.hip", "k_rope.hip", "k_window.hip",
-           "k_window_bf16.hip", "k_window_grad.hip", "k_paged.hip"]
+           "k_window_bf16.hip", "k_window_grad.hip", "k_paged.hip", "k_pages.hip", "k_chunk.hip"]
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 FLAGS = [

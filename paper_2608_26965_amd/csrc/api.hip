@@ -197,7 +197,7 @@ int check_strides(const int64_t* st, int n, int dtype, const char* name) {
 
 // an output's rows must have places of their own
 int check_written(const int64_t* st, int s0, int s1, int s2, const char* name) {
-  const int size[3] = {s0, s1, s2};
+  const int size[3] = {s0, s1, s2};  // (the stride of a dimension of one is not looked at)
   for (int j = 0; j < 3; ++j)
     if (size[j] > 1 && st[j] == 0)
       return fail(CA_E_INVALID, "%s_stride[%d] is 0: the rows of an output would overlap", name, j);
@@ -332,6 +332,87 @@ int check_paged_attn(const ca_paged* p, ca::PagedProb* P) {
     return s;
   if ((p->batch > 1 && p->out_stride[0] == 0) || (p->heads > 1 && p->out_stride[1] == 0))
     return fail(CA_E_INVALID, "out_stride is 0: the rows of an output would overlap");
+  return CA_OK;
+}
+
+int check_pool(int page, int pages, int max_pages) {
+  if (page < 1 || pages < 1 || max_pages < 1)
+    return fail(CA_E_INVALID, "page, pages and max_pages must be >= 1");
+  if ((int64_t)page * max_pages >= (1 << 30))
+    return fail(CA_E_UNSUPPORTED, "max_pages * page must be below 2^30");
+  return CA_OK;
+}
+
+int check_pages(const ca_pages* p, ca::PagesProb* P) {
+  if (!p) return fail(CA_E_INVALID, "pages is NULL");
+  int s;
+  if (p->batch < 1) return fail(CA_E_INVALID, "batch must be >= 1");
+  if (p->batch > 65535) return fail(CA_E_UNSUPPORTED, "batch above 65535");
+  if ((s = check_pool(p->page, p->pages, p->max_pages))) return s;
+  // rows are written: they must not overlap
+  if (p->batch > 1 && p->table_stride < p->max_pages)
+    return fail(CA_E_INVALID, "table_stride = %lld is less than max_pages = %d",
+                (long long)p->table_stride, p->max_pages);
+  P->B = p->batch;
+  P->page = p->page;
+  P->pages = p->pages;
+  P->max_pages = p->max_pages;
+  P->tokens = p->tokens;
+  P->left = p->left < 0 || p->left > ca::kNoWindow ? ca::kNoWindow : p->left;
+  P->sinks = p->sinks;
+  P->table_sb = p->table_stride;
+  return CA_OK;
+}
+
+constexpr int kMostTokens = 1 << 24;
+
+int check_chunk(const ca_chunk* p, ca::ChunkProb* P) {
+  if (!p) return fail(CA_E_INVALID, "chunk is NULL");
+  int s;
+  if (p->batch < 1 || p->heads < 1 || p->heads_k < 1)
+    return fail(CA_E_INVALID, "batch, heads and heads_k must be >= 1");
+  if (p->heads % p->heads_k != 0)
+    return fail(CA_E_INVALID, "heads = %d is not a multiple of heads_k = %d", p->heads, p->heads_k);
+  if (p->batch > 65535 || p->heads > 65535)
+    return fail(CA_E_UNSUPPORTED, "batch or heads above 65535");
+  if ((s = check_dtype(p->dtype)) || (s = check_head_dim(p->d, p->dtype)) ||
+      (s = check_pool(p->page, p->pages, p->max_pages)))
+    return s;
+  if (p->tokens < 1 || p->tokens > kMostTokens)
+    return fail(CA_E_INVALID, "tokens = %d must be in [1, 2^24]", p->tokens);
+  if (p->sinks < 0) return fail(CA_E_INVALID, "sinks = %d must be >= 0", p->sinks);
+  if (p->table_stride < 0) return fail(CA_E_INVALID, "table_stride must be >= 0");
+  if ((s = check_strides(p->k_stride, 3, p->dtype, "k")) ||
+      (s = check_strides(p->v_stride, 3, p->dtype, "v")) ||
+      (s = check_strides(p->q_stride, 2, p->dtype, "q")) ||
+      (s = check_strides(p->out_stride, 2, p->dtype, "out")) ||
+      (s = check_written(p->out_stride, p->tokens, p->heads, 1, "out")))
+    return s;
+  auto side = [](int x) { return x < 0 || x >= ca::kNoWindow ? ca::kNoWindow - 1 : x; };
+  P->B = p->batch;
+  P->H = p->heads;
+  P->Hk = p->heads_k;
+  P->G = p->heads / p->heads_k;
+  P->d = p->d;
+  P->dtype = p->dtype;
+  P->page = p->page;
+  P->pages = p->pages;
+  P->max_pages = p->max_pages;
+  P->tokens = p->tokens;
+  P->m = ca::WinMask{side(p->left), side(p->right), p->sinks, p->causal != 0};
+  P->scale = scale_of(p->scale, p->d);
+  P->table = P->lens = P->starts = nullptr;
+  P->table_sb = p->table_stride;
+  P->q_st = p->q_stride[0];
+  P->q_sh = p->q_stride[1];
+  P->o_st = p->out_stride[0];
+  P->o_sh = p->out_stride[1];
+  P->k_sp = p->k_stride[0];
+  P->k_st = p->k_stride[1];
+  P->k_sh = p->k_stride[2];
+  P->v_sp = p->v_stride[0];
+  P->v_st = p->v_stride[1];
+  P->v_sh = p->v_stride[2];
   return CA_OK;
 }
 
@@ -860,6 +941,112 @@ int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages, const v
   return device_status(ca::launch_paged(P, q, k_pages, v_pages, out, lse, (char*)ws,
                                         (hipStream_t)stream),
                        "ca_paged_attn");
+}
+
+int ca_cache_grow(const ca_pages* p, const int32_t* lens, const int32_t* n_new, int32_t* table,
+                  int32_t* free_pages, int32_t* state, int32_t* starts, int64_t* slots,
+                  int32_t* positions, void* stream) {
+  ca::PagesProb P;
+  int s = check_pages(p, &P);
+  if (s) return s;
+  if (p->tokens < 1 || p->tokens > kMostTokens)
+    return fail(CA_E_INVALID, "tokens = %d must be in [1, 2^24]", p->tokens);
+  if (!lens || !n_new || !table || !free_pages || !state || !starts || !slots || !positions)
+    return fail(CA_E_INVALID, "lens, n_new, table, free_pages, state, starts, slots and positions are required");
+  P.lens = lens;
+  P.table = table;
+  P.free = free_pages;
+  P.state = state;
+  return device_status(ca::launch_grow(P, n_new, starts, slots, positions, (hipStream_t)stream),
+                       "ca_cache_grow");
+}
+
+int ca_cache_release_workspace_size(const ca_pages* p, size_t* bytes) {
+  ca::PagesProb P;
+  int s = check_pages(p, &P);
+  if (s) return s;
+  if (!bytes) return fail(CA_E_INVALID, "bytes is NULL");
+  *bytes = ca::release_bytes(P);
+  return ok();
+}
+
+int ca_cache_release(const ca_pages* p, const int32_t* lens, int32_t* table, int32_t* free_pages,
+                     int32_t* state, void* ws, size_t ws_bytes, void* stream) {
+  ca::PagesProb P;
+  int s = check_pages(p, &P);
+  if (s) return s;
+  if (p->sinks < 0) return fail(CA_E_INVALID, "sinks = %d must be >= 0", p->sinks);
+  if (!lens || !table || !free_pages || !state)
+    return fail(CA_E_INVALID, "lens, table, free_pages and state are required");
+  if ((s = check_bytes(ca::release_bytes(P), ws, ws_bytes))) return s;
+  P.lens = lens;
+  P.table = table;
+  P.free = free_pages;
+  P.state = state;
+  return device_status(ca::launch_release(P, (char*)ws, (hipStream_t)stream), "ca_cache_release");
+}
+
+int ca_cache_write(const ca_chunk* p, const void* k, const void* v, void* k_pages, void* v_pages,
+                   const int64_t* slots, void* stream) {
+  if (!p) return fail(CA_E_INVALID, "chunk is NULL");
+  int s;
+  if (p->heads_k < 1 || p->heads_k > 65535)
+    return fail(CA_E_INVALID, "heads_k = %d must be in [1, 65535]", p->heads_k);
+  if ((s = check_dtype(p->dtype)) || (s = check_head_dim(p->d, p->dtype)) ||
+      (s = check_pool(p->page, p->pages, 1)))
+    return s;
+  if (p->tokens < 1 || p->tokens > kMostTokens)
+    return fail(CA_E_INVALID, "tokens = %d must be in [1, 2^24]", p->tokens);
+  if ((int64_t)p->tokens * p->heads_k * (p->d / 4) >= ((int64_t)1 << 31))
+    return fail(CA_E_UNSUPPORTED, "tokens * heads_k * d too large");
+  if (!slots) return fail(CA_E_INVALID, "slots is NULL");
+  if ((s = check_base(k, "k")) || (s = check_base(v, "v")) || (s = check_base(k_pages, "k_pages")) ||
+      (s = check_base(v_pages, "v_pages")) || (s = check_strides(p->k_stride, 3, p->dtype, "k")) ||
+      (s = check_strides(p->v_stride, 3, p->dtype, "v")) ||
+      (s = check_strides(p->k_new_stride, 2, p->dtype, "k_new")) ||
+      (s = check_strides(p->v_new_stride, 2, p->dtype, "v_new")) ||
+      (s = check_written(p->k_stride, p->pages, p->page, p->heads_k, "k")) ||
+      (s = check_written(p->v_stride, p->pages, p->page, p->heads_k, "v")))
+    return s;
+  const ca::WriteProb P{p->heads_k,         p->d,
+                        p->dtype,           p->page,
+                        p->pages,           p->tokens,
+                        slots,              p->k_new_stride[0],
+                        p->k_new_stride[1], p->v_new_stride[0],
+                        p->v_new_stride[1], p->k_stride[0],
+                        p->k_stride[1],     p->k_stride[2],
+                        p->v_stride[0],     p->v_stride[1],
+                        p->v_stride[2]};
+  return device_status(ca::launch_write(P, k, v, k_pages, v_pages, (hipStream_t)stream),
+                       "ca_cache_write");
+}
+
+int ca_paged_chunk_workspace_size(const ca_chunk* p, size_t* bytes) {
+  ca::ChunkProb P;
+  int s = check_chunk(p, &P);
+  if (s) return s;
+  if (!bytes) return fail(CA_E_INVALID, "bytes is NULL");
+  *bytes = ca::chunk_bytes(P);
+  return ok();
+}
+
+int ca_paged_chunk_attn(const ca_chunk* p, const void* q, const void* k_pages, const void* v_pages,
+                        const int32_t* table, const int32_t* lens, const int32_t* starts, void* out,
+                        float* lse, void* ws, size_t ws_bytes, void* stream) {
+  ca::ChunkProb P;
+  int s = check_chunk(p, &P);
+  if (s) return s;
+  if (!table || !lens || !starts) return fail(CA_E_INVALID, "table, lens and starts are required");
+  if ((s = check_base(q, "q")) || (s = check_base(k_pages, "k_pages")) ||
+      (s = check_base(v_pages, "v_pages")) || (s = check_base(out, "out")))
+    return s;
+  if ((s = check_bytes(ca::chunk_bytes(P), ws, ws_bytes))) return s;
+  P.table = table;
+  P.lens = lens;
+  P.starts = starts;
+  return device_status(ca::launch_chunk(P, q, k_pages, v_pages, out, lse, (char*)ws,
+                                        (hipStream_t)stream),
+                       "ca_paged_chunk_attn");
 }
 
 }  // extern "C"

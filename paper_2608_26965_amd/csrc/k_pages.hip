@@ -1,0 +1,303 @@
+// Page tables and slot maps from the sequences' lengths, pages given back, and
+// new keys and values written by the slot map.
+//
+// What bounds them: latency. A step's tables are a few kilobytes; the launches and
+// the chains of dependent loads (length, entry, free page) are what takes time.
+// The writes of keys and values are bound by memory traffic, each read and
+// written once.
+#include "seq.h"
+
+namespace ca {
+
+namespace {
+
+constexpr int kGrow = 1024;  // threads of the growing workgroup
+constexpr int kItems = 8;    // entries that a thread looks at in one go
+
+// Sum of x over the threads before this one, and over all of them (NW wavefronts)
+template <int NW, typename T>
+__device__ __forceinline__ T scan_before(T x, T (&sums)[NW], T* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  T in = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(in, o, 64);
+    if (lane >= o) in += y;
+  }
+  __syncthreads();  // the sums of a scan before are read
+  if (lane == 63) sums[w] = in;
+  __syncthreads();
+  T before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    if (i < w) before += sums[i];
+    all += sums[i];
+  }
+  *total = all;
+  return before + in - x;
+}
+
+// New tokens of sequence b, its last n of len
+struct NewTokens {
+  int len, n;
+  __device__ __forceinline__ NewTokens(const PagesProb& P, const int32_t* n_new, int b) {
+    len = P.len(b);
+    n = min(max(n_new[b], 0), len);
+  }
+};
+
+// Slot and position of packed row t, from the starts and the grown table
+__device__ __forceinline__ void place_token(const PagesProb& P, const int32_t* n_new,
+                                            const int32_t* starts, int t, int64_t* slots,
+                                            int32_t* positions) {
+  int64_t slot = -1;
+  int pos = 0;
+  if (t < starts[P.B]) {
+    int lo = 0, hi = P.B;  // starts[lo] <= t < starts[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (starts[mid] <= t)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const NewTokens s(P, n_new, lo);
+    pos = s.len - s.n + (t - starts[lo]);
+    const int e = P.table[lo * P.table_sb + pos / P.page];
+    if (e >= 0 && e < P.pages) slot = (int64_t)e * P.page + pos % P.page;
+  }
+  slots[t] = slot;
+  positions[t] = pos;
+}
+
+// One workgroup: starts, and pages for the entries that lack one. Sequences are
+// taken 1,024 at a time, the entries that their new tokens lie on one after the
+// other, thread by thread; a ballot says how many of the entries before lack a
+// page. With SLOTS also the slots (few tokens: one launch less).
+template <bool SLOTS>
+__global__ __launch_bounds__(kGrow) void grow_kernel(const PagesProb P,
+                                                     const int32_t* n_new, int32_t* starts,
+                                                     int64_t* slots, int32_t* positions) {
+  constexpr int NW = kGrow / 64;
+  __shared__ int64_t first_item[kGrow + 1];  // entries of the sequences before
+  __shared__ int32_t first_entry[kGrow];
+  __shared__ int64_t sums[NW];
+  __shared__ int32_t counts[kItems][NW];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n_free = min(max(P.state[0], 0), P.pages);
+  int64_t tokens = 0, taken = 0;
+  for (int b0 = 0; b0 < P.B; b0 += kGrow) {
+    const int b = b0 + tid;
+    int n = 0, e0 = 0, entries = 0;
+    if (b < P.B) {
+      const NewTokens s(P, n_new, b);
+      n = s.n;
+      e0 = (s.len - s.n) / P.page;
+      entries = n > 0 ? (s.len - 1) / P.page - e0 + 1 : 0;
+    }
+    int64_t total, items;
+    const int64_t before = tokens + scan_before<NW, int64_t>(n, sums, &total);
+    const int64_t item0 = scan_before<NW, int64_t>(entries, sums, &items);
+    if (b < P.B) starts[b] = (int32_t)min(before, (int64_t)P.tokens);
+    tokens += total;
+    first_item[tid] = item0;
+    first_entry[tid] = e0;
+    if (tid == 0) first_item[kGrow] = items;
+    __syncthreads();
+    for (int64_t i0 = 0; i0 < items; i0 += kGrow * kItems) {
+      int64_t at[kItems];
+      uint32_t lack = 0;
+#pragma unroll
+      for (int r = 0; r < kItems; ++r) {
+        const int64_t i = i0 + r * kGrow + tid;
+        bool l = false;
+        at[r] = 0;
+        if (i < items) {
+          int lo = 0, hi = kGrow;  // first_item[lo] <= i < first_item[hi]
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first_item[mid] <= i)
+              lo = mid;
+            else
+              hi = mid;
+          }
+          at[r] = (b0 + lo) * P.table_sb + first_entry[lo] + (i - first_item[lo]);
+          const int e = P.table[at[r]];
+          l = e < 0 || e >= P.pages;
+        }
+        const uint64_t who = __ballot(l);
+        if (lane == 0) counts[r][w] = __popcll(who);
+        if (l) lack |= 1u << r;
+      }
+      __syncthreads();
+      int64_t rank = taken;
+#pragma unroll
+      for (int r = 0; r < kItems; ++r) {
+        const bool l = (lack >> r) & 1u;
+        const uint64_t who = __ballot(l);
+        int before_me = 0, all = 0;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) {
+          if (x < w) before_me += counts[r][x];
+          all += counts[r][x];
+        }
+        if (l) {
+          const int64_t k = rank + before_me + __popcll(who & ((1ull << lane) - 1));
+          if (k < n_free) P.table[at[r]] = P.free[n_free - 1 - k];
+        }
+        rank += all;
+      }
+      taken = rank;
+      __syncthreads();  // the counts are read
+    }
+  }
+  if (tid == 0) {
+    starts[P.B] = (int32_t)min(tokens, (int64_t)P.tokens);
+    P.state[0] = (int32_t)max(n_free - taken, (int64_t)0);
+    P.state[1] = (int32_t)min(max(taken - n_free, (int64_t)0), (int64_t)INT32_MAX);
+    P.state[2] = (int32_t)min(max(tokens - P.tokens, (int64_t)0), (int64_t)INT32_MAX);
+  }
+  if constexpr (SLOTS) {
+    __syncthreads();
+    for (int t = tid; t < P.tokens; t += kGrow)
+      place_token(P, n_new, starts, t, slots, positions);
+  }
+}
+
+__global__ __launch_bounds__(256) void slots_kernel(const PagesProb P,
+                                                    const int32_t* __restrict__ n_new,
+                                                    const int32_t* __restrict__ starts,
+                                                    int64_t* __restrict__ slots,
+                                                    int32_t* __restrict__ positions) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t < P.tokens) place_token(P, n_new, starts, t, slots, positions);
+}
+
+// Whether entry i of a sequence of n tokens holds a page that goes back
+__device__ __forceinline__ bool goes_back(const PagesProb& P, int n, int i, int e) {
+  const int first = i * P.page, last = min(first + P.page, n) - 1;
+  const bool keep = first < n && (P.left == kNoWindow || first < P.sinks || last >= n - P.left);
+  return !keep && e >= 0 && e < P.pages;
+}
+
+// counts[b]: pages of row b that go back; counts[B]: the free pages before
+__global__ __launch_bounds__(256) void release_count_kernel(const PagesProb P, int32_t* counts) {
+  __shared__ int64_t sums[4];
+  const int b = blockIdx.x, n = P.len(b);
+  int64_t c = 0, total;
+  for (int i = threadIdx.x; i < P.max_pages; i += 256)
+    c += goes_back(P, n, i, P.table[b * P.table_sb + i]);
+  scan_before<4, int64_t>(c, sums, &total);
+  if (threadIdx.x == 0) {
+    counts[b] = (int32_t)total;
+    if (b == 0) counts[P.B] = min(max(P.state[0], 0), P.pages);
+  }
+}
+
+__global__ __launch_bounds__(256) void release_kernel(const PagesProb P,
+                                                      const int32_t* __restrict__ counts) {
+  __shared__ int64_t sums[4];
+  __shared__ int32_t each[4];
+  const int b = blockIdx.x, n = P.len(b), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int mine = counts[b], n_free = counts[P.B];
+  if (mine == 0 && b != 0) return;
+  // pages of the rows from this one on; the stack ends with row 0's first
+  int64_t after = 0, total;
+  for (int x = b + tid; x < P.B; x += 256) after += counts[x];
+  scan_before<4, int64_t>(after, sums, &total);
+  if (b == 0 && tid == 0) P.state[0] = (int32_t)min((int64_t)n_free + total, (int64_t)P.pages);
+  int64_t top = n_free + total - 1;  // place of the row's next page
+  for (int i0 = 0; i0 < P.max_pages; i0 += 256) {
+    const int i = i0 + tid;
+    int e = -1;
+    if (i < P.max_pages) e = P.table[b * P.table_sb + i];
+    const bool back = i < P.max_pages && goes_back(P, n, i, e);
+    const uint64_t who = __ballot(back);
+    if (lane == 0) each[w] = __popcll(who);
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (x < w) before += each[x];
+      all += each[x];
+    }
+    if (back) {
+      const int64_t at = top - before - __popcll(who & ((1ull << lane) - 1));
+      if (at >= 0 && at < P.pages) P.free[at] = e;
+      P.table[b * P.table_sb + i] = -1;
+    }
+    top -= all;
+    __syncthreads();
+  }
+}
+
+template <typename T>
+struct Piece {  // 16 bytes
+  T x[16 / sizeof(T)];
+};
+
+// One thread per 16 bytes of a head, keys and values
+template <typename T>
+__global__ __launch_bounds__(256) void write_kernel(const WriteProb P, const T* __restrict__ k,
+                                                    const T* __restrict__ v, T* __restrict__ kp,
+                                                    T* __restrict__ vp, int pieces) {
+  constexpr int N = 16 / sizeof(T);
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c = (int)(id % pieces);
+  const int64_t row = id / pieces;
+  const int h = (int)(row % P.Hk);
+  const int64_t t = row / P.Hk;
+  if (t >= P.tokens) return;
+  const int64_t slot = P.slots[t];
+  if (slot < 0 || slot >= (int64_t)P.pages * P.page) return;
+  const int64_t pg = slot / P.page, in = slot - pg * P.page;
+  *(Piece<T>*)(kp + pg * P.k_sp + in * P.k_st + h * P.k_sh + N * c) =
+      *(const Piece<T>*)(k + t * P.kn_st + h * P.kn_sh + N * c);
+  *(Piece<T>*)(vp + pg * P.v_sp + in * P.v_st + h * P.v_sh + N * c) =
+      *(const Piece<T>*)(v + t * P.vn_st + h * P.vn_sh + N * c);
+}
+
+}  // namespace
+
+hipError_t launch_grow(const PagesProb& P, const int32_t* n_new, int32_t* starts, int64_t* slots,
+                       int32_t* positions, hipStream_t st) {
+  if (P.tokens <= 2 * kGrow) {
+    hipLaunchKernelGGL((grow_kernel<true>), dim3(1), dim3(kGrow), 0, st, P, n_new, starts, slots,
+                       positions);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((grow_kernel<false>), dim3(1), dim3(kGrow), 0, st, P, n_new, starts, slots,
+                     positions);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(slots_kernel, dim3((P.tokens + 255) / 256), dim3(256), 0, st, P, n_new, starts,
+                     slots, positions);
+  return hipGetLastError();
+}
+
+size_t release_bytes(const PagesProb& P) { return ((size_t)(P.B + 1) * 4 + 255) & ~(size_t)255; }
+
+hipError_t launch_release(const PagesProb& P, char* ws, hipStream_t st) {
+  int32_t* counts = (int32_t*)ws;
+  hipLaunchKernelGGL(release_count_kernel, dim3(P.B), dim3(256), 0, st, P, counts);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(release_kernel, dim3(P.B), dim3(256), 0, st, P, counts);
+  return hipGetLastError();
+}
+
+hipError_t launch_write(const WriteProb& P, const void* k, const void* v, void* kp, void* vp,
+                        hipStream_t st) {
+  const int pieces = P.d / (P.dtype == CA_BF16 ? 8 : 4);
+  const int64_t threads = (int64_t)P.tokens * P.Hk * pieces;
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  if (P.dtype == CA_BF16)
+    hipLaunchKernelGGL((write_kernel<bf16>), grid, dim3(256), 0, st, P, (const bf16*)k,
+                       (const bf16*)v, (bf16*)kp, (bf16*)vp, pieces);
+  else
+    hipLaunchKernelGGL((write_kernel<float>), grid, dim3(256), 0, st, P, (const float*)k,
+                       (const float*)v, (float*)kp, (float*)vp, pieces);
+  return hipGetLastError();
+}
+
+}  // namespace ca

@@ -146,6 +146,53 @@ size_t paged_bytes(const PagedProb& P);
 hipError_t launch_paged(const PagedProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st);
 
+// ---- chunks of new tokens over the paged cache --------------------------------------------
+
+struct PagesProb {
+  int B, page, pages, max_pages, tokens;
+  int left, sinks;  // left: kNoWindow without a window
+  int64_t table_sb;
+  const int32_t* lens;
+  int32_t *table, *free, *state;
+
+  __device__ __forceinline__ int len(int b) const {
+    return (int)min((int64_t)max(lens[b], 0), (int64_t)max_pages * page);
+  }
+};
+
+hipError_t launch_grow(const PagesProb& P, const int32_t* n_new, int32_t* starts, int64_t* slots,
+                       int32_t* positions, hipStream_t st);
+size_t release_bytes(const PagesProb& P);
+hipError_t launch_release(const PagesProb& P, char* ws, hipStream_t st);
+
+struct ChunkProb {
+  int B, H, Hk, G, d, dtype, page, pages, max_pages, tokens;
+  WinMask m;  // unlimited sides: kNoWindow - 1 (caches hold fewer tokens; position + side fits)
+  float scale;
+  const int32_t *table, *lens, *starts;
+  int64_t table_sb;
+  int64_t q_st, q_sh, o_st, o_sh;              // token, head
+  int64_t k_sp, k_st, k_sh, v_sp, v_st, v_sh;  // page, token, head
+
+  __device__ __forceinline__ int klen(int b) const {
+    return (int)min((int64_t)max(lens[b], 0), (int64_t)max_pages * page);
+  }
+  __device__ __forceinline__ int start(int b) const { return min(max(starts[b], 0), tokens); }
+};
+
+struct WriteProb {
+  int Hk, d, dtype, page, pages, tokens;
+  const int64_t* slots;
+  int64_t kn_st, kn_sh, vn_st, vn_sh;          // new rows: token, head
+  int64_t k_sp, k_st, k_sh, v_sp, v_st, v_sh;  // pools: page, token, head
+};
+
+hipError_t launch_write(const WriteProb& P, const void* k, const void* v, void* kp, void* vp,
+                        hipStream_t st);
+size_t chunk_bytes(const ChunkProb& P);
+hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
+                        float* lse, char* ws, hipStream_t st);
+
 // ---- elements ------------------------------------------------------------------------------
 
 // four consecutive elements in fp32

@@ -1,11 +1,13 @@
 """The sequence operators of libclusterattn: rotary positions of several axes,
 attention with a sliding window and sinks and its gradients, and the paged
-key-value cache with the attention of one new token (see
+key-value cache with the attention of one new token or of chunks of them (see
 include/clusterattn.h for their definitions).
 
     rope                              turn queries and keys by their positions
     window_attn, window_attn_backward
     cache_append, paged_attn          serving: write new tokens, attend over the pages
+    cache_grow, cache_release         pages for the new tokens of a step, and back
+    cache_write, paged_chunk_attn     packed new tokens: write them by slots, attend
 
 As in the rest of the binding, every step runs in the HIP library: these
 functions read shapes and strides, allocate outputs and workspaces with torch
@@ -21,6 +23,7 @@ import ctypes
 import functools
 import warnings
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -28,7 +31,8 @@ from . import _lib
 from ._lib import CA_BF16, CA_F32
 
 __all__ = ["Rope", "rope_axes", "rope", "Window", "window_attn", "window_attn_backward",
-           "cache_append", "paged_attn"]
+           "cache_append", "paged_attn", "PagePool", "page_pool", "CacheStep", "cache_grow",
+           "cache_release", "cache_write", "paged_chunk_attn"]
 
 _DT = {torch.float32: CA_F32, torch.bfloat16: CA_BF16}
 _I64x3 = ctypes.c_int64 * 3
@@ -476,3 +480,209 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     if out is not None:
         _wrote(out)
     return o, lse
+
+
+# ---- chunks of new tokens over the paged cache -------------------------------------------
+
+@dataclass(frozen=True)
+class PagePool:
+    """The pages of `page` tokens that no sequence holds: free, int32 [pages],
+    of which the first state[0] are free pages (a stack, the next one to be taken
+    last); state, int32 [3]: free pages, pages that the last cache_grow lacked, new
+    tokens for which it had no rows. page_pool makes one of a whole pool."""
+    page: int
+    free: torch.Tensor
+    state: torch.Tensor
+
+    def __post_init__(self):
+        object.__setattr__(self, "page", int(self.page))
+
+    @property
+    def pages(self):
+        return self.free.shape[0]
+
+
+def page_pool(pages, page, device="cuda") -> PagePool:
+    """A PagePool of `pages` pages, all free; page 0 is taken first."""
+    pages = _int(pages, "pages", 1)
+    return PagePool(_int(page, "page", 1),
+                    torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device),
+                    torch.tensor([pages, 0, 0], dtype=torch.int32, device=device))
+
+
+class CacheStep(NamedTuple):
+    """Where a step's new tokens lie, packed: sequence b's in rows starts[b] ..
+    starts[b + 1] - 1. starts: int32 [B + 1]; slots: int64 [tokens], places in the
+    pools (-1: none); positions: int32 [1, tokens], places in the sequences, as
+    rope takes them."""
+    starts: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+
+
+@_kept
+def _pages(page, free, state, table, lens, new, tokens, left, sinks, out):
+    """(descriptor, bytes of workspace) of a cache_grow (new given) or a
+    cache_release."""
+    if len(free[0]) != 1 or free[1][0] != 1:
+        raise ValueError("pool.free: expected a contiguous [pages]")
+    _int32(free, "pool.free", free[0])
+    _int32(state, "pool.state", (3,))
+    if len(table[0]) != 2:
+        raise ValueError("page_table: expected [B, max_pages]")
+    batch, width = table[0]
+    _int32(table, "page_table", (batch, width))
+    _int32(lens, "lens", (batch,))
+    if state[1][0] != 1 or (table[1][1] != 1 and width > 1) or (lens[1][0] != 1 and batch > 1):
+        raise ValueError("pool.state, lens and the rows of page_table must be contiguous")
+    if new is not None:
+        _int32(new, "new", (batch,))
+        if new[1][0] != 1 and batch > 1:
+            raise ValueError("new must be contiguous")
+        if out is not None:
+            starts, slots, positions = out
+            _int32(starts, "out.starts", (batch + 1,))
+            _int32(positions, "out.positions", (1, tokens))
+            if slots[2] != torch.int64 or tuple(slots[0]) != (tokens,):
+                raise ValueError(f"out.slots: expected int64 [{tokens}]")
+            if starts[1][0] != 1 or (tokens > 1 and (slots[1][0] != 1 or positions[1][1] != 1)):
+                raise ValueError("out: expected contiguous tensors")
+    c = _lib.CaPages(batch, _int(page, "page"), free[0][0], width, tokens, _side(left),
+                     _int(min(sinks, _MOST), "sinks"), table[1][0] if batch > 1 else 0)
+    return c, _bytes("ca_cache_release_workspace_size", c) if new is None else 0
+
+
+def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, out=None) -> CacheStep:
+    """Pages for the new tokens of a step, and where they go. page_table: int32
+    [B, max_pages], changed in place; lens: int32 [B], the sequences' tokens, the
+    new ones, the last new[b] of them (int32 [B]), included; tokens: rows of the
+    packed arrays, at least the sum of `new` (the program knows it, or a bound for
+    arrays of a fixed size). Entries that a new token lies on and that hold no page
+    (-1, or any value outside the pool) get one; where the pool runs short they
+    stay, their tokens have slot -1, and pool.state[1] says how many pages
+    lacked. Repeating the call changes nothing. Returns CacheStep, in `out` (one
+    of an earlier call of the same sizes) if given; rows behind the last sequence
+    have slot -1 and position 0."""
+    tokens = _int(tokens, "tokens", 1)
+    _on_ints(pool.free, pool.state, page_table, lens, new, *(out or ()))
+    c, _ = _pages(pool.page, _geo(pool.free), _geo(pool.state), _geo(page_table), _geo(lens), _geo(new),
+                  tokens, -1, 0, None if out is None else tuple(_geo(t) for t in out))
+    if out is None:
+        out = CacheStep(lens.new_empty(lens.shape[0] + 1), lens.new_empty(tokens, dtype=torch.int64),
+                        lens.new_empty((1, tokens)))
+    starts, slots, positions = out
+    _call("ca_cache_grow", lens.device, c, lens.data_ptr(), new.data_ptr(), page_table.data_ptr(),
+          pool.free.data_ptr(), pool.state.data_ptr(), starts.data_ptr(), slots.data_ptr(),
+          positions.data_ptr())
+    _wrote(page_table, pool.state, starts, slots, positions)
+    return CacheStep(starts, slots, positions)
+
+
+def cache_release(pool: PagePool, page_table, lens, *, left=-1, sinks=0, ws=None):
+    """Gives the pages back that hold none of a sequence's lens[b] tokens, or with
+    left >= 0 none that its next token sees with that window (the last `left` and
+    the first `sinks`): all of a finished sequence (lens 0), those of
+    rejected tokens (lens less than it was), those behind a window. Their entries
+    become -1. page_table: int32 [B, max_pages], changed in place. A page that
+    several rows share must not go back from two of them. Returns nothing."""
+    _on_ints(pool.free, pool.state, page_table, lens)
+    c, nbytes = _pages(pool.page, _geo(pool.free), _geo(pool.state), _geo(page_table), _geo(lens), None,
+                       0, int(left), int(sinks), None)
+    ws = _workspace(nbytes, lens, ws)
+    _call("ca_cache_release", lens.device, c, lens.data_ptr(), page_table.data_ptr(),
+          pool.free.data_ptr(), pool.state.data_ptr(), _ptr(ws), 0 if ws is None else ws.nbytes)
+    _wrote(page_table, pool.free, pool.state)
+
+
+def _on_ints(like, *tensors):
+    """All on one GPU."""
+    if not like.is_cuda:
+        raise ValueError("expected tensors on the GPU")
+    i = like.get_device()
+    for t in tensors:
+        if t.get_device() != i:
+            raise ValueError(f"expected all tensors on {like.device}, got one on {t.device}")
+
+
+@_kept
+def _chunk(k_pages, v_pages, w, table, lens, starts, q, out, scale, k, v, slots):
+    """(descriptor, bytes of workspace) of a cache_write (k, v and slots given) or an
+    attention (w, table, lens, starts and q given)."""
+    dtype = k_pages[2]
+    dt = _dtype(dtype)
+    (P, page, Hk, d), ks = _rows(k_pages, "k_pages", 4, dtype)
+    vs = _rows(v_pages, "v_pages", 4, dtype, k_pages[0])[1]
+    ks, vs, z = _I64x3(*ks[:3]), _I64x3(*vs[:3]), _I64x2()
+    if k is not None:
+        (T, h, x), kn = _rows(k, "k", 3, dtype)
+        if (h, x) != (Hk, d):
+            raise ValueError(f"k: expected shape [T, {Hk}, {d}], got {[T, h, x]}")
+        vn = _rows(v, "v", 3, dtype, k[0])[1]
+        if slots[2] != torch.int64 or tuple(slots[0]) != (T,) or (slots[1][0] != 1 and T > 1):
+            raise ValueError(f"slots: expected a contiguous int64 tensor of [{T}]")
+        return _lib.CaChunk(1, Hk, Hk, d, dt, page, P, 1, T, -1, -1, 0, 0, 0.0, 0, ks, vs, z, z,
+                            _I64x2(*kn[:2]), _I64x2(*vn[:2])), 0
+    (T, H, x), qs = _rows(q, "q", 3, dtype)
+    if x != d:
+        raise ValueError(f"q: expected a last dimension of {d}, got {x}")
+    os = _rows(out or _dense(q), "out", 3, dtype, q[0])[1]
+    if len(table[0]) != 2:
+        raise ValueError("page_table: expected [B, max_pages]")
+    B, width = table[0]
+    _int32(table, "page_table", (B, width))
+    _int32(lens, "lens", (B,))
+    _int32(starts, "starts", (B + 1,))
+    if (table[1][1] != 1 and width > 1) or (lens[1][0] != 1 and B > 1) or starts[1][0] != 1:
+        raise ValueError("lens, starts and the rows of page_table must be contiguous")
+    c = _lib.CaChunk(B, H, Hk, d, dt, page, P, width, T, _side(w.left), _side(w.right),
+                     _int(min(w.sinks, _MOST), "sinks"), int(w.causal), 0.0 if scale is None else scale,
+                     table[1][0] if B > 1 else 0, ks, vs, _I64x2(*qs[:2]), _I64x2(*os[:2]), z, z)
+    return c, _bytes("ca_paged_chunk_workspace_size", c)
+
+
+def cache_write(k, v, k_pages, v_pages, slots):
+    """Writes the packed new keys and values k, v [T,Hk,d] (any strides) to their
+    slots (int64 [T], as cache_grow gives them: page * its index + place in the
+    page); rows with a slot outside the pools are left out. k_pages, v_pages:
+    [pages, page, Hk, d], any strides. Returns nothing. Not recorded by autograd."""
+    if torch.is_grad_enabled():
+        _unrecorded((k, v), (k_pages, v_pages))
+    _on(k, v, k_pages, v_pages, slots)
+    c, _ = _chunk(_geo(k_pages), _geo(v_pages), None, None, None, None, None, None, None, _geo(k), _geo(v),
+                  _geo(slots))
+    _call("ca_cache_write", k.device, c, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(),
+          v_pages.data_ptr(), slots.data_ptr())
+    _wrote(k_pages, v_pages)
+
+
+def paged_chunk_attn(w: Window, q, k_pages, v_pages, page_table, lens, starts, *, scale=None,
+                     want_lse=False, out=None, lse=None, ws=None):
+    """Attention of the new tokens of each sequence, any number of them, over the
+    sequence's cached keys, the new tokens' own (written before) included. q:
+    [T,H,d] packed, any strides, rows starts[b] .. starts[b + 1] - 1 those of the
+    last tokens of sequence b (starts: int32 [B + 1]); lens: int32 [B], all tokens of
+    the sequences; k_pages, v_pages: [pages, page, Hk, d], any strides, Hk a
+    divisor of H; page_table: int32 [B, max_pages]. Who sees whom is w, as in
+    window_attn: Window(causal=True) for text, Window() where the new tokens see each
+    other. Returns (out [T,H,d], lse [T,H] fp32 or None); a query that sees no key has
+    0 and -inf. Rows behind the last sequence are left as they were (in new
+    tensors: as they come). Not recorded by autograd, and without a backward pass."""
+    if torch.is_grad_enabled():
+        _unrecorded((q, k_pages, v_pages), (out, lse))
+    _on(q, k_pages, v_pages, page_table, lens, starts, out, lse)
+    if q.dim() != 3:
+        raise ValueError("q: expected [T, H, d]")
+    c, nbytes = _chunk(_geo(k_pages), _geo(v_pages), w, _geo(page_table), _geo(lens), _geo(starts), _geo(q),
+                       None if out is None else _geo(out), _scale(scale), None, None, None)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or
+                            not lse.is_contiguous()):
+        raise ValueError(f"lse: expected a contiguous fp32 tensor of {list(q.shape[:2])}")
+    o = _new(q) if out is None else out
+    z = q.new_empty(q.shape[:2], dtype=torch.float32) if lse is None and want_lse else lse
+    ws = _workspace(nbytes, q, ws)
+    _call("ca_paged_chunk_attn", q.device, c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+          page_table.data_ptr(), lens.data_ptr(), starts.data_ptr(), o.data_ptr(), _ptr(z), _ptr(ws),
+          0 if ws is None else ws.nbytes)
+    if out is not None or lse is not None:
+        _wrote(out, lse)
+    return o, z
