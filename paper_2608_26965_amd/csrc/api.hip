@@ -413,6 +413,7 @@ int check_chunk(const ca_chunk* p, ca::ChunkProb* P) {
   P->v_sp = p->v_stride[0];
   P->v_st = p->v_stride[1];
   P->v_sh = p->v_stride[2];
+  if (!ca::chunk_fits(*P)) return fail(CA_E_UNSUPPORTED, "tokens * heads too large");
   return CA_OK;
 }
 

@@ -1,18 +1,497 @@
 // Attention of packed chunks of new tokens over a paged key-value cache.
 //
-// One workgroup per (token, head). Its wavefronts take every fourth group of 64
-// keys, a lane a key: the logits of a group, an online softmax, and the value
-// product with a lane for one or two dims. The wavefronts' states are joined
-// through LDS.
+// All query heads of a key head share its keys, so a sequence's rows are its new
+// tokens times the G heads of the group (row r: token r / G, head r % G), taken
+// in blocks; a block walks the 64-key tiles that one of its rows sees. Blocks
+// have very different lengths (a prompt's beside a single token's on a long cache),
+// so a first launch plans them: it counts all tiles and cuts long blocks into parts of
+// about what a workgroup's share is. The parts' softmax states are joined by a
+// last launch. The plan is the same for all key heads.
+//
+// What bounds it: the matrix cores for prompts, the cache (read once by each block)
+// for few new tokens.
 #include <math.h>
 
 #include "seq.h"
+#include "walk_bf16.h"
 
 namespace ca {
 
 namespace {
 
-// The sequence whose new tokens hold packed row t; -1 if none does
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kPlan = 1024;    // threads of the planning workgroup
+constexpr int kPartTiles = 8;  // tiles of a part, at least
+constexpr int kF32Rows = 64;   // rows of a block, fp32
+
+// A workgroup's work, for every key head: tiles [t0, t1) of block a of sequence b (with
+// its lengths and first row). slot: where a part's state goes, -1 for a whole block.
+struct Item {
+  int b, a, t0, t1, slot, lq, lk, start;
+};
+// A block that is cut: its parts' states lie in slots slot .. slot + n - 1
+struct Cut {
+  int a, slot, n, lq, lk, start;
+};
+struct PlanHead {
+  int items, cuts;
+};
+
+// Bounds that the host knows, and where things lie in the workspace
+struct Plan {
+  int rows;                           // of a block
+  int blocks, share, items, slots;    // at most, for one key head; share: parts that blocks
+                                      // are cut for
+  int cuts;
+  size_t item_at, cut_at, part_at, bytes;
+};
+
+__device__ __forceinline__ int blocks_of(const ChunkProb& P, int rows, int b) {
+  const int64_t r = (int64_t)max(0, P.start(b + 1) - P.start(b)) * P.G;
+  return (int)((r + rows - 1) / rows);
+}
+
+// Positions of a block's first and last row, and its tiles
+struct BlockSpan {
+  int p0, p1, real;
+  __device__ __forceinline__ BlockSpan(int a, int rows, int G, int lq, int lk) {
+    const int64_t all = (int64_t)lq * G, r0 = (int64_t)a * rows;
+    real = (int)min((int64_t)rows, all - r0);
+    p0 = (int)(r0 / G) + lk - lq;
+    p1 = (int)((r0 + real - 1) / G) + lk - lq;
+  }
+};
+
+// Sum of x over the threads before this one, and over all of them
+__device__ __forceinline__ int64_t plan_scan(int64_t x, int64_t (&sums)[kPlan / 64],
+                                             int64_t* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int64_t in = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(in, o, 64);
+    if (lane >= o) in += y;
+  }
+  __syncthreads();  // the sums of a scan before are read
+  if (lane == 63) sums[w] = in;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kPlan / 64; ++i) {
+    if (i < w) before += sums[i];
+    all += sums[i];
+  }
+  *total = all;
+  return before + in - x;
+}
+
+// One workgroup: blocks by sequence, the last one (with most keys, if causal) first.
+__global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, const Plan L,
+                                                           char* ws) {
+  __shared__ int64_t sums[kPlan / 64];
+  __shared__ int first[kPlan + 1], s_lq[kPlan], s_lk[kPlan], s_start[kPlan];
+  PlanHead* head = (PlanHead*)ws;
+  Item* items = (Item*)(ws + L.item_at);
+  Cut* cuts = (Cut*)(ws + L.cut_at);
+  const int tid = threadIdx.x;
+  int64_t all_tiles = 0, n_items = 0, n_slots = 0, n_cuts = 0;
+  int part = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t seen = 0;  // blocks so far: no more than the host counted
+    for (int b0 = 0; b0 < P.B && seen < L.blocks; b0 += kPlan) {
+      const int b = b0 + tid;
+      int n = 0;
+      if (b < P.B) {
+        n = blocks_of(P, L.rows, b);
+        s_start[tid] = P.start(b);
+        s_lq[tid] = max(0, P.start(b + 1) - P.start(b));
+        s_lk[tid] = P.klen(b);
+      }
+      int64_t total;
+      const int64_t before = plan_scan(n, sums, &total);
+      total = min(total, (int64_t)L.blocks - seen);
+      first[tid] = (int)min(before, total);
+      if (tid == 0) first[kPlan] = (int)total;
+      __syncthreads();
+      for (int64_t i0 = 0; i0 < total; i0 += kPlan) {
+        const int i = (int)i0 + tid;
+        int64_t tiles = 0, parts = 0;
+        int lo = 0, a = 0;
+        if (i < total) {
+          int hi = kPlan;  // first[lo] <= i < first[hi]
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= i)
+              lo = mid;
+            else
+              hi = mid;
+          }
+          a = blocks_of(P, L.rows, b0 + lo) - 1 - (i - first[lo]);
+          const BlockSpan s(a, L.rows, P.G, s_lq[lo], s_lk[lo]);
+          tiles = visible_tiles<KT>(P.m, s.p0, s.p1, s_lk[lo]).n;
+          parts = 1;
+          if (pass == 1 && tiles > part) parts = (tiles + part - 1) / part;
+        }
+        int64_t sum;
+        if (pass == 0) {
+          plan_scan(tiles, sums, &sum);
+          all_tiles += sum;
+          continue;
+        }
+        int64_t n_cut;
+        const int64_t cut = plan_scan(parts > 1 ? 1 : 0, sums, &n_cut);
+        const int64_t slot = n_slots + plan_scan(parts > 1 ? parts : 0, sums, &sum);
+        n_slots += sum;
+        const int64_t item = n_items + plan_scan(parts, sums, &sum);
+        n_items += sum;
+        // (the host's bounds hold for ascending starts; nothing is written outside them)
+        const bool whole = parts == 1;
+        if (i < total && item + parts <= L.items &&
+            (whole || (slot + parts <= L.slots && n_cuts + cut < L.cuts))) {
+          if (!whole)
+            cuts[n_cuts + cut] = Cut{a, (int)slot, (int)parts, s_lq[lo], s_lk[lo], s_start[lo]};
+          const int per = (int)((tiles + parts - 1) / parts);
+          for (int x = 0; x < parts; ++x) {
+            const int t0 = min((int)tiles, x * per), t1 = min((int)tiles, t0 + per);
+            items[item + x] = Item{b0 + lo, a, t0, t1, whole ? -1 : (int)slot + x,
+                                   s_lq[lo], s_lk[lo], s_start[lo]};
+          }
+        }
+        n_cuts += n_cut;
+      }
+      seen += total;
+      __syncthreads();  // the segment's lists are read
+    }
+    part = (int)max((int64_t)kPartTiles, (all_tiles + L.share - 1) / L.share);
+  }
+  if (tid == 0) {
+    head->items = (int)min(n_items, (int64_t)L.items);
+    head->cuts = (int)min(n_cuts, (int64_t)L.cuts);
+  }
+}
+
+// Workgroup w of the grid runs on XCD w % 8. The key heads are spread over the XCDs,
+// each of which then works on one head at a time, whose keys stay in its L2; where
+// the heads' number and 8 have g as their greatest common divisor, 8 / g XCDs share a
+// head, neighbouring items on different ones.
+struct ItemOrder {
+  int g, slots;  // slots: heads of an XCD
+  static ItemOrder of(int Hk) {
+    int g = 8;
+    while (Hk % g) g /= 2;
+    return ItemOrder{g, Hk / g};
+  }
+  int64_t grid(int items) const { return (int64_t)8 * slots * ((items + 8 / g - 1) / (8 / g)); }
+  __device__ __forceinline__ bool at(int wg, int items, int* item, int* hk) const {
+    const int r = 8 / g, x = wg & 7, s = wg >> 3, per = (items + r - 1) / r;
+    if (per == 0) return false;
+    const int hs = s / per;
+    *item = (s - hs * per) * r + x / g;
+    *hk = hs * g + x % g;
+    return hs < slots && *item < items;
+  }
+};
+
+// ---- bf16 ---------------------------------------------------------------------------------
+
+// n / d for 0 <= n < 2^30, d < 2^30
+struct FastDiv {
+  uint32_t m;
+  int s;
+  static FastDiv of(int d) {
+    int k = 0;
+    while ((1 << k) < d) ++k;
+    return FastDiv{(uint32_t)(((uint64_t)1 << (30 + k)) / (uint32_t)d + 1), 30 + k};
+  }
+  __host__ __device__ __forceinline__ int div(int n) const {
+    return (int)(((uint64_t)(uint32_t)n * m) >> s);
+  }
+};
+
+__device__ __forceinline__ void lds_dma16_at(const void* p, uint32_t lds) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(p), "s"(lds)
+      : "memory");
+}
+
+// Tiles whose rows lie on pages. Wavefront w copies rows 16 w .. 16 w + 15 of a
+// tile. GROUPS: pages of a multiple of 16 tokens, so that the sixteen lie on one page,
+// whose entry is one scalar load (from the constant address space: no kernel writes the
+// table while this one runs); else a lane looks up its row's entry. Entries are
+// loaded a tile before the copies that need them.
+template <int D, bool GROUPS>
+struct PagedTiles : WalkRows {
+  static constexpr bool kHoles = true;
+  static constexpr float kMostSum = 0x1p30f;
+  static constexpr int RB = 2 * D, TILE = KT * RB, NI = RB / 64, RPI = 1024 / RB;
+  typedef const __attribute__((address_space(4))) int32_t* Entries;
+  const bf16 *kh, *vh;  // of this key head
+  const int32_t* table;
+  int64_t k_sp, k_st, v_sp, v_st;
+  int page, pages, most;  // most: last entry of the row
+  FastDiv by_page;
+  char* smem;
+  uint16_t (*hole)[4];
+  uint32_t lds0;
+  int w, lane;
+  int ev, ek;  // entries of the tile whose values, and of the one whose keys are next
+
+  __device__ __forceinline__ int key(int t) const {
+    return KT * tile(t) + 16 * w + (GROUPS ? 0 : lane & 15);
+  }
+  __device__ __forceinline__ int entry(int t) const {
+    const int e = min(by_page.div(min(key(t), lk - 1)), most);
+    if constexpr (GROUPS)
+      return ((Entries)table)[__builtin_amdgcn_readfirstlane(e)];
+    else
+      return table[e];
+  }
+  // keys (V false) or values of tile t, entry e, into LDS tile `at`
+  template <bool V>
+  __device__ __forceinline__ void copy(int t, int e, int at, int buf) const {
+    const bf16* base = V ? vh : kh;
+    const int64_t sp = V ? v_sp : k_sp, st = V ? v_st : k_st;
+    const uint32_t dst = lds0 + at * TILE + 1024 * NI * w;
+    const int row = lane / (RB / 16), j = key(t);
+    auto chunk = [&](int c) __attribute__((always_inline)) {
+      return ((lane % (RB / 16)) ^ row_key<RB>(RPI * c + row)) << 4;
+    };
+    auto nothing = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < NI; ++c)
+        *(f32x4*)(smem + at * TILE + 1024 * (NI * w + c) + 16 * lane) = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    if constexpr (GROUPS) {
+      const bool there = e >= 0 && e < pages;
+      const int last = lk - 1 - j;  // of the group's rows
+      if (!V && lane == 0) hole[buf][w] = there || last < 0 ? 0 : 0xffff;
+      if (!there || last < 0) {
+        nothing();
+        return;
+      }
+      const int in = j - by_page.div(j) * page;
+      const char* src = (const char*)(base + e * sp + in * st);
+      const uint32_t rb = (uint32_t)st * 2;
+      if (last >= 15) {
+#pragma unroll
+        for (int c = 0; c < NI; ++c)
+          lds_dma16(src + (int64_t)(RPI * c) * rb, (uint32_t)row * rb + chunk(c),
+                    __builtin_amdgcn_readfirstlane(dst + 1024 * c));
+      } else {  // rows past the last are copies of it
+#pragma unroll
+        for (int c = 0; c < NI; ++c)
+          lds_dma16(src, (uint32_t)min(RPI * c + row, last) * rb + chunk(c),
+                    __builtin_amdgcn_readfirstlane(dst + 1024 * c));
+      }
+    } else {
+      const bool there = e >= 0 && e < pages;
+      const uint32_t any = (uint32_t)__builtin_amdgcn_ballot_w64(there) & 0xffff;
+      const uint32_t gone = (uint32_t)__builtin_amdgcn_ballot_w64(!there && j < lk) & 0xffff;
+      if (!V && lane == 0) hole[buf][w] = (uint16_t)gone;
+      if (any == 0) {
+        nothing();
+        return;
+      }
+      const int n = min(j, lk - 1), in = n - by_page.div(n) * page;
+      int64_t o = there ? e * sp + in * st : 0;
+      // rows that are not there: copies of one that is
+      const int64_t o1 = __shfl(o, __builtin_ctz(any), 64);
+      o = there ? o : o1;
+#pragma unroll
+      for (int c = 0; c < NI; ++c)
+        lds_dma16_at((const char*)(base + __shfl(o, RPI * c + row, 64)) + chunk(c),
+                     __builtin_amdgcn_readfirstlane(dst + 1024 * c));
+    }
+  }
+  __device__ __forceinline__ void issue_k(int t, int buf) { copy<false>(t, ek, buf, buf); }
+  __device__ __forceinline__ void issue_v(int t, int buf) {
+    copy<true>(t, ev, 2 + buf, buf);
+    ev = ek;
+    ek = entry(min(t + 2, t1 - 1));
+  }
+  __device__ __forceinline__ void first_k() {
+    ev = entry(t0);
+    copy<false>(t0, ev, 0, 0);
+    ek = entry(min(t0 + 1, t1 - 1));
+  }
+  __device__ __forceinline__ void issue_both(int t) const {
+    const int e = entry(t);
+    copy<false>(t, e, 0, 0);
+    copy<true>(t, e, 2, 0);
+  }
+  __device__ __forceinline__ uint64_t holes(int buf) const {
+    uint2 x;
+    __builtin_memcpy(&x, hole[buf], 8);
+    return (uint64_t)__builtin_amdgcn_readfirstlane(x.y) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane(x.x);
+  }
+};
+
+template <int D, bool GROUPS>
+__global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
+    const ChunkProb P, const Plan L, const ItemOrder order, const FastDiv by_page,
+    const bf16* __restrict__ q, const bf16* __restrict__ kp, const bf16* __restrict__ vp,
+    bf16* __restrict__ out, float* __restrict__ lse, char* __restrict__ ws, float sl2) {
+  constexpr int KS = D / 16, DT = D / 32, RB = 2 * D, TILE = KT * RB;
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // two tiles of keys, two of values
+  __shared__ __attribute__((aligned(8))) uint16_t hole[2][4];
+  __shared__ int redo;
+  int item, hk;
+  if (!order.at(blockIdx.x, ((const PlanHead*)ws)->items, &item, &hk)) return;
+  const Item it = ((const Item*)(ws + L.item_at))[item];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int off = it.lk - it.lq, r0 = it.a * kWalkRows, rows = it.lq * P.G;
+  const BlockSpan span(it.a, kWalkRows, P.G, it.lq, it.lk);
+  const int w0 = r0 + 32 * w, wreal = max(0, min(32, rows - w0));
+  const int row = min(w0 + min(l32, max(wreal, 1) - 1), rows - 1);  // this lane's row
+  const int tok = row / P.G, head = hk * P.G + row - tok * P.G;
+  const int wl = min(w0 + max(wreal, 1) - 1, rows - 1);
+  PagedTiles<D, GROUPS> T;
+  T.mask = P.m;
+  T.list = visible_tiles<KT>(P.m, span.p0, span.p1, it.lk);
+  T.t0 = it.t0;
+  T.t1 = it.t1;
+  T.lk = it.lk;
+  T.ra = visible_keys(P.m, min(w0, rows - 1) / P.G + off, it.lk);
+  T.rz = visible_keys(P.m, wl / P.G + off, it.lk);
+  T.pos = tok + off;
+  T.real = wreal;
+  T.block_first = span.p0;
+  T.block_last = span.p1;
+  T.kh = kp + hk * P.k_sh;
+  T.vh = vp + hk * P.v_sh;
+  T.table = P.table + it.b * P.table_sb;
+  T.k_sp = P.k_sp;
+  T.k_st = P.k_st;
+  T.v_sp = P.v_sp;
+  T.v_st = P.v_st;
+  T.page = P.page;
+  T.pages = P.pages;
+  T.most = P.max_pages - 1;
+  T.by_page = by_page;
+  T.smem = smem;
+  T.hole = hole;
+  T.lds0 = lds_addr(smem);
+  T.w = w;
+  T.lane = lane;
+  T.ev = T.ek = 0;
+
+  bf16x8 qreg[KS];
+  {
+    const bf16* src = q + (it.start + tok) * P.q_st + head * P.q_sh;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qreg[kk] = *(const bf16x8*)(src + 16 * kk + 8 * h);
+  }
+  // Retire the loads here (a wait the compiler sees), so that no vmcnt wait of
+  // theirs lands in the loop, where it would also wait for the copies in flight.
+  __builtin_amdgcn_s_waitcnt(kWalkVmcnt0);
+  if (tid == 0) redo = 0;  // ordered before any write by the barriers of the tiles
+  f32x16 oacc[DT];
+  float m, l_tot;
+  walk_bf16<D>(T, smem, &redo, qreg, sl2, w, lane, oacc, m, l_tot);
+  if (it.slot >= 0) {
+    // A sum far above its reference goes out against a reference at its own size: the
+    // joining compares references, and adds up as many sums as there are parts
+    const int up = l_tot > 0x1p22f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
+    m += (float)up;
+    l_tot = __builtin_amdgcn_ldexpf(l_tot, -up);
+    if (l32 >= wreal) return;
+    float* x = (float*)(ws + L.part_at) +
+               (((size_t)hk * L.slots + it.slot) * L.rows + 32 * w + l32) * (D + 4);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_ldexpf(oacc[dt][4 * g + j], -up);
+        *(f32x4*)(x + 32 * dt + 8 * g + 4 * h) = y;
+      }
+    if (h == 0) {
+      x[D] = m;
+      x[D + 1] = l_tot;
+    }
+    return;
+  }
+  if (l32 >= wreal) return;
+  const bool any = l_tot != 0.f;
+  const float inv = any ? 1.f / l_tot : 0.f;
+  bf16* orow = out + (it.start + tok) * P.o_st + head * P.o_sh;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = f2bf(any ? oacc[dt][4 * g + j] * inv : 0.f);
+      *(bf16x4*)(orow + 32 * dt + 8 * g + 4 * h) = x;
+    }
+  if (lse && h == 0)
+    lse[(size_t)(it.start + tok) * P.H + head] =
+        any ? (m + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
+}
+
+// ---- joining the parts --------------------------------------------------------------------
+
+// Workgroup (cut block, key head, group of kJoinRows rows); one wavefront a row at a time.
+constexpr int kJoinRows = 16;
+
+template <typename T>
+__global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, const Plan L,
+                                                         const char* __restrict__ ws,
+                                                         T* __restrict__ out,
+                                                         float* __restrict__ lse) {
+  const int c = blockIdx.x, hk = blockIdx.y, lane = threadIdx.x & 63;
+  if (c >= ((const PlanHead*)ws)->cuts) return;
+  const Cut cut = ((const Cut*)(ws + L.cut_at))[c];
+  const int64_t r0 = (int64_t)cut.a * L.rows;
+  const int real = (int)min((int64_t)L.rows, (int64_t)cut.lq * P.G - r0);
+  const int stride = P.d + 4, end = min(real, (int)(blockIdx.z + 1) * kJoinRows);
+  const int d0 = min(lane, P.d - 1), d1 = min(lane + 64, P.d - 1);
+  for (int r = blockIdx.z * kJoinRows + (threadIdx.x >> 6); r < end; r += 4) {
+    const float* p = (const float*)(ws + L.part_at) +
+                     (((size_t)hk * L.slots + cut.slot) * L.rows + r) * stride;
+    const size_t next = (size_t)L.rows * stride;
+    float mx = -INFINITY;
+    for (int i = lane; i < cut.n; i += 64)
+      if (p[i * next + P.d + 1] != 0.f) mx = fmaxf(mx, p[i * next + P.d]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f, a0 = 0.f, a1 = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < cut.n; ++i) {
+      const float* x = p + i * next;
+      const float s = x[P.d + 1], y0 = x[d0], y1 = x[d1];
+      // no key of the part is there: its reference is not one
+      const float f = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[P.d] - ref);
+      sum += f * s;
+      a0 += f * y0;
+      a1 += f * y1;
+    }
+    const int64_t row = r0 + r;
+    const int tok = (int)(row / P.G), head = hk * P.G + (int)(row - (int64_t)tok * P.G);
+    T* o = out + (cut.start + tok) * P.o_st + head * P.o_sh;
+    if (lane < P.d) store_f(o + lane, sum != 0.f ? a0 / sum : 0.f);
+    if (lane + 64 < P.d) store_f(o + lane + 64, sum != 0.f ? a1 / sum : 0.f);
+    if (lse && lane == 0)
+      lse[(size_t)(cut.start + tok) * P.H + head] =
+          sum != 0.f ? (ref + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// ---- fp32 ---------------------------------------------------------------------------------
+
+// One workgroup per (token, head): a lane a key, then a lane one or two dims.
 __device__ __forceinline__ int seq_of(const ChunkProb& P, int t) {
   if (t < P.start(0) || t >= P.start(P.B)) return -1;
   int lo = 0, hi = P.B;  // start(lo) <= t < start(hi)
@@ -106,19 +585,81 @@ __global__ __launch_bounds__(256) void chunk_kernel(const ChunkProb P, const T* 
   if (lse && tid == 0) lse[(size_t)t * P.H + h] = sum != 0.f ? mx + logf(sum) : -INFINITY;
 }
 
+// ---- launches -----------------------------------------------------------------------------
+
+// Workgroups that the compute units hold at once (256 units, two or three each): the share
+// of one of them is what a block is cut to, so that no workgroup runs much longer
+// than all need together.
+Plan plan_of(const ChunkProb& P) {
+  Plan L;
+  L.rows = P.dtype == CA_BF16 ? kWalkRows : kF32Rows;
+  const int held = P.d <= 64 ? 768 : 512;
+  const int64_t rows = (int64_t)P.tokens * P.G;
+  L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
+  L.share = (held + P.Hk - 1) / P.Hk;
+  // a cut block has more than `part` tiles, part >= all tiles / share: the parts of the cut
+  // blocks are at most twice the share, and so few blocks are cut
+  L.slots = 2 * L.share;
+  L.cuts = L.share < L.blocks ? L.share : L.blocks;
+  int64_t most = ((int64_t)P.max_pages * P.page + KT - 1) / KT + 2;  // tiles of a block
+  most = (most + kPartTiles - 1) / kPartTiles;
+  if (most == 1) L.slots = L.cuts = 0;
+  if (L.slots > L.blocks * most) L.slots = (int)(L.blocks * most);
+  L.items = L.blocks + L.slots;
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  L.item_at = 256;
+  L.cut_at = align(L.item_at + (size_t)L.items * sizeof(Item));
+  L.part_at = align(L.cut_at + (size_t)L.cuts * sizeof(Cut));
+  L.bytes = align(L.part_at + (size_t)P.Hk * L.slots * L.rows * (P.d + 4) * 4);
+  return L;
+}
+
+template <int D, bool GROUPS>
+hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16* kp,
+                    const bf16* vp, bf16* out, float* lse, char* ws, hipStream_t st) {
+  const ItemOrder order = ItemOrder::of(P.Hk);
+  hipLaunchKernelGGL((chunk_bf16_kernel<D, GROUPS>), dim3((unsigned)order.grid(L.items)),
+                     dim3(256), 0, st, P, L, order, FastDiv::of(P.page), q, kp, vp, out, lse, ws,
+                     P.scale * kLog2e);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16* kp,
+                    const bf16* vp, bf16* out, float* lse, char* ws, hipStream_t st) {
+  // the rows of a page that a group of 16 takes are reached by 32-bit offsets
+  const bool groups = P.page % 16 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23);
+  return groups ? run_bf16<D, true>(P, L, q, kp, vp, out, lse, ws, st)
+                : run_bf16<D, false>(P, L, q, kp, vp, out, lse, ws, st);
+}
+
 }  // namespace
 
-size_t chunk_bytes(const ChunkProb& P) { return 0; }
+bool chunk_fits(const ChunkProb& P) {
+  if ((int64_t)P.tokens * P.G >= ((int64_t)1 << 31)) return false;
+  // workgroups of 256 threads, fewer than 2^32 of them
+  return ItemOrder::of(P.Hk).grid(plan_of(P).items) < (1 << 24);
+}
+
+size_t chunk_bytes(const ChunkProb& P) { return P.dtype == CA_BF16 ? plan_of(P).bytes : 0; }
 
 hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st) {
-  const dim3 grid(P.tokens, P.H);
-  if (P.dtype == CA_BF16)
-    hipLaunchKernelGGL((chunk_kernel<bf16>), grid, dim3(256), 0, st, P, (const bf16*)q,
-                       (const bf16*)kp, (const bf16*)vp, (bf16*)out, lse);
-  else
-    hipLaunchKernelGGL((chunk_kernel<float>), grid, dim3(256), 0, st, P, (const float*)q,
-                       (const float*)kp, (const float*)vp, (float*)out, lse);
+  if (P.dtype == CA_F32) {
+    hipLaunchKernelGGL((chunk_kernel<float>), dim3(P.tokens, P.H), dim3(256), 0, st, P,
+                       (const float*)q, (const float*)kp, (const float*)vp, (float*)out, lse);
+    return hipGetLastError();
+  }
+  const Plan L = plan_of(P);
+  hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L, ws);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const bf16 *a = (const bf16*)q, *b = (const bf16*)kp, *c = (const bf16*)vp;
+  e = P.d == 64 ? run_bf16<64>(P, L, a, b, c, (bf16*)out, lse, ws, st)
+                : run_bf16<128>(P, L, a, b, c, (bf16*)out, lse, ws, st);
+  if (e != hipSuccess || L.slots == 0) return e;
+  hipLaunchKernelGGL((chunk_join_kernel<bf16>), dim3(L.cuts, P.Hk, L.rows / kJoinRows), dim3(256), 0,
+                     st, P, L, ws, (bf16*)out, lse);
   return hipGetLastError();
 }
 

@@ -189,6 +189,7 @@ struct WriteProb {
 
 hipError_t launch_write(const WriteProb& P, const void* k, const void* v, void* kp, void* vp,
                         hipStream_t st);
+bool chunk_fits(const ChunkProb& P);  // sizes that one launch can have
 size_t chunk_bytes(const ChunkProb& P);
 hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st);
