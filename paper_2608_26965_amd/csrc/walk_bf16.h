@@ -116,7 +116,8 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
   };
   // accumulator r of row tile mt is key k0 + 32 mt + 8 (r / 4) + 4 h + r % 4
   // (the query's ranges are formed here: kept over the loop they cost registers)
-  auto mask = [&](int k0, uint64_t hv) __attribute__((always_inline)) {
+  uint64_t hv = 0;  // keys of the tile that are not there
+  auto mask = [&](int k0) __attribute__((always_inline)) {
     int p = T.pos;
     asm volatile("" : "+v"(p));
     const KeyRange rr = visible_keys(T.mask, p, T.lk);
@@ -130,12 +131,12 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
         if (!((uint32_t)(a0 + c) < len || c < b0)) sacc[mt][r] = -INFINITY;
       }
     if (Tiles::kHoles && hv) {
-      hv >>= 4 * h;
+      const uint64_t x = hv >> (4 * h);
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if ((hv >> (32 * mt + 8 * (r >> 2) + (r & 3))) & 1) sacc[mt][r] = -INFINITY;
+          if ((x >> (32 * mt + 8 * (r >> 2) + (r & 3))) & 1) sacc[mt][r] = -INFINITY;
     }
   };
   auto exp_group = [&](int mt, int s2, float ref) __attribute__((always_inline)) {
@@ -154,18 +155,21 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
       oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pb[mt][s2], oacc[dt], 0, 0, 0);
     }
   };
-  // The reference of the tile in key buffer `buf`, from key k0 on: the rows' own where every
-  // row has one and sees all of the tile (`keep`), else raised to the tile's maximum. True
-  // if raised.
-  auto reference = [&](int buf, int k0, bool keep) __attribute__((always_inline)) {
+  // The class of the tile in key buffer `buf`, and its holes (before its logits: nothing
+  // waits for them there)
+  auto class_of = [&](int buf, int k0) __attribute__((always_inline)) {
     int c = tile_class(T.ra, T.rz, k0);
-    uint64_t hv = 0;
     if constexpr (Tiles::kHoles) {
       hv = T.holes(buf);
       if (hv && c == 2) c = 1;
     }
+    return c;
+  };
+  // The reference of a tile of class c: the rows' own where every row has one and
+  // sees all of the tile (`keep`), else raised to the tile's maximum. True if raised.
+  auto reference = [&](int c, int k0, bool keep) __attribute__((always_inline)) {
     if (keep && c == 2 && set) return false;
-    if (c == 1) mask(k0, hv);
+    if (c == 1) mask(k0);
     if (c == 0) {
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -221,9 +225,9 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
   auto step = [&](auto par_tag, int t) __attribute__((always_inline)) {
     constexpr int PAR = decltype(par_tag)::value;
     copies(par_tag, t);
-    const int k0 = KT * T.tile(t);
+    const int k0 = KT * T.tile(t), c = class_of(PAR, k0);
     logits(smem + PAR * TILE);
-    const bool raised = reference(PAR, k0, true);
+    const bool raised = reference(c, k0, true);
     const float ref = m == -INFINITY ? 0.f : m;  // no key yet
     const char* vs = smem + (2 + (PAR ^ 1)) * TILE;
     constexpr int SV = DT / 2;  // steps of a group: two products and some of its exponentials
@@ -280,9 +284,9 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
       }
       sync_stage();
     } else {
-      const int k0 = KT * T.tile(T.t0);
+      const int k0 = KT * T.tile(T.t0), c = class_of(0, k0);
       logits(smem);
-      reference(0, k0, true);
+      reference(c, k0, true);
       const float ref = m == -INFINITY ? 0.f : m;
       groups([&](int mt, int s2) { exp_group(mt, s2, ref); });
       for (int t = T.t0 + 1; t < T.t1; t += 2) {
@@ -334,7 +338,7 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
         for (int c = 0; c < NCH; ++c) *(f32x4*)(vs + lane * RB + c * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       __syncthreads();
-      if constexpr (Tiles::kHoles) bad &= ~T.holes(0);  // (those hold another key's value)
+      if constexpr (Tiles::kHoles) bad &= ~T.holes(0);  // (they hold another key's value)
       const KeyRange rr = visible_keys(T.mask, T.pos, T.lk);
       for (; bad; bad &= bad - 1) poison |= sees(rr, k0 + __builtin_ctzll(bad));
     };
@@ -346,8 +350,9 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
       sync_stage();
       guard(smem + 2 * TILE, k0);
       if (T.real) {
+        const int c = class_of(0, k0);
         logits(smem);
-        const bool raised = reference(0, k0, false);
+        const bool raised = reference(c, k0, false);
         const float ref = m == -INFINITY ? 0.f : m;
         if (raised) rescale();
         groups([&](int mt, int s2) {
