@@ -21,7 +21,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kPlan = 1024;    // threads of the planning workgroup
+constexpr int kPlan = 256;     // threads of the planning workgroup
 constexpr int kPartTiles = 8;  // tiles of a part, at least
 constexpr int kF32Rows = 64;   // rows of a block, fp32
 
@@ -47,127 +47,147 @@ struct Plan {
   size_t item_at, cut_at, part_at, bytes;
 };
 
-__device__ __forceinline__ int blocks_of(const ChunkProb& P, int rows, int b) {
-  const int64_t r = (int64_t)max(0, P.start(b + 1) - P.start(b)) * P.G;
-  return (int)((r + rows - 1) / rows);
-}
-
-// Positions of a block's first and last row, and its tiles
+// Positions of a block's first and last row (a sequence has fewer than 2^30 rows)
 struct BlockSpan {
-  int p0, p1, real;
+  int p0, p1;
   __device__ __forceinline__ BlockSpan(int a, int rows, int G, int lq, int lk) {
-    const int64_t all = (int64_t)lq * G, r0 = (int64_t)a * rows;
-    real = (int)min((int64_t)rows, all - r0);
-    p0 = (int)(r0 / G) + lk - lq;
-    p1 = (int)((r0 + real - 1) / G) + lk - lq;
+    const int r0 = a * rows;
+    p0 = r0 / G + lk - lq;
+    p1 = min((r0 + rows - 1) / G, lq - 1) + lk - lq;
   }
 };
 
-// Sum of x over the threads before this one, and over all of them
-__device__ __forceinline__ int64_t plan_scan(int64_t x, int64_t (&sums)[kPlan / 64],
-                                             int64_t* total) {
+// Sums of x and y over the threads before this one, and over all of them
+struct Pair {
+  int x, y;
+};
+__device__ __forceinline__ Pair plan_scan(int x, int y, Pair (&sums)[kPlan / 64], Pair* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t in = x;
+  int a = x, b = y;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(in, o, 64);
-    if (lane >= o) in += y;
+    const int c = __shfl_up(a, o, 64), d = __shfl_up(b, o, 64);
+    if (lane >= o) {
+      a += c;
+      b += d;
+    }
   }
   __syncthreads();  // the sums of a scan before are read
-  if (lane == 63) sums[w] = in;
+  if (lane == 63) sums[w] = Pair{a, b};
   __syncthreads();
-  int64_t before = 0, all = 0;
+  Pair before{a - x, b - y}, all{0, 0};
 #pragma unroll
   for (int i = 0; i < kPlan / 64; ++i) {
-    if (i < w) before += sums[i];
-    all += sums[i];
+    if (i < w) {
+      before.x += sums[i].x;
+      before.y += sums[i].y;
+    }
+    all.x += sums[i].x;
+    all.y += sums[i].y;
   }
   *total = all;
-  return before + in - x;
+  return before;
 }
 
-// One workgroup: blocks by sequence, the last one (with most keys, if causal) first.
+// The last place of ascending list[0 .. kPlan - 1] that holds at most i
+__device__ __forceinline__ int plan_find(const int* list, int i) {
+  int lo = 0;
+#pragma unroll
+  for (int step = kPlan / 2; step > 0; step >>= 1)
+    if (list[lo + step] <= i) lo += step;
+  return lo;
+}
+
+// One workgroup: blocks by sequence, the last one (with most keys, if causal) first. A pass
+// counts the tiles, another one cuts and writes the items, thread by item.
 __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, const Plan L,
                                                            char* ws) {
-  __shared__ int64_t sums[kPlan / 64];
-  __shared__ int first[kPlan + 1], s_lq[kPlan], s_lk[kPlan], s_start[kPlan];
+  __shared__ Pair sums[kPlan / 64];
+  __shared__ int64_t tiles_of[kPlan / 64];
+  // of a sequence: its first block; of a block: its first item
+  __shared__ int first[kPlan], s_n[kPlan], s_lq[kPlan], s_lk[kPlan], s_start[kPlan];
+  __shared__ int b_item[kPlan], b_seq[kPlan], b_a[kPlan], b_tiles[kPlan], b_slot[kPlan];
   PlanHead* head = (PlanHead*)ws;
   Item* items = (Item*)(ws + L.item_at);
   Cut* cuts = (Cut*)(ws + L.cut_at);
   const int tid = threadIdx.x;
-  int64_t all_tiles = 0, n_items = 0, n_slots = 0, n_cuts = 0;
-  int part = 0;
+  int64_t tiles_seen = 0;
+  int n_items = 0, n_slots = 0, n_cuts = 0, part = 1;
   for (int pass = 0; pass < 2; ++pass) {
-    int64_t seen = 0;  // blocks so far: no more than the host counted
+    int seen = 0;  // blocks so far: no more than the host counted
     for (int b0 = 0; b0 < P.B && seen < L.blocks; b0 += kPlan) {
       const int b = b0 + tid;
       int n = 0;
       if (b < P.B) {
-        n = blocks_of(P, L.rows, b);
-        s_start[tid] = P.start(b);
-        s_lq[tid] = max(0, P.start(b + 1) - P.start(b));
+        const int start = P.start(b), lq = max(0, P.start(b + 1) - start);
+        s_start[tid] = start;
+        s_lq[tid] = lq;
         s_lk[tid] = P.klen(b);
+        s_n[tid] = n = (int)(((uint32_t)lq * (uint32_t)P.G + L.rows - 1) / (uint32_t)L.rows);
       }
-      int64_t total;
-      const int64_t before = plan_scan(n, sums, &total);
-      total = min(total, (int64_t)L.blocks - seen);
-      first[tid] = (int)min(before, total);
-      if (tid == 0) first[kPlan] = (int)total;
+      Pair total;
+      const Pair before = plan_scan(min(n, L.blocks), 0, sums, &total);
+      // (unsigned: the sum of starts that do not ascend may pass 2^31)
+      const int blocks = (int)min((uint32_t)total.x, (uint32_t)(L.blocks - seen));
+      first[tid] = (int)min((uint32_t)before.x, (uint32_t)INT32_MAX);
       __syncthreads();
-      for (int64_t i0 = 0; i0 < total; i0 += kPlan) {
-        const int i = (int)i0 + tid;
-        int64_t tiles = 0, parts = 0;
-        int lo = 0, a = 0;
-        if (i < total) {
-          int hi = kPlan;  // first[lo] <= i < first[hi]
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first[mid] <= i)
-              lo = mid;
-            else
-              hi = mid;
-          }
-          a = blocks_of(P, L.rows, b0 + lo) - 1 - (i - first[lo]);
+      for (int i0 = 0; i0 < blocks; i0 += kPlan) {
+        const int i = i0 + tid;
+        int tiles = 0, parts = 0, lo = 0, a = 0;
+        if (i < blocks) {
+          lo = plan_find(first, i);
+          a = s_n[lo] - 1 - (i - first[lo]);
           const BlockSpan s(a, L.rows, P.G, s_lq[lo], s_lk[lo]);
           tiles = visible_tiles<KT>(P.m, s.p0, s.p1, s_lk[lo]).n;
-          parts = 1;
-          if (pass == 1 && tiles > part) parts = (tiles + part - 1) / part;
+          parts = max(1, (tiles + part - 1) / part);
         }
-        int64_t sum;
         if (pass == 0) {
-          plan_scan(tiles, sums, &sum);
-          all_tiles += sum;
+          tiles_seen += tiles;
           continue;
         }
-        int64_t n_cut;
-        const int64_t cut = plan_scan(parts > 1 ? 1 : 0, sums, &n_cut);
-        const int64_t slot = n_slots + plan_scan(parts > 1 ? parts : 0, sums, &sum);
-        n_slots += sum;
-        const int64_t item = n_items + plan_scan(parts, sums, &sum);
-        n_items += sum;
+        const Pair at = plan_scan(parts, parts > 1 ? 1 : 0, sums, &total);
+        // slots count the parts of cut blocks: all items but those of whole ones
+        const int slot = n_slots + at.x - (tid - at.y), cut = n_cuts + at.y;
+        b_item[tid] = at.x;
+        b_seq[tid] = lo;
+        b_a[tid] = a;
+        b_tiles[tid] = tiles;
+        b_slot[tid] = parts > 1 ? slot : -1;
         // (the host's bounds hold for ascending starts; nothing is written outside them)
-        const bool whole = parts == 1;
-        if (i < total && item + parts <= L.items &&
-            (whole || (slot + parts <= L.slots && n_cuts + cut < L.cuts))) {
-          if (!whole)
-            cuts[n_cuts + cut] = Cut{a, (int)slot, (int)parts, s_lq[lo], s_lk[lo], s_start[lo]};
-          const int per = (int)((tiles + parts - 1) / parts);
-          for (int x = 0; x < parts; ++x) {
-            const int t0 = min((int)tiles, x * per), t1 = min((int)tiles, t0 + per);
-            items[item + x] = Item{b0 + lo, a, t0, t1, whole ? -1 : (int)slot + x,
-                                   s_lq[lo], s_lk[lo], s_start[lo]};
-          }
+        if (parts > 1 && cut < L.cuts && slot + parts <= L.slots)
+          cuts[cut] = Cut{a, slot, parts, s_lq[lo], s_lk[lo], s_start[lo]};
+        __syncthreads();
+        const int some = min(kPlan, blocks - i0);
+        for (int j = tid; j < total.x; j += kPlan) {
+          const int x = min(plan_find(b_item, j), some - 1), y = j - b_item[x], q = b_seq[x];
+          const int all = (x + 1 < some ? b_item[x + 1] : total.x) - b_item[x];
+          const int per = (b_tiles[x] + all - 1) / all, t0 = min(b_tiles[x], y * per);
+          const int z = b_slot[x] < 0 ? -1 : b_slot[x] + y;
+          if (n_items + j < L.items && z < L.slots)
+            items[n_items + j] = Item{b0 + q, b_a[x], t0, min(b_tiles[x], t0 + per), z,
+                                      s_lq[q], s_lk[q], s_start[q]};
         }
-        n_cuts += n_cut;
+        n_items += total.x;
+        n_cuts += total.y;
+        n_slots += total.x - (some - total.y);
       }
-      seen += total;
+      seen += blocks;
       __syncthreads();  // the segment's lists are read
     }
-    part = (int)max((int64_t)kPartTiles, (all_tiles + L.share - 1) / L.share);
+    if (pass == 0) {
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) tiles_seen += __shfl_xor(tiles_seen, o, 64);
+      if ((tid & 63) == 0) tiles_of[tid >> 6] = tiles_seen;
+      __syncthreads();
+      int64_t all = 0;
+#pragma unroll
+      for (int x = 0; x < kPlan / 64; ++x) all += tiles_of[x];
+      part = (int)min(max((int64_t)kPartTiles, (all + L.share - 1) / L.share), (int64_t)1 << 25);
+    }
   }
   if (tid == 0) {
-    head->items = (int)min(n_items, (int64_t)L.items);
-    head->cuts = (int)min(n_cuts, (int64_t)L.cuts);
+    head->items = min(n_items, L.items);
+    head->cuts = min(n_cuts, L.cuts);
   }
 }
 
@@ -442,50 +462,83 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
 
 // ---- joining the parts --------------------------------------------------------------------
 
-// Workgroup (cut block, key head, group of kJoinRows rows); one wavefront a row at a time.
-constexpr int kJoinRows = 16;
+// A row's parts are read 16 bytes a lane, D / 4 lanes a part, by one wavefront where there
+// are few of them, by the four of the workgroup where there are many. The workgroups take
+// groups of four rows (few parts) or a row (many) one after the other.
+constexpr int kJoinGrid = 2048, kFewParts = 16;
 
-template <typename T>
+template <typename T, int DP>
 __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, const Plan L,
                                                          const char* __restrict__ ws,
                                                          T* __restrict__ out,
                                                          float* __restrict__ lse) {
-  const int c = blockIdx.x, hk = blockIdx.y, lane = threadIdx.x & 63;
-  if (c >= ((const PlanHead*)ws)->cuts) return;
-  const Cut cut = ((const Cut*)(ws + L.cut_at))[c];
-  const int64_t r0 = (int64_t)cut.a * L.rows;
-  const int real = (int)min((int64_t)L.rows, (int64_t)cut.lq * P.G - r0);
-  const int stride = P.d + 4, end = min(real, (int)(blockIdx.z + 1) * kJoinRows);
-  const int d0 = min(lane, P.d - 1), d1 = min(lane + 64, P.d - 1);
-  for (int r = blockIdx.z * kJoinRows + (threadIdx.x >> 6); r < end; r += 4) {
-    const float* p = (const float*)(ws + L.part_at) +
-                     (((size_t)hk * L.slots + cut.slot) * L.rows + r) * stride;
-    const size_t next = (size_t)L.rows * stride;
-    float mx = -INFINITY;
-    for (int i = lane; i < cut.n; i += 64)
-      if (p[i * next + P.d + 1] != 0.f) mx = fmaxf(mx, p[i * next + P.d]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f, a0 = 0.f, a1 = 0.f;
+  constexpr int LP = DP / 4, NP = 64 / LP;  // lanes of a part, parts of a wavefront's read
+  __shared__ float acc[4][DP], wmax[4], wsum[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int t = 4 * (lane % LP), stride = P.d + 4, n_cuts = ((const PlanHead*)ws)->cuts;
+  const size_t next = (size_t)L.rows * stride;
+  for (int c = blockIdx.x; c < n_cuts * P.Hk * (L.rows / 4); c += gridDim.x) {
+    const int rq = c % (L.rows / 4), x = c / (L.rows / 4), hk = x / n_cuts;
+    const Cut cut = ((const Cut*)(ws + L.cut_at))[x - hk * n_cuts];
+    const int r0 = cut.a * L.rows, real = min(L.rows, cut.lq * P.G - r0);
+    const bool few = cut.n <= kFewParts;
+    for (int r = 4 * rq + (few ? w : 0); r < min(real, 4 * rq + 4); r += few ? 4 : 1) {
+      const float* p = (const float*)(ws + L.part_at) +
+                       (((size_t)hk * L.slots + cut.slot) * L.rows + r) * stride;
+      // each lane's own parts against their own maximum, then all against the largest
+      float mx = -INFINITY, sum = 0.f;
+      f32x4 a = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int i = 0; i < cut.n; ++i) {
-      const float* x = p + i * next;
-      const float s = x[P.d + 1], y0 = x[d0], y1 = x[d1];
-      // no key of the part is there: its reference is not one
-      const float f = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[P.d] - ref);
-      sum += f * s;
-      a0 += f * y0;
-      a1 += f * y1;
+      for (int i = (few ? 0 : w * NP) + lane / LP; i < cut.n; i += few ? NP : 4 * NP) {
+        const float* y = p + i * next;
+        const f32x4 v = t < P.d ? *(const f32x4*)(y + t) : f32x4{0.f, 0.f, 0.f, 0.f};
+        const float m = y[P.d], s = y[P.d + 1];
+        // no key of the part is there: its reference is not one
+        const float m1 = s == 0.f ? mx : fmaxf(mx, m);
+        const float ref = m1 == -INFINITY ? 0.f : m1;
+        const float f = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - ref);
+        const float g = __builtin_amdgcn_exp2f(mx - ref);
+        sum = sum * g + s * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = a[e] * g + v[e] * f;
+        mx = m1;
+      }
+      auto merge = [&](float m2, float s2, f32x4 a2) __attribute__((always_inline)) {
+        const float m1 = fmaxf(mx, m2), ref = m1 == -INFINITY ? 0.f : m1;
+        const float f = __builtin_amdgcn_exp2f(mx - ref), g = __builtin_amdgcn_exp2f(m2 - ref);
+        sum = sum * f + s2 * g;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = a[e] * f + a2[e] * g;
+        mx = m1;
+      };
+#pragma unroll
+      for (int o = LP; o < 64; o <<= 1) {
+        const f32x4 b = {__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64), __shfl_xor(a[2], o, 64),
+                         __shfl_xor(a[3], o, 64)};
+        merge(__shfl_xor(mx, o, 64), __shfl_xor(sum, o, 64), b);
+      }
+      if (!few) {
+        __syncthreads();  // the row before is read
+        if (lane < LP) *(f32x4*)&acc[w][t] = a;
+        if (lane == 0) {
+          wmax[w] = mx;
+          wsum[w] = sum;
+        }
+        __syncthreads();
+        if (w > 0) continue;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) merge(wmax[i], wsum[i], *(const f32x4*)&acc[i][t]);
+      }
+      if (lane >= LP) continue;
+      const int row = r0 + r, tok = row / P.G, h = hk * P.G + row - tok * P.G;
+      T* o = out + (cut.start + tok) * P.o_st + h * P.o_sh + t;
+      if (t < P.d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_f(o + e, sum != 0.f ? a[e] / sum : 0.f);
+      if (lse && lane == 0)
+        lse[(size_t)(cut.start + tok) * P.H + h] =
+            sum != 0.f ? (mx + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     }
-    const int64_t row = r0 + r;
-    const int tok = (int)(row / P.G), head = hk * P.G + (int)(row - (int64_t)tok * P.G);
-    T* o = out + (cut.start + tok) * P.o_st + head * P.o_sh;
-    if (lane < P.d) store_f(o + lane, sum != 0.f ? a0 / sum : 0.f);
-    if (lane + 64 < P.d) store_f(o + lane + 64, sum != 0.f ? a1 / sum : 0.f);
-    if (lse && lane == 0)
-      lse[(size_t)(cut.start + tok) * P.H + head] =
-          sum != 0.f ? (ref + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
   }
 }
 
@@ -636,7 +689,7 @@ hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16
 }  // namespace
 
 bool chunk_fits(const ChunkProb& P) {
-  if ((int64_t)P.tokens * P.G >= ((int64_t)1 << 31)) return false;
+  if ((int64_t)P.tokens * P.G >= ((int64_t)1 << 30)) return false;
   // workgroups of 256 threads, fewer than 2^32 of them
   return ItemOrder::of(P.Hk).grid(plan_of(P).items) < (1 << 24);
 }
@@ -658,8 +711,12 @@ hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const
   e = P.d == 64 ? run_bf16<64>(P, L, a, b, c, (bf16*)out, lse, ws, st)
                 : run_bf16<128>(P, L, a, b, c, (bf16*)out, lse, ws, st);
   if (e != hipSuccess || L.slots == 0) return e;
-  hipLaunchKernelGGL((chunk_join_kernel<bf16>), dim3(L.cuts, P.Hk, L.rows / kJoinRows), dim3(256), 0,
-                     st, P, L, ws, (bf16*)out, lse);
+  const int64_t quads = (int64_t)L.cuts * P.Hk * (L.rows / 4);
+  const dim3 grid((unsigned)(quads < kJoinGrid ? quads : kJoinGrid));
+  if (P.d == 64)
+    hipLaunchKernelGGL((chunk_join_kernel<bf16, 64>), grid, dim3(256), 0, st, P, L, ws, (bf16*)out, lse);
+  else
+    hipLaunchKernelGGL((chunk_join_kernel<bf16, 128>), grid, dim3(256), 0, st, P, L, ws, (bf16*)out, lse);
   return hipGetLastError();
 }
 
