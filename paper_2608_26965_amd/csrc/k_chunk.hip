@@ -543,99 +543,215 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 }
 
 // ---- fp32 ---------------------------------------------------------------------------------
+//
+// One wavefront per 16 rows, on the fp32 matrix instructions (v_mfma_f32_16x16x4_f32): S^T =
+// K Q^T leaves lane l with row l % 16 and the logits of keys 4 (l / 16) + r, which is
+// the P^T operand of O^T = V^T P^T as it stands. Half tiles of 32 keys go through registers
+// to LDS, one ahead of the one that is computed; rows of DP + 4 floats there, so that
+// neither the keys' 16-byte reads nor the values' 4-byte reads meet on a bank. What bounds
+// it: the matrix instructions, 32 cycles each.
 
-// One workgroup per (token, head): a lane a key, then a lane one or two dims.
-__device__ __forceinline__ int seq_of(const ChunkProb& P, int t) {
-  if (t < P.start(0) || t >= P.start(P.B)) return -1;
-  int lo = 0, hi = P.B;  // start(lo) <= t < start(hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (P.start(mid) <= t)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
-}
+template <int DP, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
+    const ChunkProb P, const Plan L, const ItemOrder order, const FastDiv by_page,
+    const float* __restrict__ q, const float* __restrict__ kp, const float* __restrict__ vp,
+    float* __restrict__ out, float* __restrict__ lse, char* __restrict__ ws, float sl2) {
+  constexpr int HK = 32, NJ = DP / 16, LD = DP + 4, NC = DP / 4;
+  constexpr int RP = 256 / NC, NP = HK / RP;  // rows of a pass of the copy, passes
+  __shared__ __attribute__((aligned(16))) float ks[2][HK][LD], vs[2][HK][LD];
+  __shared__ uint32_t gone[4], bad[4];  // keys not there, values that are not finite
+  int item, hk;
+  if (!order.at(blockIdx.x, ((const PlanHead*)ws)->items, &item, &hk)) return;
+  const Item it = ((const Item*)(ws + L.item_at))[item];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int off = it.lk - it.lq, r0 = it.a * kF32Rows, rows = it.lq * P.G;
+  const BlockSpan span(it.a, kF32Rows, P.G, it.lq, it.lk);
+  const TileList list = visible_tiles<KT>(P.m, span.p0, span.p1, it.lk);
+  const int w0 = r0 + 16 * w, wreal = max(0, min(16, rows - w0));
+  const int wl = min(w0 + max(wreal, 1) - 1, rows - 1);
+  const int row = min(w0 + l16, wl);  // this lane's row
+  const int tok = row / P.G, head = hk * P.G + row - tok * P.G;
+  const KeyRange ra = visible_keys(P.m, min(w0, rows - 1) / P.G + off, it.lk);
+  const KeyRange rz = visible_keys(P.m, wl / P.G + off, it.lk);
+  const KeyRange mine = visible_keys(P.m, tok + off, it.lk);
 
-template <typename T>
-__global__ __launch_bounds__(256) void chunk_kernel(const ChunkProb P, const T* __restrict__ q,
-                                                    const T* __restrict__ kp,
-                                                    const T* __restrict__ vp, T* __restrict__ out,
-                                                    float* __restrict__ lse) {
-  __shared__ float qs[kMaxD], prob[4][64], o[4][kMaxD], ms[4], ls[4];
-  __shared__ int64_t at[4][64];
-  const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int b = seq_of(P, t);
-  if (b < 0) return;
-  const int s0 = P.start(b), lq = P.start(b + 1) - s0, lk = P.klen(b), hk = h / P.G;
-  const KeyRange r = visible_keys(P.m, t - s0 + lk - lq, lk);
-  for (int i = tid; i < P.d; i += 256) qs[i] = to_f(q[t * P.q_st + h * P.q_sh + i]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
-  for (int j0 = 64 * w; j0 < lk; j0 += 256) {
-    const int j = j0 + lane;
-    float s = -INFINITY;
-    int64_t va = -1;
-    if (j < lk && sees(r, j)) {
-      const int e = P.table[b * P.table_sb + j / P.page], in = j % P.page;
-      if (e >= 0 && e < P.pages) {
-        const T* row = kp + e * P.k_sp + in * P.k_st + hk * P.k_sh;
-        s = 0.f;
-        for (int x = 0; x < P.d; x += 4) {
-          const f32x4 y = load4f(row + x);
+  f32x4 qf[NJ];
+  {
+    const float* src = q + (it.start + tok) * P.q_st + head * P.q_sh;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) s = fmaf(y[c], qs[x + c], s);
-        }
-        s *= P.scale;
-        va = e * P.v_sp + in * P.v_st + hk * P.v_sh;
+    for (int j = 0; j < NJ; ++j) {
+      const int x = 16 * j + 4 * g;
+      qf[j] = x < P.d ? *(const f32x4*)(src + x) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  const int cc = 4 * (tid % NC), cr = tid / NC;  // this thread's piece of a row, and row
+  const int32_t* table = P.table + it.b * P.table_sb;
+  const float *kh = kp + hk * P.k_sh + cc, *vh = vp + hk * P.v_sh + cc;
+  const int n = 2 * (it.t1 - it.t0);  // half tiles
+  auto first_key = [&](int i) __attribute__((always_inline)) {
+    return KT * list.tile(it.t0 + (i >> 1)) + HK * (i & 1);
+  };
+  int ent[NP];
+  auto entries = [&](int i) __attribute__((always_inline)) {
+    const int j0 = first_key(min(i, n - 1)) + cr;
+#pragma unroll
+    for (int x = 0; x < NP; ++x) ent[x] = table[by_page.div(min(j0 + x * RP, it.lk - 1))];
+  };
+  f32x4 kr[NP], vr[NP];
+  uint32_t missing;
+  auto load = [&](int i) __attribute__((always_inline)) {
+    const int j0 = first_key(i) + cr;
+    missing = 0;
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const int j = j0 + x * RP, e = ent[x], c = min(j, it.lk - 1), in = c - by_page.div(c) * P.page;
+      const bool there = e >= 0 && e < P.pages;
+      kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (there && j < it.lk && cc < P.d) {
+        kr[x] = *(const f32x4*)(kh + e * P.k_sp + in * P.k_st);
+        vr[x] = *(const f32x4*)(vh + e * P.v_sp + in * P.v_st);
       }
+      if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
     }
-    float mx = s;
+  };
+  auto store = [&](int i) __attribute__((always_inline)) {
+    if (missing) atomicOr(&gone[i & 3], missing);
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float m_new = fmaxf(m, mx);
-    if (m_new == -INFINITY) continue;
-    const float al = expf(m - m_new), p = expf(s - m_new);
-    float sum = p;
+    for (int x = 0; x < NP; ++x) {
+      const int r = cr + x * RP;
+      bool fine = true;
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    l = l * al + sum;
-    m = m_new;
-    acc[0] *= al;
-    acc[1] *= al;
-    prob[w][lane] = p;
-    at[w][lane] = va;
-    __builtin_amdgcn_wave_barrier();
-    for (int i = 0; i < 64; ++i) {
-      const int64_t a = at[w][i];
-      if (a < 0) continue;
-      const float x = prob[w][i];
-      if (lane < P.d) acc[0] = fmaf(x, to_f(vp[a + lane]), acc[0]);
-      if (lane + 64 < P.d) acc[1] = fmaf(x, to_f(vp[a + lane + 64]), acc[1]);
+      for (int e = 0; e < 4; ++e) fine &= fabsf(vr[x][e]) < INFINITY;
+      if (__builtin_expect(!fine, 0)) {
+        // zero times it would reach rows that do not see it: those that do get NaN at the end
+        atomicOr(&bad[i & 3], 1u << r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!(fabsf(vr[x][e]) < INFINITY)) vr[x][e] = 0.f;
+      }
+      *(f32x4*)&ks[i & 1][r][cc] = kr[x];
+      *(f32x4*)&vs[i & 1][r][cc] = vr[x];
     }
-    __builtin_amdgcn_wave_barrier();
-  }
-  o[w][lane] = acc[0];
-  o[w][lane + 64] = acc[1];
-  if (lane == 0) {
-    ms[w] = m;
-    ls[w] = l;
-  }
+  };
+  f32x4 o[NJ];
+  float m = -INFINITY, l = 0.f;  // reference (log2 units), this lane's part of the sum
+  bool poison = false;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](int i) __attribute__((always_inline)) {
+    const int k0 = first_key(i);
+    // no row sees a key; every row sees all
+    if (k0 >= rz.s_end && (k0 >= rz.hi || k0 + HK <= ra.lo)) return;
+    const uint32_t hv = gone[i & 3], bv = bad[i & 3];
+    const bool all = (k0 + HK <= ra.s_end || (k0 >= rz.lo && k0 + HK <= ra.hi)) && hv == 0;
+    const float(*kt)[LD] = ks[i & 1];
+    const float(*vt)[LD] = vs[i & 1];
+    // four partial sums a logit: shorter chains of rounded sums
+    f32x4 p[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[u][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const f32x4 kf = *(const f32x4*)&kt[16 * u + l16][16 * j + 4 * g];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          p[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[j][e], p[u][e], 0, 0, 0);
+      }
+    float s[2][4], mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[u][r] = (p[u][0][r] + p[u][1][r]) + (p[u][2][r] + p[u][3][r]);
+        const int j = 16 * u + 4 * g + r;
+        if (!all && (!sees(mine, k0 + j) || ((hv >> j) & 1))) s[u][r] = -INFINITY;
+        mx = fmaxf(mx, s[u][r]);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
+    if (__builtin_amdgcn_ballot_w64(mx > m)) {
+      const float m1 = fmaxf(m, mx), al = m1 > m ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
+      l *= al;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[j][r] *= al;
+      m = m1;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], sl2, -ref));
+        l += s[u][r];
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[16 * u + 4 * g + r][16 * j + l16], s[u][r],
+                                                      o[j], 0, 0, 0);
+    if (__builtin_expect(bv != 0, 0))
+      for (uint32_t x = bv; x; x &= x - 1) poison |= sees(mine, k0 + __builtin_ctz(x));
+  };
+  if (tid < 4) gone[tid] = bad[tid] = 0;
   __syncthreads();
-  float mx = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-  if (mx == -INFINITY) mx = 0.f;
-  float sum = 0.f, f[4];
+  if (n > 0) {
+    entries(0);
+    load(0);
+    entries(1);
+    store(0);
+    __syncthreads();
+    for (int i = 0; i < n; ++i) {
+      if (i + 1 < n) load(i + 1);
+      entries(i + 2);
+      // the flags of half tile i + 2 (those of i - 2 were read before the last barrier)
+      if (tid == 0) gone[(i + 2) & 3] = bad[(i + 2) & 3] = 0;
+      if (wreal) compute(i);
+      if (i + 1 < n) store(i + 1);
+      __syncthreads();
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (l16 >= wreal) return;
+  if (poison) {
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    f[x] = expf(ms[x] - mx);
-    sum += f[x] * ls[x];
+    for (int j = 0; j < NJ; ++j) o[j] = f32x4{NAN, NAN, NAN, NAN};
   }
-  for (int i = tid; i < P.d; i += 256) {
-    const float x = f[0] * o[0][i] + f[1] * o[1][i] + f[2] * o[2][i] + f[3] * o[3][i];
-    store_f(out + t * P.o_st + h * P.o_sh + i, sum != 0.f ? x / sum : 0.f);
+  if (it.slot >= 0) {
+    float* x = (float*)(ws + L.part_at) +
+               (((size_t)hk * L.slots + it.slot) * L.rows + 16 * w + l16) * (P.d + 4);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      if (16 * j + 4 * g < P.d) *(f32x4*)(x + 16 * j + 4 * g) = o[j];
+    if (g == 0) {
+      x[P.d] = m;
+      x[P.d + 1] = l;
+    }
+    return;
   }
-  if (lse && tid == 0) lse[(size_t)t * P.H + h] = sum != 0.f ? mx + logf(sum) : -INFINITY;
+  const bool any = l != 0.f;
+  float* orow = out + (it.start + tok) * P.o_st + head * P.o_sh;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+    if (16 * j + 4 * g < P.d) {
+      f32x4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = any ? o[j][r] / l : 0.f;
+      *(f32x4*)(orow + 16 * j + 4 * g) = x;
+    }
+  if (lse && g == 0)
+    lse[(size_t)(it.start + tok) * P.H + head] =
+        any ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---- launches -----------------------------------------------------------------------------
@@ -646,7 +762,7 @@ __global__ __launch_bounds__(256) void chunk_kernel(const ChunkProb P, const T* 
 Plan plan_of(const ChunkProb& P) {
   Plan L;
   L.rows = P.dtype == CA_BF16 ? kWalkRows : kF32Rows;
-  const int held = P.d <= 64 ? 768 : 512;
+  const int held = P.d > 64 ? 512 : P.dtype == CA_BF16 ? 768 : 1024;
   const int64_t rows = (int64_t)P.tokens * P.G;
   L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
   L.share = (held + P.Hk - 1) / P.Hk;
@@ -667,23 +783,42 @@ Plan plan_of(const ChunkProb& P) {
   return L;
 }
 
-template <int D, bool GROUPS>
-hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16* kp,
-                    const bf16* vp, bf16* out, float* lse, char* ws, hipStream_t st) {
-  const ItemOrder order = ItemOrder::of(P.Hk);
-  hipLaunchKernelGGL((chunk_bf16_kernel<D, GROUPS>), dim3((unsigned)order.grid(L.items)),
-                     dim3(256), 0, st, P, L, order, FastDiv::of(P.page), q, kp, vp, out, lse, ws,
-                     P.scale * kLog2e);
+template <typename T, int DP>
+hipError_t run_join(const ChunkProb& P, const Plan& L, T* out, float* lse, const char* ws,
+                    hipStream_t st) {
+  if (L.slots == 0) return hipSuccess;
+  const int64_t quads = (int64_t)L.cuts * P.Hk * (L.rows / 4);
+  const dim3 grid((unsigned)(quads < kJoinGrid ? quads : kJoinGrid));
+  hipLaunchKernelGGL((chunk_join_kernel<T, DP>), grid, dim3(256), 0, st, P, L, ws, out, lse);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16* kp,
                     const bf16* vp, bf16* out, float* lse, char* ws, hipStream_t st) {
+  const ItemOrder order = ItemOrder::of(P.Hk);
+  const dim3 grid((unsigned)order.grid(L.items));
+  const FastDiv by_page = FastDiv::of(P.page);
   // the rows of a page that a group of 16 takes are reached by 32-bit offsets
-  const bool groups = P.page % 16 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23);
-  return groups ? run_bf16<D, true>(P, L, q, kp, vp, out, lse, ws, st)
-                : run_bf16<D, false>(P, L, q, kp, vp, out, lse, ws, st);
+  if (P.page % 16 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23))
+    hipLaunchKernelGGL((chunk_bf16_kernel<D, true>), grid, dim3(256), 0, st, P, L, order, by_page,
+                       q, kp, vp, out, lse, ws, P.scale * kLog2e);
+  else
+    hipLaunchKernelGGL((chunk_bf16_kernel<D, false>), grid, dim3(256), 0, st, P, L, order, by_page,
+                       q, kp, vp, out, lse, ws, P.scale * kLog2e);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : run_join<bf16, D>(P, L, out, lse, ws, st);
+}
+
+template <int DP, int WAVES>
+hipError_t run_f32(const ChunkProb& P, const Plan& L, const float* q, const float* kp,
+                   const float* vp, float* out, float* lse, char* ws, hipStream_t st) {
+  const ItemOrder order = ItemOrder::of(P.Hk);
+  hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES>), dim3((unsigned)order.grid(L.items)), dim3(256), 0,
+                     st, P, L, order, FastDiv::of(P.page), q, kp, vp, out, lse, ws,
+                     P.scale * kLog2e);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : run_join<float, DP>(P, L, out, lse, ws, st);
 }
 
 }  // namespace
@@ -694,30 +829,23 @@ bool chunk_fits(const ChunkProb& P) {
   return ItemOrder::of(P.Hk).grid(plan_of(P).items) < (1 << 24);
 }
 
-size_t chunk_bytes(const ChunkProb& P) { return P.dtype == CA_BF16 ? plan_of(P).bytes : 0; }
+size_t chunk_bytes(const ChunkProb& P) { return plan_of(P).bytes; }
 
 hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st) {
-  if (P.dtype == CA_F32) {
-    hipLaunchKernelGGL((chunk_kernel<float>), dim3(P.tokens, P.H), dim3(256), 0, st, P,
-                       (const float*)q, (const float*)kp, (const float*)vp, (float*)out, lse);
-    return hipGetLastError();
-  }
   const Plan L = plan_of(P);
   hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L, ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const bf16 *a = (const bf16*)q, *b = (const bf16*)kp, *c = (const bf16*)vp;
-  e = P.d == 64 ? run_bf16<64>(P, L, a, b, c, (bf16*)out, lse, ws, st)
-                : run_bf16<128>(P, L, a, b, c, (bf16*)out, lse, ws, st);
-  if (e != hipSuccess || L.slots == 0) return e;
-  const int64_t quads = (int64_t)L.cuts * P.Hk * (L.rows / 4);
-  const dim3 grid((unsigned)(quads < kJoinGrid ? quads : kJoinGrid));
-  if (P.d == 64)
-    hipLaunchKernelGGL((chunk_join_kernel<bf16, 64>), grid, dim3(256), 0, st, P, L, ws, (bf16*)out, lse);
-  else
-    hipLaunchKernelGGL((chunk_join_kernel<bf16, 128>), grid, dim3(256), 0, st, P, L, ws, (bf16*)out, lse);
-  return hipGetLastError();
+  if (P.dtype == CA_BF16) {
+    const bf16 *a = (const bf16*)q, *b = (const bf16*)kp, *c = (const bf16*)vp;
+    return P.d == 64 ? run_bf16<64>(P, L, a, b, c, (bf16*)out, lse, ws, st)
+                     : run_bf16<128>(P, L, a, b, c, (bf16*)out, lse, ws, st);
+  }
+  const float *a = (const float*)q, *b = (const float*)kp, *c = (const float*)vp;
+  return P.d <= 32   ? run_f32<32, 4>(P, L, a, b, c, (float*)out, lse, ws, st)
+         : P.d <= 64 ? run_f32<64, 4>(P, L, a, b, c, (float*)out, lse, ws, st)
+                     : run_f32<128, 2>(P, L, a, b, c, (float*)out, lse, ws, st);
 }
 
 }  // namespace ca

@@ -651,6 +651,8 @@ def test_chunk_workspaces_and_refusals(dt):
     ws = torch.full((256 << 20,), 255, dtype=torch.uint8, device="cuda")  # NaN all over
     b = ca.paged_chunk_attn(w, q, kp, vp, table, n, starts, want_lse=True, ws=ws)
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+    with pytest.raises(ca.CAError, match="workspace"):
+        ca.paged_chunk_attn(w, q, kp, vp, table, n, starts, ws=ws[:256])
     call = lambda **kw: ca.paged_chunk_attn(w, **{**dict(q=q, k_pages=kp, v_pages=vp, page_table=table, lens=n,  # noqa: E731
                                                          starts=starts), **kw})
     other = torch.float32 if dt == "bf16" else torch.bfloat16
