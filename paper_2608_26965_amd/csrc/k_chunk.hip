@@ -3,13 +3,16 @@
 // All query heads of a key head share its keys, so a sequence's rows are its new
 // tokens times the G heads of the group (row r: token r / G, head r % G), taken
 // in blocks; a block walks the 64-key tiles that one of its rows sees. Blocks
-// have very different lengths (a prompt's beside a single token's on a long cache),
-// so a first launch plans them: it counts all tiles and cuts long blocks into parts of
-// about what a workgroup's share is. The parts' softmax states are joined by a
-// last launch. The plan is the same for all key heads.
+// have very different lengths (a prompt's beside a single token's on a long cache)
+// and their number seldom fills the compute units evenly, so a first launch plans the
+// work: it lists the blocks and gives every workgroup an equal share of all their
+// tiles, from some tile of one block to some tile of a later one. A block that
+// several workgroups share leaves its softmax states in the workspace, and a last launch
+// joins them. Where there is more than a round of blocks, the first rounds are whole ones
+// (the workgroups that run at a time then read the same keys at a time), and
+// the shares even out the rest; where there are many, no block is cut.
 //
-// What bounds it: the matrix cores for prompts, the cache (read once by each block)
-// for few new tokens.
+// What bounds it: the matrix cores for prompts, the cache for few new tokens.
 #include <math.h>
 
 #include "seq.h"
@@ -22,29 +25,53 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPlan = 256;     // threads of the planning workgroup
-constexpr int kPartTiles = 8;  // tiles of a part, at least
 constexpr int kF32Rows = 64;   // rows of a block, fp32
+constexpr int kXcdUnits = 32;  // compute units of an XCD
+constexpr int kShareTiles = 4; // tiles of a share, at least
+constexpr int kRounds = 6;     // rounds of blocks from which on none is cut
+constexpr int kStart = 4;      // what starting a block costs, in tiles
+constexpr int kSnap = 3;       // shares begin no nearer to a block's ends, in tiles
+constexpr int kIndex = 2048;   // entries of the planning workgroup's index of the blocks
 
-// A workgroup's work, for every key head: tiles [t0, t1) of block a of sequence b (with
-// its lengths and first row). slot: where a part's state goes, -1 for a whole block.
-struct Item {
-  int b, a, t0, t1, slot, lq, lk, start;
+// A block of a sequence's rows, for every key head. cost: of the blocks before it.
+struct Block {
+  int b, a, tiles, lq, lk, start;
+  int64_t cost;
 };
-// A block that is cut: its parts' states lie in slots slot .. slot + n - 1
+// Where a share begins: tile t of a block of the hs-th of the heads that its workgroups take
+struct Share {
+  int hs, block, t, pad;
+};
+// A block that is cut: its first part is the end of share u - 1, the others begin shares u,
+// u + 1, ..; n parts in all
 struct Cut {
-  int a, slot, n, lq, lk, start;
+  int hs, u, n, a, lq, start, pad0, pad1;
 };
 struct PlanHead {
-  int items, cuts;
+  // rounds: whole blocks of a workgroup before its share; shares 0: no block is cut, a
+  // workgroup takes one block
+  int blocks, shares, cuts, rounds;
+};
+
+// Workgroup w of the grid runs on XCD w % 8. The key heads are spread over the XCDs, in g
+// classes (g the greatest common divisor of their number and 8); the 8 / g XCDs of a class take
+// its heads one after the other, whose keys then stay in their L2.
+struct Classes {
+  int g, heads;  // heads of a class
+  int held;      // workgroups of a class that run at a time
+  static Classes of(int Hk, int per_unit) {
+    int g = 8;
+    while (Hk % g) g /= 2;
+    return Classes{g, Hk / g, 8 / g * kXcdUnits * per_unit};
+  }
 };
 
 // Bounds that the host knows, and where things lie in the workspace
 struct Plan {
-  int rows;                           // of a block
-  int blocks, share, items, slots;    // at most, for one key head; share: parts that blocks
-                                      // are cut for
-  int cuts;
-  size_t item_at, cut_at, part_at, bytes;
+  int rows;        // of a block
+  int slot_waves;  // wavefronts of a block that have rows, at most
+  int blocks;      // at most, for one key head
+  size_t block_at, share_at, cut_at, part_at, bytes;
 };
 
 // Positions of a block's first and last row (a sequence has fewer than 2^30 rows)
@@ -57,33 +84,24 @@ struct BlockSpan {
   }
 };
 
-// Sums of x and y over the threads before this one, and over all of them
-struct Pair {
-  int x, y;
-};
-__device__ __forceinline__ Pair plan_scan(int x, int y, Pair (&sums)[kPlan / 64], Pair* total) {
+// Sum of x over the threads before this one, and over all of them
+__device__ __forceinline__ int64_t plan_scan(int64_t x, int64_t (&sums)[kPlan / 64],
+                                             int64_t* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int a = x, b = y;
+  int64_t in = x;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int c = __shfl_up(a, o, 64), d = __shfl_up(b, o, 64);
-    if (lane >= o) {
-      a += c;
-      b += d;
-    }
+    const int64_t y = __shfl_up(in, o, 64);
+    if (lane >= o) in += y;
   }
   __syncthreads();  // the sums of a scan before are read
-  if (lane == 63) sums[w] = Pair{a, b};
+  if (lane == 63) sums[w] = in;
   __syncthreads();
-  Pair before{a - x, b - y}, all{0, 0};
+  int64_t before = in - x, all = 0;
 #pragma unroll
   for (int i = 0; i < kPlan / 64; ++i) {
-    if (i < w) {
-      before.x += sums[i].x;
-      before.y += sums[i].y;
-    }
-    all.x += sums[i].x;
-    all.y += sums[i].y;
+    if (i < w) before += sums[i];
+    all += sums[i];
   }
   *total = all;
   return before;
@@ -98,122 +116,139 @@ __device__ __forceinline__ int plan_find(const int* list, int i) {
   return lo;
 }
 
-// One workgroup: blocks by sequence, the last one (with most keys, if causal) first. A pass
-// counts the tiles, another one cuts and writes the items, thread by item.
+// One workgroup: lists the blocks by sequence, the last one (with most keys, if causal)
+// first, then cuts their tiles into equal shares.
 __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, const Plan L,
-                                                           char* ws) {
-  __shared__ Pair sums[kPlan / 64];
-  __shared__ int64_t tiles_of[kPlan / 64];
-  // of a sequence: its first block; of a block: its first item
+                                                           const Classes C, char* ws) {
+  __shared__ int64_t sums[kPlan / 64];
+  __shared__ int most_of[kPlan / 64];
   __shared__ int first[kPlan], s_n[kPlan], s_lq[kPlan], s_lk[kPlan], s_start[kPlan];
-  __shared__ int b_item[kPlan], b_seq[kPlan], b_a[kPlan], b_tiles[kPlan], b_slot[kPlan];
-  PlanHead* head = (PlanHead*)ws;
-  Item* items = (Item*)(ws + L.item_at);
+  __shared__ int64_t index[kIndex];  // cost of every 2^step-th block
+  __shared__ int n_cuts;
+  Block* list = (Block*)(ws + L.block_at);
+  Share* shares = (Share*)(ws + L.share_at);
   Cut* cuts = (Cut*)(ws + L.cut_at);
   const int tid = threadIdx.x;
-  int64_t tiles_seen = 0;
-  int n_items = 0, n_slots = 0, n_cuts = 0, part = 1;
-  for (int pass = 0; pass < 2; ++pass) {
-    int seen = 0;  // blocks so far: no more than the host counted
-    for (int b0 = 0; b0 < P.B && seen < L.blocks; b0 += kPlan) {
-      const int b = b0 + tid;
-      int n = 0;
-      if (b < P.B) {
-        const int start = P.start(b), lq = max(0, P.start(b + 1) - start);
-        s_start[tid] = start;
-        s_lq[tid] = lq;
-        s_lk[tid] = P.klen(b);
-        s_n[tid] = n = (int)(((uint32_t)lq * (uint32_t)P.G + L.rows - 1) / (uint32_t)L.rows);
-      }
-      Pair total;
-      const Pair before = plan_scan(min(n, L.blocks), 0, sums, &total);
-      // (unsigned: the sum of starts that do not ascend may pass 2^31)
-      const int blocks = (int)min((uint32_t)total.x, (uint32_t)(L.blocks - seen));
-      first[tid] = (int)min((uint32_t)before.x, (uint32_t)INT32_MAX);
-      __syncthreads();
-      for (int i0 = 0; i0 < blocks; i0 += kPlan) {
-        const int i = i0 + tid;
-        int tiles = 0, parts = 0, lo = 0, a = 0;
-        if (i < blocks) {
-          lo = plan_find(first, i);
-          a = s_n[lo] - 1 - (i - first[lo]);
-          const BlockSpan s(a, L.rows, P.G, s_lq[lo], s_lk[lo]);
-          tiles = visible_tiles<KT>(P.m, s.p0, s.p1, s_lk[lo]).n;
-          parts = max(1, (tiles + part - 1) / part);
-        }
-        if (pass == 0) {
-          tiles_seen += tiles;
-          continue;
-        }
-        const Pair at = plan_scan(parts, parts > 1 ? 1 : 0, sums, &total);
-        // slots count the parts of cut blocks: all items but those of whole ones
-        const int slot = n_slots + at.x - (tid - at.y), cut = n_cuts + at.y;
-        b_item[tid] = at.x;
-        b_seq[tid] = lo;
-        b_a[tid] = a;
-        b_tiles[tid] = tiles;
-        b_slot[tid] = parts > 1 ? slot : -1;
-        // (the host's bounds hold for ascending starts; nothing is written outside them)
-        if (parts > 1 && cut < L.cuts && slot + parts <= L.slots)
-          cuts[cut] = Cut{a, slot, parts, s_lq[lo], s_lk[lo], s_start[lo]};
-        __syncthreads();
-        const int some = min(kPlan, blocks - i0);
-        for (int j = tid; j < total.x; j += kPlan) {
-          const int x = min(plan_find(b_item, j), some - 1), y = j - b_item[x], q = b_seq[x];
-          const int all = (x + 1 < some ? b_item[x + 1] : total.x) - b_item[x];
-          const int per = (b_tiles[x] + all - 1) / all, t0 = min(b_tiles[x], y * per);
-          const int z = b_slot[x] < 0 ? -1 : b_slot[x] + y;
-          if (n_items + j < L.items && z < L.slots)
-            items[n_items + j] = Item{b0 + q, b_a[x], t0, min(b_tiles[x], t0 + per), z,
-                                      s_lq[q], s_lk[q], s_start[q]};
-        }
-        n_items += total.x;
-        n_cuts += total.y;
-        n_slots += total.x - (some - total.y);
-      }
-      seen += blocks;
-      __syncthreads();  // the segment's lists are read
+  int step = 0;
+  while ((L.blocks >> step) >= kIndex) ++step;
+  int64_t cost = 0;
+  int seen = 0, longest = 0;  // seen: blocks so far, no more than the host counted
+  for (int b0 = 0; b0 < P.B && seen < L.blocks; b0 += kPlan) {
+    const int b = b0 + tid;
+    int n = 0;
+    if (b < P.B) {
+      const int start = P.start(b), lq = max(0, P.start(b + 1) - start);
+      s_start[tid] = start;
+      s_lq[tid] = lq;
+      s_lk[tid] = P.klen(b);
+      s_n[tid] = n = (int)(((uint32_t)lq * (uint32_t)P.G + L.rows - 1) / (uint32_t)L.rows);
     }
-    if (pass == 0) {
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) tiles_seen += __shfl_xor(tiles_seen, o, 64);
-      if ((tid & 63) == 0) tiles_of[tid >> 6] = tiles_seen;
-      __syncthreads();
-      int64_t all = 0;
-#pragma unroll
-      for (int x = 0; x < kPlan / 64; ++x) all += tiles_of[x];
-      part = (int)min(max((int64_t)kPartTiles, (all + L.share - 1) / L.share), (int64_t)1 << 25);
+    int64_t total;
+    const int64_t before = plan_scan(n, sums, &total);
+    const int blocks = (int)min(total, (int64_t)(L.blocks - seen));
+    first[tid] = (int)min(before, (int64_t)INT32_MAX);
+    __syncthreads();
+    for (int i0 = 0; i0 < blocks; i0 += kPlan) {
+      const int i = i0 + tid;
+      int tiles = 0, lo = 0, a = 0;
+      if (i < blocks) {
+        lo = plan_find(first, i);
+        a = s_n[lo] - 1 - (i - first[lo]);
+        const BlockSpan s(a, L.rows, P.G, s_lq[lo], s_lk[lo]);
+        tiles = visible_tiles<KT>(P.m, s.p0, s.p1, s_lk[lo]).n;
+        longest = max(longest, tiles + kStart);
+      }
+      const int64_t c = cost + plan_scan(i < blocks ? tiles + kStart : 0, sums, &total);
+      if (i < blocks) {
+        list[seen + i] = Block{b0 + lo, a, tiles, s_lq[lo], s_lk[lo], s_start[lo], c};
+        if (((seen + i) & ((1 << step) - 1)) == 0) index[(seen + i) >> step] = c;
+      }
+      cost += total;
     }
+    seen += blocks;
+    __syncthreads();  // the segment's lists are read
   }
-  if (tid == 0) {
-    head->items = min(n_items, L.items);
-    head->cuts = min(n_cuts, L.cuts);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+  if ((tid & 63) == 0) most_of[tid >> 6] = longest;
+  if (tid == 0) n_cuts = 0;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kPlan / 64; ++x) longest = max(longest, most_of[x]);
+  const int64_t all = cost * C.heads;
+  const int64_t share = all / C.held;
+  const int rounds = seen == 0 ? kRounds : (int)min((int64_t)kRounds, share / longest);
+  const bool whole = rounds == kRounds;
+  const int n = rounds > 0 ? C.held
+                           : (int)min((int64_t)C.held, (all + kShareTiles - 1) / kShareTiles);
+  if (tid == 0) *(PlanHead*)ws = PlanHead{seen, whole ? 0 : n, 0, whole ? 1 : rounds};
+  if (whole) return;
+  // cost of the class's blocks before the i-th
+  auto cost_of = [&](int i) {
+    const int h = i / seen;
+    return h * cost + list[i - h * seen].cost;
+  };
+  for (int u = tid; u <= n; u += kPlan) {
+    Share s{C.heads, 0, 0, 0};
+    if (u < n) {
+      // all workgroups' whole blocks, what the shares before leave to be done by the
+      // workgroups before u beside their own whole blocks
+      int64_t pos = all * u / n;
+      if (rounds > 0) {
+        pos += cost_of(rounds * C.held);
+        for (int k = 0; k < rounds; ++k) pos -= cost_of(k * C.held + u) - cost_of(k * C.held);
+      }
+      s.hs = (int)(pos / cost);
+      const int64_t off = pos - s.hs * cost;
+      int lo = 0, hi = ((seen - 1) >> step) + 1;  // index[lo] <= off < index[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (index[mid] <= off)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      hi = min((lo + 1) << step, seen);
+      lo <<= step;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (list[mid].cost <= off)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      const int tiles = list[lo].tiles;
+      s.block = lo;
+      s.t = max(0, (int)(off - list[lo].cost) - kStart);
+      if (s.t < kSnap) s.t = 0;
+      if (s.t > 0 && tiles - s.t < kSnap) {  // at the next block's beginning instead
+        s.t = 0;
+        if (++s.block == seen) {
+          s.block = 0;
+          ++s.hs;
+        }
+      }
+    }
+    shares[u] = s;
   }
+  __syncthreads();
+  for (int u = 1 + tid; u < n; u += kPlan) {
+    const Share s = shares[u], p = shares[u - 1];
+    if (s.t == 0 || (p.t > 0 && p.hs == s.hs && p.block == s.block)) continue;
+    int lo = u, hi = n;  // share lo begins in the block, share hi after it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (shares[mid].hs == s.hs && shares[mid].block == s.block)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const Block b = list[s.block];
+    cuts[atomicAdd(&n_cuts, 1)] = Cut{s.hs, u, lo - u + 2, b.a, b.lq, b.start, 0, 0};
+  }
+  __syncthreads();
+  if (tid == 0) ((PlanHead*)ws)->cuts = n_cuts;
 }
-
-// Workgroup w of the grid runs on XCD w % 8. The key heads are spread over the XCDs,
-// each of which then works on one head at a time, whose keys stay in its L2; where
-// the heads' number and 8 have g as their greatest common divisor, 8 / g XCDs share a
-// head, neighbouring items on different ones.
-struct ItemOrder {
-  int g, slots;  // slots: heads of an XCD
-  static ItemOrder of(int Hk) {
-    int g = 8;
-    while (Hk % g) g /= 2;
-    return ItemOrder{g, Hk / g};
-  }
-  int64_t grid(int items) const { return (int64_t)8 * slots * ((items + 8 / g - 1) / (8 / g)); }
-  __device__ __forceinline__ bool at(int wg, int items, int* item, int* hk) const {
-    const int r = 8 / g, x = wg & 7, s = wg >> 3, per = (items + r - 1) / r;
-    if (per == 0) return false;
-    const int hs = s / per;
-    *item = (s - hs * per) * r + x / g;
-    *hk = hs * g + x % g;
-    return hs < slots && *item < items;
-  }
-};
-
-// ---- bf16 ---------------------------------------------------------------------------------
 
 // n / d for 0 <= n < 2^30, d < 2^30
 struct FastDiv {
@@ -228,6 +263,110 @@ struct FastDiv {
     return (int)(((uint64_t)(uint32_t)n * m) >> s);
   }
 };
+
+// What the attention kernels are called with. They read it anew for each piece of work and after
+// its walk (args()): kept in registers over the walk, which needs nearly all that there are,
+// it would be spilled.
+struct ChunkArgs {
+  ChunkProb P;
+  Plan L;
+  Classes C;
+  FastDiv by_page;
+  float sl2;
+  const void *q, *kp, *vp;
+  void* out;
+  float* lse;
+  char* ws;
+};
+typedef const __attribute__((address_space(4))) ChunkArgs* Args;
+__device__ __forceinline__ Args args() {
+  Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();  // the only argument
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
+// Tiles [t0, t1) of a block. slot: where the softmax state of a part goes, -1 for a whole block.
+struct Piece {
+  int b, a, t0, t1, slot, lq, lk, start;
+};
+// The pieces of a workgroup's share, one after the other
+struct Pieces {
+  // (from the constant address space: scalar loads of what the launch before wrote)
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  typedef const __attribute__((address_space(4))) i32x8* Blocks;
+  typedef const __attribute__((address_space(4))) i32x4* Heads;
+  int hs, block, t, hs1, block1, t1;  // from here to there
+  int k, u, cls;
+
+  static __device__ __forceinline__ i32x4 plan_head() { return *(Heads)args()->ws; }  // PlanHead
+  // false: no work
+  __device__ __forceinline__ bool first() {
+    const Args A = args();
+    const int g = A->C.g;
+    cls = (blockIdx.x & 7) % g;
+    u = (blockIdx.x >> 3) * (8 / g) + (blockIdx.x & 7) / g;
+    k = -1;
+    const i32x4 h = plan_head();
+    return h[0] > 0 && (h[1] == 0 || u < h[1]) && range();
+  }
+  // the next whole block, or the share
+  __device__ __forceinline__ bool range() {
+    const Args A = args();
+    const i32x4 h = plan_head();
+    if (++k < h[3]) {
+      const int i = k * A->C.held + u;
+      hs = i / h[0];
+      block = i - hs * h[0];
+      t = 0;
+      hs1 = hs;
+      block1 = block + 1;
+      t1 = 0;
+      return hs < A->C.heads;
+    }
+    if (k > h[3] || h[1] == 0) return false;
+    const Heads shares = (Heads)(A->ws + A->L.share_at);
+    const i32x4 a = shares[u], z = shares[u + 1];
+    hs = a[0];
+    block = a[1];
+    t = a[2];
+    hs1 = z[0];
+    block1 = z[1];
+    t1 = z[2];
+    return more();
+  }
+  __device__ __forceinline__ bool more() const {
+    return hs < hs1 || (hs == hs1 && (block < block1 || (block == block1 && t < t1)));
+  }
+  __device__ __forceinline__ int head() const { return hs * args()->C.g + cls; }
+  __device__ __forceinline__ Piece piece() const {
+    const Args A = args();
+    const i32x8 x = ((Blocks)(A->ws + A->L.block_at))[block];  // Block
+    const int end = hs == hs1 && block == block1 ? t1 : x[2];
+    return Piece{x[0], x[1], t, end, t == 0 && end == x[2] ? -1 : 2 * u + (t == 0), x[3], x[4], x[5]};
+  }
+  __device__ __forceinline__ bool next() {
+    if (hs == hs1 && block == block1) {
+      t = t1;  // the end
+    } else {
+      t = 0;
+      if (++block == plan_head()[0] && hs < hs1) {
+        block = 0;
+        ++hs;
+      }
+    }
+    return more() || range();
+  }
+};
+
+// State of a part, wavefront by wavefront as its lanes hold it: `chunks` times four sums a
+// lane, its row's reference (log2 units) and sum of exponentials
+__device__ __forceinline__ float* part_wave(char* parts, int held, int slot_waves, int cls, int slot,
+                                            int w, int chunks) {
+  return (float*)parts + (((size_t)cls * 2 * held + slot) * slot_waves + w) * (64 * (4 * chunks + 2));
+}
+
+// ---- bf16 ---------------------------------------------------------------------------------
 
 __device__ __forceinline__ void lds_dma16_at(const void* p, uint32_t lds) {
   uint32_t saved;
@@ -357,188 +496,198 @@ struct PagedTiles : WalkRows {
 
 template <int D, bool GROUPS>
 __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
-    const ChunkProb P, const Plan L, const ItemOrder order, const FastDiv by_page,
-    const bf16* __restrict__ q, const bf16* __restrict__ kp, const bf16* __restrict__ vp,
-    bf16* __restrict__ out, float* __restrict__ lse, char* __restrict__ ws, float sl2) {
+    const ChunkArgs) {
   constexpr int KS = D / 16, DT = D / 32, RB = 2 * D, TILE = KT * RB;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];  // two tiles of keys, two of values
   __shared__ __attribute__((aligned(8))) uint16_t hole[2][4];
   __shared__ int redo;
-  int item, hk;
-  if (!order.at(blockIdx.x, ((const PlanHead*)ws)->items, &item, &hk)) return;
-  const Item it = ((const Item*)(ws + L.item_at))[item];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int off = it.lk - it.lq, r0 = it.a * kWalkRows, rows = it.lq * P.G;
-  const BlockSpan span(it.a, kWalkRows, P.G, it.lq, it.lk);
-  const int w0 = r0 + 32 * w, wreal = max(0, min(32, rows - w0));
-  const int row = min(w0 + min(l32, max(wreal, 1) - 1), rows - 1);  // this lane's row
-  const int tok = row / P.G, head = hk * P.G + row - tok * P.G;
-  const int wl = min(w0 + max(wreal, 1) - 1, rows - 1);
-  PagedTiles<D, GROUPS> T;
-  T.mask = P.m;
-  T.list = visible_tiles<KT>(P.m, span.p0, span.p1, it.lk);
-  T.t0 = it.t0;
-  T.t1 = it.t1;
-  T.lk = it.lk;
-  T.ra = visible_keys(P.m, min(w0, rows - 1) / P.G + off, it.lk);
-  T.rz = visible_keys(P.m, wl / P.G + off, it.lk);
-  T.pos = tok + off;
-  T.real = wreal;
-  T.block_first = span.p0;
-  T.block_last = span.p1;
-  T.kh = kp + hk * P.k_sh;
-  T.vh = vp + hk * P.v_sh;
-  T.table = P.table + it.b * P.table_sb;
-  T.k_sp = P.k_sp;
-  T.k_st = P.k_st;
-  T.v_sp = P.v_sp;
-  T.v_st = P.v_st;
-  T.page = P.page;
-  T.pages = P.pages;
-  T.most = P.max_pages - 1;
-  T.by_page = by_page;
-  T.smem = smem;
-  T.hole = hole;
-  T.lds0 = lds_addr(smem);
-  T.w = w;
-  T.lane = lane;
-  T.ev = T.ek = 0;
+  Pieces S;
+  for (bool go = S.first(); go; go = S.next()) {
+    const Piece it = S.piece();
+    const int hk = S.head();
+    __syncthreads();  // every wavefront is past the piece before
+    const Args A = args();
+    const int G = A->P.G, off = it.lk - it.lq, rows = it.lq * G;
+    const int w0 = it.a * kWalkRows + 32 * w, wreal = max(0, min(32, rows - w0));
+    // the wavefront's last row, this lane's
+    const int wl = min(w0 + max(wreal, 1), rows) - 1, row = min(w0 + l32, wl);
+    const BlockSpan span(it.a, kWalkRows, G, it.lq, it.lk);
+    PagedTiles<D, GROUPS> T;
+    T.mask = WinMask{A->P.m.left, A->P.m.right, A->P.m.sinks, A->P.m.causal};
+    T.list = visible_tiles<KT>(T.mask, span.p0, span.p1, it.lk);
+    T.t0 = it.t0;
+    T.t1 = it.t1;
+    T.lk = it.lk;
+    T.ra = visible_keys(T.mask, min(w0, wl) / G + off, it.lk);
+    T.rz = visible_keys(T.mask, wl / G + off, it.lk);
+    T.pos = row / G + off;
+    T.real = wreal;
+    T.block_first = span.p0;
+    T.block_last = span.p1;
+    T.kh = (const bf16*)A->kp + hk * A->P.k_sh;
+    T.vh = (const bf16*)A->vp + hk * A->P.v_sh;
+    T.table = A->P.table + it.b * A->P.table_sb;
+    T.k_sp = A->P.k_sp;
+    T.k_st = A->P.k_st;
+    T.v_sp = A->P.v_sp;
+    T.v_st = A->P.v_st;
+    T.page = A->P.page;
+    T.pages = A->P.pages;
+    T.most = A->P.max_pages - 1;
+    T.by_page = FastDiv{A->by_page.m, A->by_page.s};
+    T.smem = smem;
+    T.hole = hole;
+    T.lds0 = lds_addr(smem);
+    T.w = w;
+    T.lane = lane;
+    T.ev = T.ek = 0;
 
-  bf16x8 qreg[KS];
-  {
-    const bf16* src = q + (it.start + tok) * P.q_st + head * P.q_sh;
+    bf16x8 qreg[KS];
+    {
+      const int tok = row / G, head = hk * G + row - tok * G;
+      const bf16* src = (const bf16*)A->q + (it.start + tok) * A->P.q_st + head * A->P.q_sh;
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) qreg[kk] = *(const bf16x8*)(src + 16 * kk + 8 * h);
-  }
-  // Retire the loads here (a wait the compiler sees), so that no vmcnt wait of
-  // theirs lands in the loop, where it would also wait for the copies in flight.
-  __builtin_amdgcn_s_waitcnt(kWalkVmcnt0);
-  if (tid == 0) redo = 0;  // ordered before any write by the barriers of the tiles
-  f32x16 oacc[DT];
-  float m, l_tot;
-  walk_bf16<D>(T, smem, &redo, qreg, sl2, w, lane, oacc, m, l_tot);
-  if (it.slot >= 0) {
-    // A sum far above its reference goes out against a reference at its own size: the
-    // joining compares references, and adds up as many sums as there are parts
-    const int up = l_tot > 0x1p22f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
-    m += (float)up;
-    l_tot = __builtin_amdgcn_ldexpf(l_tot, -up);
-    if (l32 >= wreal) return;
-    float* x = (float*)(ws + L.part_at) +
-               (((size_t)hk * L.slots + it.slot) * L.rows + 32 * w + l32) * (D + 4);
+      for (int kk = 0; kk < KS; ++kk) qreg[kk] = *(const bf16x8*)(src + 16 * kk + 8 * h);
+    }
+    // Retire the loads here (a wait the compiler sees), so that no vmcnt wait of
+    // theirs lands in the loop, where it would also wait for the copies in flight.
+    __builtin_amdgcn_s_waitcnt(kWalkVmcnt0);
+    if (tid == 0) redo = 0;  // ordered before any write by the barriers of the tiles
+    f32x16 oacc[DT];
+    float m, l_tot;
+    walk_bf16<D>(T, smem, &redo, qreg, A->sl2, w, lane, oacc, m, l_tot);
+    const Args B = args();
+    if (it.slot >= 0) {
+      if (wreal == 0) continue;
+      // A sum far above its reference goes out against a reference at its own size: the
+      // joining compares references, and adds up as many sums as there are parts
+      const int up = l_tot > 0x1p22f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
+      float* x = part_wave(B->ws + B->L.part_at, B->C.held, B->L.slot_waves, S.cls, it.slot, w, D / 8) +
+                 4 * lane;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 y;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_ldexpf(oacc[dt][4 * g + j], -up);
+          *(f32x4*)(x + 256 * (4 * dt + g)) = y;
+        }
+      x += 32 * D - 3 * lane;
+      x[0] = m + (float)up;
+      x[64] = __builtin_amdgcn_ldexpf(l_tot, -up);
+      continue;
+    }
+    if (l32 >= wreal) continue;
+    const bool any = l_tot != 0.f;
+    const float inv = any ? 1.f / l_tot : 0.f;
+    const int tok = row / G, head = hk * G + row - tok * G;
+    bf16* orow = (bf16*)B->out + (it.start + tok) * B->P.o_st + head * B->P.o_sh;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        f32x4 y;
+        bf16x4 x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = __builtin_amdgcn_ldexpf(oacc[dt][4 * g + j], -up);
-        *(f32x4*)(x + 32 * dt + 8 * g + 4 * h) = y;
+        for (int j = 0; j < 4; ++j) x[j] = f2bf(any ? oacc[dt][4 * g + j] * inv : 0.f);
+        *(bf16x4*)(orow + 32 * dt + 8 * g + 4 * h) = x;
       }
-    if (h == 0) {
-      x[D] = m;
-      x[D + 1] = l_tot;
-    }
-    return;
+    if (B->lse && h == 0)
+      B->lse[(size_t)(it.start + tok) * B->P.H + head] =
+          any ? (m + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
   }
-  if (l32 >= wreal) return;
-  const bool any = l_tot != 0.f;
-  const float inv = any ? 1.f / l_tot : 0.f;
-  bf16* orow = out + (it.start + tok) * P.o_st + head * P.o_sh;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      bf16x4 x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = f2bf(any ? oacc[dt][4 * g + j] * inv : 0.f);
-      *(bf16x4*)(orow + 32 * dt + 8 * g + 4 * h) = x;
-    }
-  if (lse && h == 0)
-    lse[(size_t)(it.start + tok) * P.H + head] =
-        any ? (m + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
 }
 
 // ---- joining the parts --------------------------------------------------------------------
 
-// A row's parts are read 16 bytes a lane, D / 4 lanes a part, by one wavefront where there
-// are few of them, by the four of the workgroup where there are many. The workgroups take
-// groups of four rows (few parts) or a row (many) one after the other.
-constexpr int kJoinGrid = 2048, kFewParts = 16;
+// A workgroup joins the rows of one wavefront, lanes as they were in the attention. Of few
+// parts its wavefronts take a quarter of the chunks each, of many every fourth part, and the
+// quarters are workgroups of their own.
+constexpr int kJoinGrid = 8192, kFewParts = 8;
 
-template <typename T, int DP>
+template <typename T, int D>
 __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, const Plan L,
-                                                         const char* __restrict__ ws,
+                                                         const Classes C, char* __restrict__ ws,
                                                          T* __restrict__ out,
                                                          float* __restrict__ lse) {
-  constexpr int LP = DP / 4, NP = 64 / LP;  // lanes of a part, parts of a wavefront's read
-  __shared__ float acc[4][DP], wmax[4], wsum[4];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int t = 4 * (lane % LP), stride = P.d + 4, n_cuts = ((const PlanHead*)ws)->cuts;
-  const size_t next = (size_t)L.rows * stride;
-  for (int c = blockIdx.x; c < n_cuts * P.Hk * (L.rows / 4); c += gridDim.x) {
-    const int rq = c % (L.rows / 4), x = c / (L.rows / 4), hk = x / n_cuts;
-    const Cut cut = ((const Cut*)(ws + L.cut_at))[x - hk * n_cuts];
-    const int r0 = cut.a * L.rows, real = min(L.rows, cut.lq * P.G - r0);
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int CH = BF ? D / 8 : D / 16, JC = CH < 4 ? 1 : CH / 4;
+  constexpr int WR = BF ? 32 : 16, NG = CH / JC;  // rows of a wavefront, groups of chunks
+  __shared__ __attribute__((aligned(16))) f32x4 acc[4][JC][64];
+  __shared__ float ms[4][64], ls[4][64];
+  const int lane = threadIdx.x & 63, lr = lane % WR;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_cuts = ((const PlanHead*)ws)->cuts, each = L.slot_waves * NG;
+  for (int c = blockIdx.x; c < n_cuts * C.g * each; c += gridDim.x) {
+    // (groups go slowest: of few parts the first n_cuts * g * slot_waves have work)
+    const int gr = c / (n_cuts * C.g * L.slot_waves), x = c - gr * n_cuts * C.g * L.slot_waves;
+    const int y = x / L.slot_waves, wv = x - y * L.slot_waves, cls = y / n_cuts;
+    const Cut cut = ((const Cut*)(ws + L.cut_at))[y - cls * n_cuts];
+    const int row = cut.a * L.rows + wv * WR + lr, rows = cut.lq * P.G;
     const bool few = cut.n <= kFewParts;
-    for (int r = 4 * rq + (few ? w : 0); r < min(real, 4 * rq + 4); r += few ? 4 : 1) {
-      const float* p = (const float*)(ws + L.part_at) +
-                       (((size_t)hk * L.slots + cut.slot) * L.rows + r) * stride;
-      // each lane's own parts against their own maximum, then all against the largest
-      float mx = -INFINITY, sum = 0.f;
-      f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    // the wavefront had no rows; another workgroup's, or wavefront's
+    if (row - lr >= rows || (few && gr > 0)) continue;
+    const int j0 = (few ? w : gr) * JC;
+    float m = -INFINITY, l = 0.f;
+    f32x4 a[JC];
+#pragma unroll
+    for (int j = 0; j < JC; ++j) a[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto merge = [&](float m2, float l2, const f32x4* v) __attribute__((always_inline)) {
+      // no key of the part is there: its reference is not one
+      const float m1 = l2 == 0.f ? m : fmaxf(m, m2), ref = m1 == -INFINITY ? 0.f : m1;
+      const float f = __builtin_amdgcn_exp2f(m - ref);
+      const float h = l2 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m2 - ref);
+      l = l * f + l2 * h;
+#pragma unroll
+      for (int j = 0; j < JC; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[j][e] = a[j][e] * f + v[j][e] * h;
+      m = m1;
+    };
+    // part 0 lies in slot 2 u - 1, parts 1, 2, .. in slots 2 u, 2 u + 2, ..
+    if (!few || w < NG) {
 #pragma unroll 4
-      for (int i = (few ? 0 : w * NP) + lane / LP; i < cut.n; i += few ? NP : 4 * NP) {
-        const float* y = p + i * next;
-        const f32x4 v = t < P.d ? *(const f32x4*)(y + t) : f32x4{0.f, 0.f, 0.f, 0.f};
-        const float m = y[P.d], s = y[P.d + 1];
-        // no key of the part is there: its reference is not one
-        const float m1 = s == 0.f ? mx : fmaxf(mx, m);
-        const float ref = m1 == -INFINITY ? 0.f : m1;
-        const float f = s == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-        const float g = __builtin_amdgcn_exp2f(mx - ref);
-        sum = sum * g + s * f;
+      for (int i = few ? 0 : w; i < cut.n; i += few ? 1 : 4) {
+        const float* p = part_wave(ws + L.part_at, C.held, L.slot_waves, cls,
+                                   2 * (cut.u + i - 1) + (i == 0), wv, CH);
+        f32x4 v[JC];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a[e] = a[e] * g + v[e] * f;
-        mx = m1;
+        for (int j = 0; j < JC; ++j) v[j] = *(const f32x4*)(p + 256 * (j0 + j) + 4 * lane);
+        merge(p[256 * CH + lane], p[256 * CH + 64 + lane], v);
       }
-      auto merge = [&](float m2, float s2, f32x4 a2) __attribute__((always_inline)) {
-        const float m1 = fmaxf(mx, m2), ref = m1 == -INFINITY ? 0.f : m1;
-        const float f = __builtin_amdgcn_exp2f(mx - ref), g = __builtin_amdgcn_exp2f(m2 - ref);
-        sum = sum * f + s2 * g;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) a[e] = a[e] * f + a2[e] * g;
-        mx = m1;
-      };
-#pragma unroll
-      for (int o = LP; o < 64; o <<= 1) {
-        const f32x4 b = {__shfl_xor(a[0], o, 64), __shfl_xor(a[1], o, 64), __shfl_xor(a[2], o, 64),
-                         __shfl_xor(a[3], o, 64)};
-        merge(__shfl_xor(mx, o, 64), __shfl_xor(sum, o, 64), b);
-      }
-      if (!few) {
-        __syncthreads();  // the row before is read
-        if (lane < LP) *(f32x4*)&acc[w][t] = a;
-        if (lane == 0) {
-          wmax[w] = mx;
-          wsum[w] = sum;
-        }
-        __syncthreads();
-        if (w > 0) continue;
-#pragma unroll
-        for (int i = 1; i < 4; ++i) merge(wmax[i], wsum[i], *(const f32x4*)&acc[i][t]);
-      }
-      if (lane >= LP) continue;
-      const int row = r0 + r, tok = row / P.G, h = hk * P.G + row - tok * P.G;
-      T* o = out + (cut.start + tok) * P.o_st + h * P.o_sh + t;
-      if (t < P.d)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) store_f(o + e, sum != 0.f ? a[e] / sum : 0.f);
-      if (lse && lane == 0)
-        lse[(size_t)(cut.start + tok) * P.H + h] =
-            sum != 0.f ? (mx + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     }
+    if (!few) {
+      __syncthreads();  // the states before are read
+      if (w > 0) {
+#pragma unroll
+        for (int j = 0; j < JC; ++j) acc[w][j][lane] = a[j];
+        ms[w][lane] = m;
+        ls[w][lane] = l;
+      }
+      __syncthreads();
+      if (w > 0) continue;
+      for (int i = 1; i < 4; ++i) {
+        f32x4 v[JC];
+#pragma unroll
+        for (int j = 0; j < JC; ++j) v[j] = acc[i][j][lane];
+        merge(ms[i][lane], ls[i][lane], v);
+      }
+    }
+    if (row >= rows || (few && w >= NG)) continue;
+    const int tok = row / P.G, h = (cut.hs * C.g + cls) * P.G + row - tok * P.G;
+    T* o = out + (cut.start + tok) * P.o_st + h * P.o_sh;
+#pragma unroll
+    for (int j = 0; j < JC; ++j) {
+      const int dim = 4 * (64 / WR * (j0 + j) + lane / WR);
+      if (dim < P.d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_f(o + dim + e, l != 0.f ? a[j][e] / l : 0.f);
+    }
+    if (lse && j0 == 0 && lane < WR)
+      lse[(size_t)(cut.start + tok) * P.H + h] =
+          l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   }
 }
 
@@ -553,272 +702,280 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 
 template <int DP, int WAVES>
 __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
-    const ChunkProb P, const Plan L, const ItemOrder order, const FastDiv by_page,
-    const float* __restrict__ q, const float* __restrict__ kp, const float* __restrict__ vp,
-    float* __restrict__ out, float* __restrict__ lse, char* __restrict__ ws, float sl2) {
+    const ChunkArgs) {
   constexpr int HK = 32, NJ = DP / 16, LD = DP + 4, NC = DP / 4;
   constexpr int RP = 256 / NC, NP = HK / RP;  // rows of a pass of the copy, passes
   __shared__ __attribute__((aligned(16))) float ks[2][HK][LD], vs[2][HK][LD];
   __shared__ uint32_t gone[4], bad[4];  // keys not there, values that are not finite
-  int item, hk;
-  if (!order.at(blockIdx.x, ((const PlanHead*)ws)->items, &item, &hk)) return;
-  const Item it = ((const Item*)(ws + L.item_at))[item];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int off = it.lk - it.lq, r0 = it.a * kF32Rows, rows = it.lq * P.G;
-  const BlockSpan span(it.a, kF32Rows, P.G, it.lq, it.lk);
-  const TileList list = visible_tiles<KT>(P.m, span.p0, span.p1, it.lk);
-  const int w0 = r0 + 16 * w, wreal = max(0, min(16, rows - w0));
-  const int wl = min(w0 + max(wreal, 1) - 1, rows - 1);
-  const int row = min(w0 + l16, wl);  // this lane's row
-  const int tok = row / P.G, head = hk * P.G + row - tok * P.G;
-  const KeyRange ra = visible_keys(P.m, min(w0, rows - 1) / P.G + off, it.lk);
-  const KeyRange rz = visible_keys(P.m, wl / P.G + off, it.lk);
-  const KeyRange mine = visible_keys(P.m, tok + off, it.lk);
+  Pieces S;
+  for (bool go = S.first(); go; go = S.next()) {
+    const Piece it = S.piece();
+    const int hk = S.head();
+    __syncthreads();  // every wavefront is past the piece before
+    const Args A = args();
+    const int G = A->P.G, d = A->P.d, off = it.lk - it.lq, rows = it.lq * G;
+    const WinMask mask{A->P.m.left, A->P.m.right, A->P.m.sinks, A->P.m.causal};
+    const BlockSpan span(it.a, kF32Rows, G, it.lq, it.lk);
+    const TileList list = visible_tiles<KT>(mask, span.p0, span.p1, it.lk);
+    const int w0 = it.a * kF32Rows + 16 * w, wreal = max(0, min(16, rows - w0));
+    // the wavefront's last row, this lane's
+    const int wl = min(w0 + max(wreal, 1), rows) - 1, row = min(w0 + l16, wl);
+    const KeyRange ra = visible_keys(mask, min(w0, wl) / G + off, it.lk);
+    const KeyRange rz = visible_keys(mask, wl / G + off, it.lk);
+    const KeyRange mine = visible_keys(mask, row / G + off, it.lk);
+    const float sl2 = A->sl2;
 
-  f32x4 qf[NJ];
-  {
-    const float* src = q + (it.start + tok) * P.q_st + head * P.q_sh;
+    f32x4 qf[NJ];
+    {
+      const int tok = row / G, head = hk * G + row - tok * G;
+      const float* src = (const float*)A->q + (it.start + tok) * A->P.q_st + head * A->P.q_sh;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int x = 16 * j + 4 * g;
-      qf[j] = x < P.d ? *(const f32x4*)(src + x) : f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < NJ; ++j) {
+        const int x = 16 * j + 4 * g;
+        qf[j] = x < d ? *(const f32x4*)(src + x) : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     }
-  }
-  const int cc = 4 * (tid % NC), cr = tid / NC;  // this thread's piece of a row, and row
-  const int32_t* table = P.table + it.b * P.table_sb;
-  const float *kh = kp + hk * P.k_sh + cc, *vh = vp + hk * P.v_sh + cc;
-  const int n = 2 * (it.t1 - it.t0);  // half tiles
-  auto first_key = [&](int i) __attribute__((always_inline)) {
-    return KT * list.tile(it.t0 + (i >> 1)) + HK * (i & 1);
-  };
-  int ent[NP];
-  auto entries = [&](int i) __attribute__((always_inline)) {
-    const int j0 = first_key(min(i, n - 1)) + cr;
+    const int cc = 4 * (tid % NC), cr = tid / NC;  // this thread's piece of a row, and row
+    const int32_t* table = A->P.table + it.b * A->P.table_sb;
+    const float *kh = (const float*)A->kp + hk * A->P.k_sh + cc,
+                *vh = (const float*)A->vp + hk * A->P.v_sh + cc;
+    const int64_t k_sp = A->P.k_sp, k_st = A->P.k_st, v_sp = A->P.v_sp, v_st = A->P.v_st;
+    const int page = A->P.page, pages = A->P.pages;
+    const FastDiv by_page{A->by_page.m, A->by_page.s};
+    const int n = 2 * (it.t1 - it.t0);  // half tiles
+    auto first_key = [&](int i) __attribute__((always_inline)) {
+      return KT * list.tile(it.t0 + (i >> 1)) + HK * (i & 1);
+    };
+    int ent[NP];
+    auto entries = [&](int i) __attribute__((always_inline)) {
+      const int j0 = first_key(min(i, n - 1)) + cr;
 #pragma unroll
-    for (int x = 0; x < NP; ++x) ent[x] = table[by_page.div(min(j0 + x * RP, it.lk - 1))];
-  };
-  f32x4 kr[NP], vr[NP];
-  uint32_t missing;
-  auto load = [&](int i) __attribute__((always_inline)) {
-    const int j0 = first_key(i) + cr;
-    missing = 0;
+      for (int x = 0; x < NP; ++x) ent[x] = table[by_page.div(min(j0 + x * RP, it.lk - 1))];
+    };
+    f32x4 kr[NP], vr[NP];
+    uint32_t missing;
+    auto load = [&](int i) __attribute__((always_inline)) {
+      const int j0 = first_key(i) + cr;
+      missing = 0;
 #pragma unroll
-    for (int x = 0; x < NP; ++x) {
-      const int j = j0 + x * RP, e = ent[x], c = min(j, it.lk - 1), in = c - by_page.div(c) * P.page;
-      const bool there = e >= 0 && e < P.pages;
-      kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (there && j < it.lk && cc < P.d) {
-        kr[x] = *(const f32x4*)(kh + e * P.k_sp + in * P.k_st);
-        vr[x] = *(const f32x4*)(vh + e * P.v_sp + in * P.v_st);
+      for (int x = 0; x < NP; ++x) {
+        const int j = j0 + x * RP, e = ent[x], c = min(j, it.lk - 1), in = c - by_page.div(c) * page;
+        const bool there = e >= 0 && e < pages;
+        kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (there && j < it.lk && cc < d) {
+          kr[x] = *(const f32x4*)(kh + e * k_sp + in * k_st);
+          vr[x] = *(const f32x4*)(vh + e * v_sp + in * v_st);
+        }
+        if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
       }
-      if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
-    }
-  };
-  auto store = [&](int i) __attribute__((always_inline)) {
-    if (missing) atomicOr(&gone[i & 3], missing);
+    };
+    auto store = [&](int i) __attribute__((always_inline)) {
+      if (missing) atomicOr(&gone[i & 3], missing);
 #pragma unroll
-    for (int x = 0; x < NP; ++x) {
-      const int r = cr + x * RP;
-      bool fine = true;
+      for (int x = 0; x < NP; ++x) {
+        const int r = cr + x * RP;
+        bool fine = true;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) fine &= fabsf(vr[x][e]) < INFINITY;
-      if (__builtin_expect(!fine, 0)) {
-        // zero times it would reach rows that do not see it: those that do get NaN at the end
-        atomicOr(&bad[i & 3], 1u << r);
+        for (int e = 0; e < 4; ++e) fine &= fabsf(vr[x][e]) < INFINITY;
+        if (__builtin_expect(!fine, 0)) {
+          // zero times it would reach rows that do not see it: those that do get NaN at the end
+          atomicOr(&bad[i & 3], 1u << r);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!(fabsf(vr[x][e]) < INFINITY)) vr[x][e] = 0.f;
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(vr[x][e]) < INFINITY)) vr[x][e] = 0.f;
+        }
+        *(f32x4*)&ks[i & 1][r][cc] = kr[x];
+        *(f32x4*)&vs[i & 1][r][cc] = vr[x];
       }
-      *(f32x4*)&ks[i & 1][r][cc] = kr[x];
-      *(f32x4*)&vs[i & 1][r][cc] = vr[x];
-    }
-  };
-  f32x4 o[NJ];
-  float m = -INFINITY, l = 0.f;  // reference (log2 units), this lane's part of the sum
-  bool poison = false;
+    };
+    f32x4 o[NJ];
+    float m = -INFINITY, l = 0.f;  // reference (log2 units), this lane's part of the sum
+    bool poison = false;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](int i) __attribute__((always_inline)) {
-    const int k0 = first_key(i);
-    // no row sees a key; every row sees all
-    if (k0 >= rz.s_end && (k0 >= rz.hi || k0 + HK <= ra.lo)) return;
-    const uint32_t hv = gone[i & 3], bv = bad[i & 3];
-    const bool all = (k0 + HK <= ra.s_end || (k0 >= rz.lo && k0 + HK <= ra.hi)) && hv == 0;
-    const float(*kt)[LD] = ks[i & 1];
-    const float(*vt)[LD] = vs[i & 1];
-    // four partial sums a logit: shorter chains of rounded sums
-    f32x4 p[2][4];
+    for (int j = 0; j < NJ; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto compute = [&](int i) __attribute__((always_inline)) {
+      const int k0 = first_key(i);
+      // no row sees a key; every row sees all
+      if (k0 >= rz.s_end && (k0 >= rz.hi || k0 + HK <= ra.lo)) return;
+      const uint32_t hv = gone[i & 3], bv = bad[i & 3];
+      const bool all = (k0 + HK <= ra.s_end || (k0 >= rz.lo && k0 + HK <= ra.hi)) && hv == 0;
+      const float(*kt)[LD] = ks[i & 1];
+      const float(*vt)[LD] = vs[i & 1];
+      // four partial sums a logit: shorter chains of rounded sums
+      f32x4 p[2][4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[u][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const f32x4 kf = *(const f32x4*)&kt[16 * u + l16][16 * j + 4 * g];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          p[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[j][e], p[u][e], 0, 0, 0);
-      }
-    float s[2][4], mx = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[u][r] = (p[u][0][r] + p[u][1][r]) + (p[u][2][r] + p[u][3][r]);
-        const int j = 16 * u + 4 * g + r;
-        if (!all && (!sees(mine, k0 + j) || ((hv >> j) & 1))) s[u][r] = -INFINITY;
-        mx = fmaxf(mx, s[u][r]);
-      }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
-    if (__builtin_amdgcn_ballot_w64(mx > m)) {
-      const float m1 = fmaxf(m, mx), al = m1 > m ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
-      l *= al;
+        for (int e = 0; e < 4; ++e) p[u][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[j][r] *= al;
-      m = m1;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;
+        for (int u = 0; u < 2; ++u) {
+          const f32x4 kf = *(const f32x4*)&kt[16 * u + l16][16 * j + 4 * g];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+          for (int e = 0; e < 4; ++e)
+            p[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[j][e], p[u][e], 0, 0, 0);
+        }
+      float s[2][4], mx = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], sl2, -ref));
-        l += s[u][r];
-      }
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r) {
+          s[u][r] = (p[u][0][r] + p[u][1][r]) + (p[u][2][r] + p[u][3][r]);
+          const int j = 16 * u + 4 * g + r;
+          if (!all && (!sees(mine, k0 + j) || ((hv >> j) & 1))) s[u][r] = -INFINITY;
+          mx = fmaxf(mx, s[u][r]);
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
+      if (__builtin_amdgcn_ballot_w64(mx > m)) {
+        const float m1 = fmaxf(m, mx), al = m1 > m ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
+        l *= al;
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-          o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[16 * u + 4 * g + r][16 * j + l16], s[u][r],
-                                                      o[j], 0, 0, 0);
-    if (__builtin_expect(bv != 0, 0))
-      for (uint32_t x = bv; x; x &= x - 1) poison |= sees(mine, k0 + __builtin_ctz(x));
-  };
-  if (tid < 4) gone[tid] = bad[tid] = 0;
-  __syncthreads();
-  if (n > 0) {
-    entries(0);
-    load(0);
-    entries(1);
-    store(0);
-    __syncthreads();
-    for (int i = 0; i < n; ++i) {
-      if (i + 1 < n) load(i + 1);
-      entries(i + 2);
-      // the flags of half tile i + 2 (those of i - 2 were read before the last barrier)
-      if (tid == 0) gone[(i + 2) & 3] = bad[(i + 2) & 3] = 0;
-      if (wreal) compute(i);
-      if (i + 1 < n) store(i + 1);
-      __syncthreads();
-    }
-  }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  if (l16 >= wreal) return;
-  if (poison) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) o[j] = f32x4{NAN, NAN, NAN, NAN};
-  }
-  if (it.slot >= 0) {
-    float* x = (float*)(ws + L.part_at) +
-               (((size_t)hk * L.slots + it.slot) * L.rows + 16 * w + l16) * (P.d + 4);
+          for (int r = 0; r < 4; ++r) o[j][r] *= al;
+        m = m1;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], sl2, -ref));
+          l += s[u][r];
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[16 * u + 4 * g + r][16 * j + l16], s[u][r],
+                                                        o[j], 0, 0, 0);
+      if (__builtin_expect(bv != 0, 0))
+        for (uint32_t x = bv; x; x &= x - 1) poison |= sees(mine, k0 + __builtin_ctz(x));
+    };
+    if (tid < 4) gone[tid] = bad[tid] = 0;
+    __syncthreads();
+    if (n > 0) {
+      entries(0);
+      load(0);
+      entries(1);
+      store(0);
+      __syncthreads();
+      for (int i = 0; i < n; ++i) {
+        if (i + 1 < n) load(i + 1);
+        entries(i + 2);
+        // the flags of half tile i + 2 (those of i - 2 were read before the last barrier)
+        if (tid == 0) gone[(i + 2) & 3] = bad[(i + 2) & 3] = 0;
+        if (wreal) compute(i);
+        if (i + 1 < n) store(i + 1);
+        __syncthreads();
+      }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (poison) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) o[j] = f32x4{NAN, NAN, NAN, NAN};
+    }
+    const Args B = args();
+    if (it.slot >= 0) {
+      if (wreal == 0) continue;
+      float* x = part_wave(B->ws + B->L.part_at, B->C.held, B->L.slot_waves, S.cls, it.slot, w, NJ) +
+                 4 * lane;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) *(f32x4*)(x + 256 * j) = o[j];
+      x += 256 * NJ - 3 * lane;
+      x[0] = m;
+      x[64] = l;
+      continue;
+    }
+    if (l16 >= wreal) continue;
+    const bool any = l != 0.f;
+    const int tok = row / G, head = hk * G + row - tok * G;
+    float* orow = (float*)B->out + (it.start + tok) * B->P.o_st + head * B->P.o_sh;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
-      if (16 * j + 4 * g < P.d) *(f32x4*)(x + 16 * j + 4 * g) = o[j];
-    if (g == 0) {
-      x[P.d] = m;
-      x[P.d + 1] = l;
-    }
-    return;
+      if (16 * j + 4 * g < d) {
+        f32x4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = any ? o[j][r] / l : 0.f;
+        *(f32x4*)(orow + 16 * j + 4 * g) = x;
+      }
+    if (B->lse && g == 0)
+      B->lse[(size_t)(it.start + tok) * B->P.H + head] =
+          any ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   }
-  const bool any = l != 0.f;
-  float* orow = out + (it.start + tok) * P.o_st + head * P.o_sh;
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-    if (16 * j + 4 * g < P.d) {
-      f32x4 x;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = any ? o[j][r] / l : 0.f;
-      *(f32x4*)(orow + 16 * j + 4 * g) = x;
-    }
-  if (lse && g == 0)
-    lse[(size_t)(it.start + tok) * P.H + head] =
-        any ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---- launches -----------------------------------------------------------------------------
 
-// Workgroups that the compute units hold at once (256 units, two or three each): the share
-// of one of them is what a block is cut to, so that no workgroup runs much longer
-// than all need together.
+// Workgroups of a compute unit: LDS (bf16), registers and LDS (fp32) hold so many
+int per_unit(const ChunkProb& P) { return P.d > 64 ? 2 : 3; }
+
 Plan plan_of(const ChunkProb& P) {
   Plan L;
   L.rows = P.dtype == CA_BF16 ? kWalkRows : kF32Rows;
-  const int held = P.d > 64 ? 512 : P.dtype == CA_BF16 ? 768 : 1024;
   const int64_t rows = (int64_t)P.tokens * P.G;
+  const int wave_rows = L.rows / 4;
+  L.slot_waves = (int)(rows < L.rows ? (rows + wave_rows - 1) / wave_rows : 4);
   L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
-  L.share = (held + P.Hk - 1) / P.Hk;
-  // a cut block has more than `part` tiles, part >= all tiles / share: the parts of the cut
-  // blocks are at most twice the share, and so few blocks are cut
-  L.slots = 2 * L.share;
-  L.cuts = L.share < L.blocks ? L.share : L.blocks;
-  int64_t most = ((int64_t)P.max_pages * P.page + KT - 1) / KT + 2;  // tiles of a block
-  most = (most + kPartTiles - 1) / kPartTiles;
-  if (most == 1) L.slots = L.cuts = 0;
-  if (L.slots > L.blocks * most) L.slots = (int)(L.blocks * most);
-  L.items = L.blocks + L.slots;
+  const Classes C = Classes::of(P.Hk, per_unit(P));
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  L.item_at = 256;
-  L.cut_at = align(L.item_at + (size_t)L.items * sizeof(Item));
-  L.part_at = align(L.cut_at + (size_t)L.cuts * sizeof(Cut));
-  L.bytes = align(L.part_at + (size_t)P.Hk * L.slots * L.rows * (P.d + 4) * 4);
+  L.block_at = 256;
+  L.share_at = align(L.block_at + (size_t)L.blocks * sizeof(Block));
+  L.cut_at = align(L.share_at + (size_t)(C.held + 1) * sizeof(Share));
+  L.part_at = align(L.cut_at + (size_t)C.held * sizeof(Cut));
+  const int dp = P.d <= 32 ? 32 : P.d <= 64 ? 64 : 128;
+  const int chunks = P.dtype == CA_BF16 ? dp / 8 : dp / 16;
+  L.bytes = align(L.part_at + (size_t)C.g * 2 * C.held * L.slot_waves * 256 * (4 * chunks + 2));
   return L;
 }
 
+// Workgroups that may have work: those that run at a time, or one for each block
+int64_t grid_of(const ChunkProb& P, const Plan& L, const Classes& C) {
+  const int64_t held = (int64_t)C.g * C.held, r = 8 / C.g;
+  const int64_t each = 8 * ((L.blocks * (int64_t)C.heads + r - 1) / r);
+  return each > held ? each : held;
+}
+
 template <typename T, int DP>
-hipError_t run_join(const ChunkProb& P, const Plan& L, T* out, float* lse, const char* ws,
-                    hipStream_t st) {
-  if (L.slots == 0) return hipSuccess;
-  const int64_t quads = (int64_t)L.cuts * P.Hk * (L.rows / 4);
-  const dim3 grid((unsigned)(quads < kJoinGrid ? quads : kJoinGrid));
-  hipLaunchKernelGGL((chunk_join_kernel<T, DP>), grid, dim3(256), 0, st, P, L, ws, out, lse);
+hipError_t run_join(const ChunkProb& P, const Plan& L, const Classes& C, T* out, float* lse,
+                    char* ws, hipStream_t st) {
+  const int64_t most = (int64_t)C.held * C.g * L.slot_waves * 4;
+  const dim3 grid((unsigned)(most < kJoinGrid ? most : kJoinGrid));
+  hipLaunchKernelGGL((chunk_join_kernel<T, DP>), grid, dim3(256), 0, st, P, L, C, ws, out, lse);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t run_bf16(const ChunkProb& P, const Plan& L, const bf16* q, const bf16* kp,
                     const bf16* vp, bf16* out, float* lse, char* ws, hipStream_t st) {
-  const ItemOrder order = ItemOrder::of(P.Hk);
-  const dim3 grid((unsigned)order.grid(L.items));
-  const FastDiv by_page = FastDiv::of(P.page);
+  const Classes C = Classes::of(P.Hk, per_unit(P));
+  const dim3 grid((unsigned)grid_of(P, L, C));
+  const ChunkArgs A{P, L, C, FastDiv::of(P.page), P.scale * kLog2e, q, kp, vp, out, lse, ws};
   // the rows of a page that a group of 16 takes are reached by 32-bit offsets
   if (P.page % 16 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23))
-    hipLaunchKernelGGL((chunk_bf16_kernel<D, true>), grid, dim3(256), 0, st, P, L, order, by_page,
-                       q, kp, vp, out, lse, ws, P.scale * kLog2e);
+    hipLaunchKernelGGL((chunk_bf16_kernel<D, true>), grid, dim3(256), 0, st, A);
   else
-    hipLaunchKernelGGL((chunk_bf16_kernel<D, false>), grid, dim3(256), 0, st, P, L, order, by_page,
-                       q, kp, vp, out, lse, ws, P.scale * kLog2e);
+    hipLaunchKernelGGL((chunk_bf16_kernel<D, false>), grid, dim3(256), 0, st, A);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : run_join<bf16, D>(P, L, out, lse, ws, st);
+  return e != hipSuccess ? e : run_join<bf16, D>(P, L, C, out, lse, ws, st);
 }
 
 template <int DP, int WAVES>
 hipError_t run_f32(const ChunkProb& P, const Plan& L, const float* q, const float* kp,
                    const float* vp, float* out, float* lse, char* ws, hipStream_t st) {
-  const ItemOrder order = ItemOrder::of(P.Hk);
-  hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES>), dim3((unsigned)order.grid(L.items)), dim3(256), 0,
-                     st, P, L, order, FastDiv::of(P.page), q, kp, vp, out, lse, ws,
-                     P.scale * kLog2e);
+  const Classes C = Classes::of(P.Hk, per_unit(P));
+  const ChunkArgs A{P, L, C, FastDiv::of(P.page), P.scale * kLog2e, q, kp, vp, out, lse, ws};
+  hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES>), dim3((unsigned)grid_of(P, L, C)), dim3(256), 0,
+                     st, A);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : run_join<float, DP>(P, L, out, lse, ws, st);
+  return e != hipSuccess ? e : run_join<float, DP>(P, L, C, out, lse, ws, st);
 }
 
 }  // namespace
@@ -826,7 +983,7 @@ hipError_t run_f32(const ChunkProb& P, const Plan& L, const float* q, const floa
 bool chunk_fits(const ChunkProb& P) {
   if ((int64_t)P.tokens * P.G >= ((int64_t)1 << 30)) return false;
   // workgroups of 256 threads, fewer than 2^32 of them
-  return ItemOrder::of(P.Hk).grid(plan_of(P).items) < (1 << 24);
+  return grid_of(P, plan_of(P), Classes::of(P.Hk, per_unit(P))) < (1 << 24);
 }
 
 size_t chunk_bytes(const ChunkProb& P) { return plan_of(P).bytes; }
@@ -834,7 +991,8 @@ size_t chunk_bytes(const ChunkProb& P) { return plan_of(P).bytes; }
 hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st) {
   const Plan L = plan_of(P);
-  hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L, ws);
+  hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L,
+                     Classes::of(P.Hk, per_unit(P)), ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (P.dtype == CA_BF16) {
@@ -843,8 +1001,8 @@ hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const
                      : run_bf16<128>(P, L, a, b, c, (bf16*)out, lse, ws, st);
   }
   const float *a = (const float*)q, *b = (const float*)kp, *c = (const float*)vp;
-  return P.d <= 32   ? run_f32<32, 4>(P, L, a, b, c, (float*)out, lse, ws, st)
-         : P.d <= 64 ? run_f32<64, 4>(P, L, a, b, c, (float*)out, lse, ws, st)
+  return P.d <= 32   ? run_f32<32, 3>(P, L, a, b, c, (float*)out, lse, ws, st)
+         : P.d <= 64 ? run_f32<64, 3>(P, L, a, b, c, (float*)out, lse, ws, st)
                      : run_f32<128, 2>(P, L, a, b, c, (float*)out, lse, ws, st);
 }
 
