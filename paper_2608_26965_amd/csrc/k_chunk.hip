@@ -10,10 +10,13 @@
 // several workgroups share leaves its softmax states in the workspace, and a last launch
 // joins them. Where there is more than a round of blocks, the first rounds are whole ones
 // (the workgroups that run at a time then read the same keys at a time), and
-// the shares even out the rest; where there are many, no block is cut.
+// the shares even out the rest. Calls whose blocks have few tiles by their sizes alone go
+// without a plan: a workgroup finds its block by itself.
 //
 // What bounds it: the matrix cores for prompts, the cache for few new tokens.
 #include <math.h>
+
+#include <algorithm>
 
 #include "seq.h"
 #include "walk_bf16.h"
@@ -24,23 +27,30 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kPlan = 256;     // threads of the planning workgroup
-constexpr int kF32Rows = 64;   // rows of a block, fp32
-constexpr int kXcdUnits = 32;  // compute units of an XCD
-constexpr int kShareTiles = 4; // tiles of a share, at least
-constexpr int kRounds = 6;     // rounds of blocks from which on none is cut
-constexpr int kStart = 4;      // what starting a block costs, in tiles
-constexpr int kSnap = 3;       // shares begin no nearer to a block's ends, in tiles
-constexpr int kIndex = 2048;   // entries of the planning workgroup's index of the blocks
+constexpr int kPlan = 256;       // threads of the planning workgroup
+constexpr int kF32Rows = 64;     // rows of a block, fp32
+constexpr int kXcdUnits = 32;    // compute units of an XCD
+constexpr int kShareTiles = 4;   // tiles of a share, at least
+constexpr int kStart = 4;        // what starting a block costs, in tiles
+constexpr int kJoinCost = 16;    // what cutting and joining costs
+constexpr int kSnap = 3;         // shares begin no nearer to a block's ends, in tiles
+constexpr int kMostRounds = 8;   // of whole blocks before the shares
+constexpr int kIndex = 2048;     // entries of the planning workgroup's index of the blocks
+constexpr int kDirectTiles = 24; // blocks of so few tiles are not planned
+constexpr int kDirectBatch = 256, kDirectBlocks = 1 << 22;
 
 // A block of a sequence's rows, for every key head. cost: of the blocks before it.
 struct Block {
   int b, a, tiles, lq, lk, start;
   int64_t cost;
 };
-// Where a share begins: tile t of a block of the hs-th of the heads that its workgroups take
-struct Share {
-  int hs, block, t, pad;
+// What a workgroup does: whole blocks for `rounds` rounds, then its share, from tile t of a block of
+// the hs-th of the heads that its workgroups take, up to another such place. blocks: number
+// of blocks. first: the block that it begins with.
+struct Turn {
+  int hs, block, t, blocks;
+  int hs1, block1, t1, rounds;
+  Block first;
 };
 // A block that is cut: its first part is the end of share u - 1, the others begin shares u,
 // u + 1, ..; n parts in all
@@ -48,9 +58,7 @@ struct Cut {
   int hs, u, n, a, lq, start, pad0, pad1;
 };
 struct PlanHead {
-  // rounds: whole blocks of a workgroup before its share; shares 0: no block is cut, a
-  // workgroup takes one block
-  int blocks, shares, cuts, rounds;
+  int blocks, turns, cuts, whole;  // whole: no block is cut, a workgroup takes one block
 };
 
 // Workgroup w of the grid runs on XCD w % 8. The key heads are spread over the XCDs, in g
@@ -71,7 +79,8 @@ struct Plan {
   int rows;        // of a block
   int slot_waves;  // wavefronts of a block that have rows, at most
   int blocks;      // at most, for one key head
-  size_t block_at, share_at, cut_at, part_at, bytes;
+  int direct;      // not planned: a workgroup takes one block, which it finds by itself
+  size_t block_at, turn_at, cut_at, part_at, bytes;
 };
 
 // Positions of a block's first and last row (a sequence has fewer than 2^30 rows)
@@ -126,7 +135,7 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   __shared__ int64_t index[kIndex];  // cost of every 2^step-th block
   __shared__ int n_cuts;
   Block* list = (Block*)(ws + L.block_at);
-  Share* shares = (Share*)(ws + L.share_at);
+  Turn* turns = (Turn*)(ws + L.turn_at);
   Cut* cuts = (Cut*)(ws + L.cut_at);
   const int tid = threadIdx.x;
   int step = 0;
@@ -175,21 +184,33 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < kPlan / 64; ++x) longest = max(longest, most_of[x]);
-  const int64_t all = cost * C.heads;
-  const int64_t share = all / C.held;
-  const int rounds = seen == 0 ? kRounds : (int)min((int64_t)kRounds, share / longest);
-  const bool whole = rounds == kRounds;
+  if (seen == 0) {
+    if (tid == 0) *(PlanHead*)ws = PlanHead{0, 0, 0, 1};
+    return;
+  }
+  // Whole blocks take as long as the longest one, and what does not fill a round leaves
+  // workgroups idle: as much as a block if all are alike, next to nothing if they get
+  // shorter (the shorter ones fill the gaps). Above what cutting costs (with many rounds
+  // also that the workgroups no longer read the same keys at a time: a twentieth), blocks
+  // are cut. 130 blocks of 112 tiles on each 64 workgroups: 575 us whole, 535 cut; 64 of 33
+  // (causal, 1 to 64): 164 and 181; 256 of 450: 3.58 and 3.75 ms.
+  const int64_t all = cost * C.heads, share = all / C.held;
+  const int count = seen * C.heads, mean = (int)(cost / seen), left = count % C.held;
+  const int idle = left == 0 ? 0
+                             : (int)((int64_t)(C.held - left) * max(0, 2 * mean - longest) / C.held);
+  const bool whole = max((int64_t)longest - share, (int64_t)idle) <= kJoinCost + share / 20;
+  const int rounds = (int)min((int64_t)kMostRounds, share / longest);
   const int n = rounds > 0 ? C.held
                            : (int)min((int64_t)C.held, (all + kShareTiles - 1) / kShareTiles);
-  if (tid == 0) *(PlanHead*)ws = PlanHead{seen, whole ? 0 : n, 0, whole ? 1 : rounds};
+  if (tid == 0) *(PlanHead*)ws = PlanHead{seen, n, 0, whole};
   if (whole) return;
   // cost of the class's blocks before the i-th
   auto cost_of = [&](int i) {
-    const int h = i / seen;
-    return h * cost + list[i - h * seen].cost;
+    const int h = i / seen, k = i - h * seen;
+    return h * cost + (step == 0 ? index[k] : list[k].cost);
   };
   for (int u = tid; u <= n; u += kPlan) {
-    Share s{C.heads, 0, 0, 0};
+    int hs = C.heads, block = 0, t = 0;
     if (u < n) {
       // all workgroups' whole blocks, what the shares before leave to be done by the
       // workgroups before u beside their own whole blocks
@@ -198,8 +219,8 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
         pos += cost_of(rounds * C.held);
         for (int k = 0; k < rounds; ++k) pos -= cost_of(k * C.held + u) - cost_of(k * C.held);
       }
-      s.hs = (int)(pos / cost);
-      const int64_t off = pos - s.hs * cost;
+      hs = (int)(pos / cost);
+      const int64_t off = pos - hs * cost;
       int lo = 0, hi = ((seen - 1) >> step) + 1;  // index[lo] <= off < index[hi]
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -217,28 +238,42 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
         else
           hi = mid;
       }
-      const int tiles = list[lo].tiles;
-      s.block = lo;
-      s.t = max(0, (int)(off - list[lo].cost) - kStart);
-      if (s.t < kSnap) s.t = 0;
-      if (s.t > 0 && tiles - s.t < kSnap) {  // at the next block's beginning instead
-        s.t = 0;
-        if (++s.block == seen) {
-          s.block = 0;
-          ++s.hs;
+      block = lo;
+      const int64_t c = step == 0 ? index[lo] : list[lo].cost;
+      const int64_t e = lo + 1 == seen ? cost : step == 0 ? index[lo + 1] : list[lo + 1].cost;
+      t = max(0, (int)(off - c) - kStart);
+      if (t < kSnap) t = 0;
+      if (t > 0 && (int)(e - c) - kStart - t < kSnap) {  // at the next block's beginning instead
+        t = 0;
+        if (++block == seen) {
+          block = 0;
+          ++hs;
         }
       }
     }
-    shares[u] = s;
+    Turn* x = turns + u;
+    if (u < n) {
+      x->hs = hs;
+      x->block = block;
+      x->t = t;
+      x->blocks = seen;
+      x->rounds = rounds;
+      x->first = list[rounds > 0 ? u % seen : block];
+    }
+    if (u > 0) {
+      x[-1].hs1 = hs;
+      x[-1].block1 = block;
+      x[-1].t1 = t;
+    }
   }
   __syncthreads();
   for (int u = 1 + tid; u < n; u += kPlan) {
-    const Share s = shares[u], p = shares[u - 1];
+    const Turn &s = turns[u], &p = turns[u - 1];
     if (s.t == 0 || (p.t > 0 && p.hs == s.hs && p.block == s.block)) continue;
     int lo = u, hi = n;  // share lo begins in the block, share hi after it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (shares[mid].hs == s.hs && shares[mid].block == s.block)
+      if (turns[mid].hs == s.hs && turns[mid].block == s.block)
         lo = mid;
       else
         hi = mid;
@@ -289,73 +324,148 @@ __device__ __forceinline__ Args args() {
 struct Piece {
   int b, a, t0, t1, slot, lq, lk, start;
 };
-// The pieces of a workgroup's share, one after the other
+// A workgroup's pieces of work, one after the other. (What the launch before wrote is read from
+// the constant address space, by scalar loads.)
+template <int ROWS>
 struct Pieces {
-  // (from the constant address space: scalar loads of what the launch before wrote)
-  typedef int i32x8 __attribute__((ext_vector_type(8)));
   typedef int i32x4 __attribute__((ext_vector_type(4)));
-  typedef const __attribute__((address_space(4))) i32x8* Blocks;
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  typedef int i32x16 __attribute__((ext_vector_type(16)));
   typedef const __attribute__((address_space(4))) i32x4* Heads;
+  typedef const __attribute__((address_space(4))) i32x8* Blocks;
+  typedef const __attribute__((address_space(4))) i32x16* Turns;
+  Piece it;                           // the piece
   int hs, block, t, hs1, block1, t1;  // from here to there
-  int k, u, cls;
+  int k, rounds, u, cls, n;           // k: ranges done
 
-  static __device__ __forceinline__ i32x4 plan_head() { return *(Heads)args()->ws; }  // PlanHead
+  __device__ __forceinline__ void set(i32x8 x) {  // x: Block
+    const int end = hs == hs1 && block == block1 ? t1 : x[2];
+    it = Piece{x[0], x[1], t, end, t == 0 && end == x[2] ? -1 : 2 * u + (t == 0), x[3], x[4], x[5]};
+  }
+  __device__ __forceinline__ void load() {
+    const Args A = args();
+    set(((Blocks)(A->ws + A->L.block_at))[block]);
+  }
+  // the i-th block of the class's as a whole
+  __device__ __forceinline__ bool whole(int i) {
+    hs = i / n;
+    block = i - hs * n;
+    hs1 = hs;
+    block1 = block + 1;
+    t = t1 = 0;
+    return hs < args()->C.heads;
+  }
+  __device__ __forceinline__ void share(i32x16 x) {  // x: Turn
+    hs = x[0];
+    block = x[1];
+    t = x[2];
+    hs1 = x[4];
+    block1 = x[5];
+    t1 = x[6];
+  }
+  __device__ __forceinline__ bool more() const {
+    return hs < hs1 || (hs == hs1 && (block < block1 || (block == block1 && t < t1)));
+  }
+  __device__ __forceinline__ int head() const { return hs * args()->C.g + cls; }
+
   // false: no work
   __device__ __forceinline__ bool first() {
     const Args A = args();
     const int g = A->C.g;
     cls = (blockIdx.x & 7) % g;
     u = (blockIdx.x >> 3) * (8 / g) + (blockIdx.x & 7) / g;
-    k = -1;
-    const i32x4 h = plan_head();
-    return h[0] > 0 && (h[1] == 0 || u < h[1]) && range();
-  }
-  // the next whole block, or the share
-  __device__ __forceinline__ bool range() {
-    const Args A = args();
-    const i32x4 h = plan_head();
-    if (++k < h[3]) {
-      const int i = k * A->C.held + u;
-      hs = i / h[0];
-      block = i - hs * h[0];
-      t = 0;
-      hs1 = hs;
-      block1 = block + 1;
-      t1 = 0;
-      return hs < A->C.heads;
+    k = 0;
+    rounds = -1;
+    if (A->L.direct) return direct(A);
+    const i32x4 h = *(Heads)A->ws;  // PlanHead
+    const i32x16 x = ((Turns)(A->ws + A->L.turn_at))[min(u, A->C.held - 1)];
+    n = h[0];
+    if (n == 0) return false;
+    if (h[3]) {
+      if (!whole(u)) return false;
+      load();
+      return true;
     }
-    if (k > h[3] || h[1] == 0) return false;
-    const Heads shares = (Heads)(A->ws + A->L.share_at);
-    const i32x4 a = shares[u], z = shares[u + 1];
-    hs = a[0];
-    block = a[1];
-    t = a[2];
-    hs1 = z[0];
-    block1 = z[1];
-    t1 = z[2];
-    return more();
-  }
-  __device__ __forceinline__ bool more() const {
-    return hs < hs1 || (hs == hs1 && (block < block1 || (block == block1 && t < t1)));
-  }
-  __device__ __forceinline__ int head() const { return hs * args()->C.g + cls; }
-  __device__ __forceinline__ Piece piece() const {
-    const Args A = args();
-    const i32x8 x = ((Blocks)(A->ws + A->L.block_at))[block];  // Block
-    const int end = hs == hs1 && block == block1 ? t1 : x[2];
-    return Piece{x[0], x[1], t, end, t == 0 && end == x[2] ? -1 : 2 * u + (t == 0), x[3], x[4], x[5]};
+    if (u >= h[1]) return false;
+    rounds = x[7];
+    if (rounds > 0)
+      whole(u);
+    else
+      share(x);
+    if (!more()) return false;
+    set(i32x8{x[8], x[9], x[10], x[11], x[12], x[13], x[14], x[15]});
+    return true;
   }
   __device__ __forceinline__ bool next() {
     if (hs == hs1 && block == block1) {
       t = t1;  // the end
     } else {
       t = 0;
-      if (++block == plan_head()[0] && hs < hs1) {
+      if (++block == n && hs < hs1) {
         block = 0;
         ++hs;
       }
     }
-    return more() || range();
+    if (!more()) {
+      ++k;
+      if (k > rounds) return false;
+      if (k < rounds) {
+        whole(k * args()->C.held + u);
+      } else {
+        const Args A = args();
+        share(((Turns)(A->ws + A->L.turn_at))[u]);
+        if (!more()) return false;
+      }
+    }
+    load();
+    return true;
+  }
+  // Block u of the class's, found from the lengths: a lane has four sequences
+  __device__ __forceinline__ bool direct(const Args A) {
+    constexpr int S = kDirectBatch / 64;
+    const int lane = threadIdx.x & 63, B = A->P.B, T = A->P.tokens, G = A->P.G;
+    int start[S], lq[S], lk[S], blocks[S], mine = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int b = S * lane + i;
+      start[i] = lq[i] = lk[i] = 0;
+      if (b < B) {
+        start[i] = min(max(A->P.starts[b], 0), T);
+        lq[i] = max(0, min(max(A->P.starts[b + 1], 0), T) - start[i]);
+        lk[i] = (int)min((int64_t)max(A->P.lens[b], 0), (int64_t)A->P.max_pages * A->P.page);
+      }
+      // (no more than the launch can have, so that the sum of starts that do not ascend fits)
+      blocks[i] = min((int)(((uint32_t)lq[i] * (uint32_t)G + ROWS - 1) / ROWS), kDirectBlocks);
+      mine += blocks[i];
+    }
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += y;
+    }
+    n = __builtin_amdgcn_readlane(sum, 63);
+    if (n <= 0 || n > A->L.blocks || !whole(u)) return false;
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > block));
+    int i = block - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(mine, l));
+    bool found = false;
+    it = Piece{0, 0, 0, 0, -1, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < S; ++x) {
+      const int c = __builtin_amdgcn_readlane(blocks[x], l);
+      if (!found && i < c) {
+        found = true;
+        it = Piece{S * l + x, c - 1 - i, 0, 0, -1, __builtin_amdgcn_readlane(lq[x], l),
+                   __builtin_amdgcn_readlane(lk[x], l), __builtin_amdgcn_readlane(start[x], l)};
+      }
+      i -= c;
+    }
+    if (!found) return false;
+    const BlockSpan s(it.a, ROWS, G, it.lq, it.lk);
+    it.t1 = visible_tiles<KT>(WinMask{A->P.m.left, A->P.m.right, A->P.m.sinks, A->P.m.causal}, s.p0,
+                              s.p1, it.lk)
+                .n;
+    return true;
   }
 };
 
@@ -381,6 +491,8 @@ __device__ __forceinline__ void lds_dma16_at(const void* p, uint32_t lds) {
       : "memory");
 }
 
+typedef const __attribute__((address_space(4))) int32_t* Entries;
+
 // Tiles whose rows lie on pages. Wavefront w copies rows 16 w .. 16 w + 15 of a
 // tile. GROUPS: pages of a multiple of 16 tokens, so that the sixteen lie on one page,
 // whose entry is one scalar load (from the constant address space: no kernel writes the
@@ -388,10 +500,9 @@ __device__ __forceinline__ void lds_dma16_at(const void* p, uint32_t lds) {
 // loaded a tile before the copies that need them.
 template <int D, bool GROUPS>
 struct PagedTiles : WalkRows {
-  static constexpr bool kHoles = true;
+  static constexpr bool kHoles = true, kBegun = true;
   static constexpr float kMostSum = 0x1p30f;
   static constexpr int RB = 2 * D, TILE = KT * RB, NI = RB / 64, RPI = 1024 / RB;
-  typedef const __attribute__((address_space(4))) int32_t* Entries;
   const bf16 *kh, *vh;  // of this key head
   const int32_t* table;
   int64_t k_sp, k_st, v_sp, v_st;
@@ -476,10 +587,15 @@ struct PagedTiles : WalkRows {
     ev = ek;
     ek = entry(min(t + 2, t1 - 1));
   }
-  __device__ __forceinline__ void first_k() {
-    ev = entry(t0);
-    copy<false>(t0, ev, 0, 0);
-    ek = entry(min(t0 + 1, t1 - 1));
+  // the first tile's keys and values and the second's keys, before the walk: with the queries
+  __device__ __forceinline__ void begin() {
+    if (t0 >= t1) return;
+    const int e = entry(t0);
+    ev = entry(min(t0 + 1, t1 - 1));
+    ek = entry(min(t0 + 2, t1 - 1));
+    copy<false>(t0, e, 0, 0);
+    copy<true>(t0, e, 2, 0);
+    if (t0 + 1 < t1) copy<false>(t0 + 1, ev, 1, 1);
   }
   __device__ __forceinline__ void issue_both(int t) const {
     const int e = entry(t);
@@ -503,9 +619,9 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
   __shared__ int redo;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Pieces S;
+  Pieces<kWalkRows> S;
   for (bool go = S.first(); go; go = S.next()) {
-    const Piece it = S.piece();
+    const Piece it = S.it;
     const int hk = S.head();
     __syncthreads();  // every wavefront is past the piece before
     const Args A = args();
@@ -551,6 +667,7 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) qreg[kk] = *(const bf16x8*)(src + 16 * kk + 8 * h);
     }
+    T.begin();
     // Retire the loads here (a wait the compiler sees), so that no vmcnt wait of
     // theirs lands in the loop, where it would also wait for the copies in flight.
     __builtin_amdgcn_s_waitcnt(kWalkVmcnt0);
@@ -700,7 +817,7 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 // neither the keys' 16-byte reads nor the values' 4-byte reads meet on a bank. What bounds
 // it: the matrix instructions, 32 cycles each.
 
-template <int DP, int WAVES>
+template <int DP, int WAVES, bool GROUPS>
 __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     const ChunkArgs) {
   constexpr int HK = 32, NJ = DP / 16, LD = DP + 4, NC = DP / 4;
@@ -709,9 +826,9 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
   __shared__ uint32_t gone[4], bad[4];  // keys not there, values that are not finite
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Pieces S;
+  Pieces<kF32Rows> S;
   for (bool go = S.first(); go; go = S.next()) {
-    const Piece it = S.piece();
+    const Piece it = S.it;
     const int hk = S.head();
     __syncthreads();  // every wavefront is past the piece before
     const Args A = args();
@@ -739,8 +856,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     }
     const int cc = 4 * (tid % NC), cr = tid / NC;  // this thread's piece of a row, and row
     const int32_t* table = A->P.table + it.b * A->P.table_sb;
-    const float *kh = (const float*)A->kp + hk * A->P.k_sh + cc,
-                *vh = (const float*)A->vp + hk * A->P.v_sh + cc;
+    const float *kh = (const float*)A->kp + hk * A->P.k_sh, *vh = (const float*)A->vp + hk * A->P.v_sh;
     const int64_t k_sp = A->P.k_sp, k_st = A->P.k_st, v_sp = A->P.v_sp, v_st = A->P.v_st;
     const int page = A->P.page, pages = A->P.pages;
     const FastDiv by_page{A->by_page.m, A->by_page.s};
@@ -748,27 +864,54 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     auto first_key = [&](int i) __attribute__((always_inline)) {
       return KT * list.tile(it.t0 + (i >> 1)) + HK * (i & 1);
     };
+    // Entries of half tile i's rows, a half tile before the rows are loaded. GROUPS: pages of a
+    // multiple of 8 tokens, so that the rows of a wavefront's pass lie on one page and its entry
+    // and their address are scalars (the lookups in vectors cost a fifth of the instructions).
+    const int lr = cr - w * (RP / 4);  // row within the wavefront's
+    const uint32_t k_off = GROUPS ? (uint32_t)(lr * k_st + cc) * 4 : 0;  // bytes
+    const uint32_t v_off = GROUPS ? (uint32_t)(lr * v_st + cc) * 4 : 0;
     int ent[NP];
     auto entries = [&](int i) __attribute__((always_inline)) {
-      const int j0 = first_key(min(i, n - 1)) + cr;
+      const int j0 = first_key(min(i, n - 1)) + (GROUPS ? w * (RP / 4) : cr);
 #pragma unroll
-      for (int x = 0; x < NP; ++x) ent[x] = table[by_page.div(min(j0 + x * RP, it.lk - 1))];
+      for (int x = 0; x < NP; ++x) {
+        const int e = by_page.div(min(j0 + x * RP, it.lk - 1));
+        if constexpr (GROUPS)
+          ent[x] = ((Entries)table)[__builtin_amdgcn_readfirstlane(e)];
+        else
+          ent[x] = table[e];
+      }
     };
     f32x4 kr[NP], vr[NP];
     uint32_t missing;
     auto load = [&](int i) __attribute__((always_inline)) {
-      const int j0 = first_key(i) + cr;
       missing = 0;
+      const int j0 = first_key(i) + (GROUPS ? w * (RP / 4) : cr);
 #pragma unroll
       for (int x = 0; x < NP; ++x) {
         const int j = j0 + x * RP, e = ent[x], c = min(j, it.lk - 1), in = c - by_page.div(c) * page;
         const bool there = e >= 0 && e < pages;
         kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (there && j < it.lk && cc < d) {
-          kr[x] = *(const f32x4*)(kh + e * k_sp + in * k_st);
-          vr[x] = *(const f32x4*)(vh + e * v_sp + in * v_st);
+        if constexpr (GROUPS) {
+          if (there && j < it.lk) {
+            const char* ks0 = (const char*)(kh + (e * k_sp + in * k_st));
+            const char* vs0 = (const char*)(vh + (e * v_sp + in * v_st));
+            if (j + RP / 4 <= it.lk && d == DP) {
+              kr[x] = *(const f32x4*)(ks0 + k_off);
+              vr[x] = *(const f32x4*)(vs0 + v_off);
+            } else if (j + lr < it.lk && cc < d) {
+              kr[x] = *(const f32x4*)(ks0 + k_off);
+              vr[x] = *(const f32x4*)(vs0 + v_off);
+            }
+          }
+          if (!there && j + lr < it.lk) missing |= 1u << (cr + x * RP);
+        } else {
+          if (there && j < it.lk && cc < d) {
+            kr[x] = *(const f32x4*)(kh + e * k_sp + in * k_st + cc);
+            vr[x] = *(const f32x4*)(vh + e * v_sp + in * v_st + cc);
+          }
+          if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
         }
-        if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
       }
     };
     auto store = [&](int i) __attribute__((always_inline)) {
@@ -925,10 +1068,19 @@ Plan plan_of(const ChunkProb& P) {
   L.slot_waves = (int)(rows < L.rows ? (rows + wave_rows - 1) / wave_rows : 4);
   L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
   const Classes C = Classes::of(P.Hk, per_unit(P));
+  // tiles of a block: the table's, or those of the sinks and of the window of its tokens
+  int64_t tiles = ((int64_t)P.max_pages * P.page + KT - 1) / KT;
+  const int64_t span = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + L.rows / P.G + 2;
+  tiles = std::min(tiles, span / KT + 2 + (P.m.sinks + KT - 1) / KT);
+  L.direct = P.B <= kDirectBatch && L.blocks < kDirectBlocks && tiles <= kDirectTiles;
+  if (L.direct) {
+    L.block_at = L.turn_at = L.cut_at = L.part_at = L.bytes = 0;
+    return L;
+  }
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
   L.block_at = 256;
-  L.share_at = align(L.block_at + (size_t)L.blocks * sizeof(Block));
-  L.cut_at = align(L.share_at + (size_t)(C.held + 1) * sizeof(Share));
+  L.turn_at = align(L.block_at + (size_t)L.blocks * sizeof(Block));
+  L.cut_at = align(L.turn_at + (size_t)(C.held + 1) * sizeof(Turn));
   L.part_at = align(L.cut_at + (size_t)C.held * sizeof(Cut));
   const int dp = P.d <= 32 ? 32 : P.d <= 64 ? 64 : 128;
   const int chunks = P.dtype == CA_BF16 ? dp / 8 : dp / 16;
@@ -940,12 +1092,13 @@ Plan plan_of(const ChunkProb& P) {
 int64_t grid_of(const ChunkProb& P, const Plan& L, const Classes& C) {
   const int64_t held = (int64_t)C.g * C.held, r = 8 / C.g;
   const int64_t each = 8 * ((L.blocks * (int64_t)C.heads + r - 1) / r);
-  return each > held ? each : held;
+  return each > held || L.direct ? each : held;
 }
 
 template <typename T, int DP>
 hipError_t run_join(const ChunkProb& P, const Plan& L, const Classes& C, T* out, float* lse,
                     char* ws, hipStream_t st) {
+  if (L.direct) return hipSuccess;
   const int64_t most = (int64_t)C.held * C.g * L.slot_waves * 4;
   const dim3 grid((unsigned)(most < kJoinGrid ? most : kJoinGrid));
   hipLaunchKernelGGL((chunk_join_kernel<T, DP>), grid, dim3(256), 0, st, P, L, C, ws, out, lse);
@@ -972,8 +1125,12 @@ hipError_t run_f32(const ChunkProb& P, const Plan& L, const float* q, const floa
                    const float* vp, float* out, float* lse, char* ws, hipStream_t st) {
   const Classes C = Classes::of(P.Hk, per_unit(P));
   const ChunkArgs A{P, L, C, FastDiv::of(P.page), P.scale * kLog2e, q, kp, vp, out, lse, ws};
-  hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES>), dim3((unsigned)grid_of(P, L, C)), dim3(256), 0,
-                     st, A);
+  const dim3 grid((unsigned)grid_of(P, L, C));
+  // (the rows of a pass are reached by 32-bit offsets)
+  if (P.page % 8 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23))
+    hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES, true>), grid, dim3(256), 0, st, A);
+  else
+    hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES, false>), grid, dim3(256), 0, st, A);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : run_join<float, DP>(P, L, C, out, lse, ws, st);
 }
@@ -991,10 +1148,12 @@ size_t chunk_bytes(const ChunkProb& P) { return plan_of(P).bytes; }
 hipError_t launch_chunk(const ChunkProb& P, const void* q, const void* kp, const void* vp, void* out,
                         float* lse, char* ws, hipStream_t st) {
   const Plan L = plan_of(P);
-  hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L,
-                     Classes::of(P.Hk, per_unit(P)), ws);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (!L.direct) {
+    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlan), 0, st, P, L,
+                       Classes::of(P.Hk, per_unit(P)), ws);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (P.dtype == CA_BF16) {
     const bf16 *a = (const bf16*)q, *b = (const bf16*)kp, *c = (const bf16*)vp;
     return P.d == 64 ? run_bf16<64>(P, L, a, b, c, (bf16*)out, lse, ws, st)

@@ -44,7 +44,7 @@ struct BlockOrder {
 // Tiles of keys and values whose rows lie `stride` apart
 template <int D>
 struct DenseTiles : WalkRows {
-  static constexpr bool kHoles = false;
+  static constexpr bool kHoles = false, kBegun = false;
   static constexpr float kMostSum = 0x1p22f;
   static constexpr int NW = 4, RB = 2 * D, TILE = KT * RB;
   const bf16 *kbase, *vbase;

@@ -42,7 +42,8 @@ __device__ __forceinline__ int tile_class(const KeyRange& a, const KeyRange& z, 
 }
 
 // What the walk knows of its tiles and rows; a Tiles class adds
-//   void first_k()            starts the copy of tile t0's keys into key buffer 0
+//   void first_k()            starts the copy of tile t0's keys into key buffer 0; with kBegun
+//                             these, its values and the keys of tile t0 + 1 are on their way
 //   void issue_k(t, buf)      ... of tile t's keys into key buffer `buf`
 //   void issue_v(t, buf)      ... of tile t's values into value buffer `buf`
 //   void issue_both(t)        ... of both into the buffers 0
@@ -242,6 +243,8 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
     };
     load(0);
     float p[8];
+    // (products before the other wavefront's exponentials: 1 to 4%)
+    if constexpr (Tiles::kBegun) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int n = 0; n < 4 * SV; ++n) {
       const int mt = n / SV / 2, s2 = n / SV % 2, st = n % SV;
@@ -260,6 +263,7 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (Tiles::kBegun) __builtin_amdgcn_s_setprio(0);
     if (raised) rescale();
   };
   const std::integral_constant<int, 0> even;
@@ -275,8 +279,12 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
   };
   reset();
   if (T.t0 < T.t1) {
-    T.first_k();
-    copies(even, T.t0);
+    if constexpr (Tiles::kBegun) {
+      sync_stage();
+    } else {
+      T.first_k();
+      copies(even, T.t0);
+    }
     if (T.real == 0) {  // no rows: copies only
       for (int t = T.t0 + 1; t < T.t1; t += 2) {
         copies(odd, t);
