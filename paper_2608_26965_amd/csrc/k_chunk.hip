@@ -30,7 +30,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPlan = 256;       // threads of the planning workgroup
 constexpr int kF32Rows = 64;     // rows of a block, fp32
 constexpr int kXcdUnits = 32;    // compute units of an XCD
+constexpr int kMostHeld = 8 * kXcdUnits * 3;  // workgroups that run at a time, at most
 constexpr int kShareTiles = 4;   // tiles of a share, at least
+constexpr int kMostParts = 128;  // of a block, about
 constexpr int kStart = 4;        // what starting a block costs, in tiles
 constexpr int kJoinCost = 16;    // what cutting and joining costs
 constexpr int kSnap = 3;         // shares begin no nearer to a block's ends, in tiles
@@ -133,6 +135,7 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   __shared__ int most_of[kPlan / 64];
   __shared__ int first[kPlan], s_n[kPlan], s_lq[kPlan], s_lk[kPlan], s_start[kPlan];
   __shared__ int64_t index[kIndex];  // cost of every 2^step-th block
+  __shared__ int place[kMostHeld + 1], tile[kMostHeld + 1];  // where the shares begin
   __shared__ int n_cuts;
   Block* list = (Block*)(ws + L.block_at);
   Turn* turns = (Turn*)(ws + L.turn_at);
@@ -200,8 +203,10 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
                              : (int)((int64_t)(C.held - left) * max(0, 2 * mean - longest) / C.held);
   const bool whole = max((int64_t)longest - share, (int64_t)idle) <= kJoinCost + share / 20;
   const int rounds = (int)min((int64_t)kMostRounds, share / longest);
+  // few tiles: fewer shares; the joining of more parts of a block costs more than they save
   const int n = rounds > 0 ? C.held
-                           : (int)min((int64_t)C.held, (all + kShareTiles - 1) / kShareTiles);
+                           : (int)min((int64_t)C.held, min((all + kShareTiles - 1) / kShareTiles,
+                                                           1 + kMostParts * all / longest));
   if (tid == 0) *(PlanHead*)ws = PlanHead{seen, n, 0, whole};
   if (whole) return;
   // cost of the class's blocks before the i-th
@@ -251,6 +256,8 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
         }
       }
     }
+    place[u] = hs * seen + block;
+    tile[u] = t;
     Turn* x = turns + u;
     if (u < n) {
       x->hs = hs;
@@ -268,18 +275,18 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   }
   __syncthreads();
   for (int u = 1 + tid; u < n; u += kPlan) {
-    const Turn &s = turns[u], &p = turns[u - 1];
-    if (s.t == 0 || (p.t > 0 && p.hs == s.hs && p.block == s.block)) continue;
+    const int at = place[u], h = at / seen;
+    if (tile[u] == 0 || (tile[u - 1] > 0 && place[u - 1] == at)) continue;
     int lo = u, hi = n;  // share lo begins in the block, share hi after it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (turns[mid].hs == s.hs && turns[mid].block == s.block)
+      if (place[mid] == at)
         lo = mid;
       else
         hi = mid;
     }
-    const Block b = list[s.block];
-    cuts[atomicAdd(&n_cuts, 1)] = Cut{s.hs, u, lo - u + 2, b.a, b.lq, b.start, 0, 0};
+    const Block b = list[at - h * seen];
+    cuts[atomicAdd(&n_cuts, 1)] = Cut{h, u, lo - u + 2, b.a, b.lq, b.start, 0, 0};
   }
   __syncthreads();
   if (tid == 0) ((PlanHead*)ws)->cuts = n_cuts;
