@@ -203,16 +203,26 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
                              : (int)((int64_t)(C.held - left) * max(0, 2 * mean - longest) / C.held);
   const bool whole = max((int64_t)longest - share, (int64_t)idle) <= kJoinCost + share / 20;
   const int rounds = (int)min((int64_t)kMostRounds, share / longest);
-  // few tiles: fewer shares; the joining of more parts of a block costs more than they save
-  const int n = rounds > 0 ? C.held
-                           : (int)min((int64_t)C.held, min((all + kShareTiles - 1) / kShareTiles,
-                                                           1 + kMostParts * all / longest));
+  // Few tiles: fewer shares (the joining of more parts of a block costs more than they save), as
+  // many on each compute unit
+  int n = C.held;
+  if (rounds == 0) {
+    const int units = 8 / C.g * kXcdUnits;
+    n = (int)min((int64_t)n, min((all + kShareTiles - 1) / kShareTiles, 1 + kMostParts * all / longest));
+    if (n > units) n -= n % units;
+  }
   if (tid == 0) *(PlanHead*)ws = PlanHead{seen, n, 0, whole};
   if (whole) return;
+  // cost of the blocks before one
+  auto before_block = [&](int i) -> int64_t {
+    if (i == seen) return cost;
+    if (step == 0) return index[i];
+    return list[i].cost;
+  };
   // cost of the class's blocks before the i-th
   auto cost_of = [&](int i) {
-    const int h = i / seen, k = i - h * seen;
-    return h * cost + (step == 0 ? index[k] : list[k].cost);
+    const int h = i / seen;
+    return h * cost + before_block(i - h * seen);
   };
   for (int u = tid; u <= n; u += kPlan) {
     int hs = C.heads, block = 0, t = 0;
@@ -244,8 +254,7 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
           hi = mid;
       }
       block = lo;
-      const int64_t c = step == 0 ? index[lo] : list[lo].cost;
-      const int64_t e = lo + 1 == seen ? cost : step == 0 ? index[lo + 1] : list[lo + 1].cost;
+      const int64_t c = before_block(lo), e = before_block(lo + 1);
       t = max(0, (int)(off - c) - kStart);
       if (t < kSnap) t = 0;
       if (t > 0 && (int)(e - c) - kStart - t < kSnap) {  // at the next block's beginning instead
@@ -802,12 +811,18 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
     if (row >= rows || (few && w >= NG)) continue;
     const int tok = row / P.G, h = (cut.hs * C.g + cls) * P.G + row - tok * P.G;
     T* o = out + (cut.start + tok) * P.o_st + h * P.o_sh;
+    const float inv = 1.f / l;
 #pragma unroll
     for (int j = 0; j < JC; ++j) {
       const int dim = 4 * (64 / WR * (j0 + j) + lane / WR);
-      if (dim < P.d)
+      if (dim >= P.d) continue;
+      f32x4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) store_f(o + dim + e, l != 0.f ? a[j][e] / l : 0.f);
+      for (int e = 0; e < 4; ++e) y[e] = l != 0.f ? a[j][e] * inv : 0.f;
+      if constexpr (BF)
+        *(bf16x4*)(o + dim) = bf16x4{f2bf(y[0]), f2bf(y[1]), f2bf(y[2]), f2bf(y[3])};
+      else
+        *(f32x4*)(o + dim) = y;
     }
     if (lse && j0 == 0 && lane < WR)
       lse[(size_t)(cut.start + tok) * P.H + h] =
