@@ -35,7 +35,7 @@ constexpr int kShareTiles = 4;   // tiles of a share, at least
 constexpr int kMostParts = 128;  // of a block, about
 constexpr int kStart = 4;        // what starting a block costs, in tiles
 constexpr int kJoinCost = 16;    // what cutting and joining costs
-constexpr int kSnap = 3;         // shares begin no nearer to a block's ends, in tiles
+constexpr int kSnap = 2;         // shares begin no nearer to a block's ends, in tiles
 constexpr int kMostRounds = 8;   // of whole blocks before the shares
 constexpr int kIndex = 2048;     // entries of the planning workgroup's index of the blocks
 constexpr int kDirectTiles = 24; // blocks of so few tiles are not planned
