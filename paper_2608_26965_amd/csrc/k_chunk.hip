@@ -202,7 +202,9 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   const int idle = left == 0 ? 0
                              : (int)((int64_t)(C.held - left) * max(0, 2 * mean - longest) / C.held);
   const bool whole = max((int64_t)longest - share, (int64_t)idle) <= kJoinCost + share / 20;
-  const int rounds = (int)min((int64_t)kMostRounds, share / longest);
+  // (a share is what is left beside the whole blocks: some tiles for each workgroup, so that no two
+  // shares begin at the same tile and every part of a block has some)
+  const int rounds = (int)max((int64_t)0, min((int64_t)kMostRounds, (share - kShareTiles) / longest));
   // Few tiles: fewer shares (the joining of more parts of a block costs more than they save), as
   // many on each compute unit
   int n = C.held;

@@ -718,3 +718,104 @@ def test_numbers_given_as_tensors_are_read_anew_by_chunks():
         assert ca.cache_grow(pool, rows, n, _i32([20]), tokens).slots.shape[0] == t
         ca.cache_release(pool, rows, n, left=left)
         assert int((rows >= 0).sum()) == 1 + (m > 10)
+
+
+# ---- how the work is divided -----------------------------------------------------------------------
+
+def _divided(dt, tokens, H, Hk, d, page, pick, wide=0, scale=None, **kw):
+    """A call of many blocks: the bounds of some sequences and heads (`pick`), checked on the GPU in 64 bits.
+    tokens: (all, new) of each sequence; wide: tokens that the table has room for."""
+    import torch
+    ca = _ca()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(len(tokens) + H)
+    lens, new = [a for a, _ in tokens], [n for _, n in tokens]
+    need = [-(-n // page) for n in lens]
+    width = max(max(need), -(-wide // page))
+    pool = sum(need) + 1
+    order = torch.randperm(pool, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), width), -1, dtype=torch.int32, device="cuda")
+    at = np.cumsum([0] + need)
+    for b, n in enumerate(need):
+        table[b, :n] = order[at[b]:at[b + 1]]
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=_torch(dt))  # noqa: E731
+    kp, vp = rnd(pool, page, Hk, d), rnd(pool, page, Hk, d)
+    starts = np.cumsum([0] + new).tolist()
+    q = rnd(starts[-1], H, d)
+    args = ca.Window(**kw), q, kp, vp, table, _i32(lens), _i32(starts)
+    out, lse = ca.paged_chunk_attn(*args, scale=scale, want_lse=True)
+    # again, into tensors and a workspace of NaN: nothing is left out, nothing read that was not written
+    again = torch.full_like(out, math.nan), torch.full_like(lse, math.nan)
+    ca.paged_chunk_attn(*args, scale=scale, out=again[0], lse=again[1],
+                        ws=torch.full((160 << 20,), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    assert bool(torch.isfinite(out).all())
+    scale = scale or 1.0 / math.sqrt(d)
+    u, r = _u(dt), 2.0 ** -8 if dt == "bf16" else 0.0
+    for b, h in pick:
+        n, a, hk = new[b], lens[b], h // (H // Hk)
+        j = torch.arange(a, device="cuda")
+        e = table[b, j // page].long()
+        k, v = (x[e, j % page, hk].double() for x in (kp, vp))
+        x = q[starts[b]:starts[b + 1], h].double()
+        p = (torch.arange(n, device="cuda") + a - n)[:, None]
+        see = torch.ones(n, a, dtype=torch.bool, device="cuda")
+        if kw.get("left", -1) >= 0:
+            see &= j >= p - kw["left"]
+        if kw.get("right", -1) >= 0:
+            see &= j <= p + kw["right"]
+        see |= (j < kw.get("sinks", 0))[None]
+        if kw.get("causal"):
+            see &= j <= p
+        s = torch.where(see, x @ k.T * scale, -math.inf)
+        want_lse = torch.logsumexp(s, 1)
+        P = torch.exp(s - want_lse[:, None])
+        o, A = P @ v, P @ v.abs()
+        w = 2 * (d + 8) * 2.0 ** -24 * scale * (x.abs() @ k.abs().T).max() + 2.0 ** -20
+        got, gl = out[starts[b]:starts[b + 1], h].double(), lse[starts[b]:starts[b + 1], h].double()
+        assert ((got - o).abs() <= u * o.abs() + (r + w) * A).all(), f"sequence {b} head {h}"
+        assert ((gl - want_lse).abs() <= 2 * w + 2.0 ** -23 * want_lse.abs()).all(), f"lse of sequence {b} head {h}"
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("H,Hk", [(4, 1), (2, 2), (3, 3), (8, 4), (5, 5), (6, 6), (16, 8), (12, 12), (20, 20)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_shares_over_every_number_of_heads(dt, H, Hk, d):
+    """Key heads that the XCDs take alone, in twos, fours or together; blocks that are cut."""
+    tokens = [(3000, 200), (2500, 1), (1700, 333), (1, 1), (4100, 77)]
+    _divided(dt, tokens, H, Hk, d, 32, [(0, 0), (1, H - 1), (2, H // 2), (3, 0), (4, H - 1)], causal=True)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("kw", [dict(), dict(left=1500, sinks=300), dict(causal=True)])
+def test_chunk_whole_rounds_and_shares(dt, kw):
+    """A little more than one, two and three rounds of blocks: whole ones first, the rest in shares."""
+    for H, n in ((40, 700 if dt == "f32" else 1560), (40, 2 * 1560), (16, 900)):
+        _divided(dt, [(2000 + n, n)], H, H, 128, 32, [(0, 0), (0, H // 2 + 1), (0, H - 1)], **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_chunk_many_sequences(dt):
+    """More sequences than the planning workgroup takes at a time, with and without new tokens; more than a call
+    without a plan has, and as many."""
+    r = random.Random(5)
+    for B, wide in ((700, 0), (256, 0), (257, 0), (300, 5000)):
+        tokens = [(a, min(a, r.choice((0, 1, 1, 2, 40)))) for a in (r.randrange(0, 300) for _ in range(B))]
+        tokens[3] = (2000, 17) if wide else tokens[3]
+        tokens[-1] = (250, 60)
+        _divided(dt, tokens, 4, 2, 64, 16, [(3, 1), (B - 1, 3)] + [(b, 0) for b in range(0, B, 61) if tokens[b][1]],
+                 wide=wide, causal=True)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_chunk_more_blocks_than_the_index(dt):
+    """Thousands of blocks, of which some are cut."""
+    tokens = [(1100, 1000)] * 34 + [(9000, 3)]
+    _divided(dt, tokens, 8, 1, 64, 64, [(0, 0), (17, 3), (33, 7), (34, 5)], wide=9500, causal=True)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("page", [8, 16, 24, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunk_pages_that_end_inside_tiles(dt, page, d):
+    _divided(dt, [(1000, 150), (777, 3), (2049, 65)], 4, 2, d, page, [(0, 0), (1, 3), (2, 2)], left=600, sinks=70, causal=True)
