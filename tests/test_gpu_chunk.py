@@ -819,3 +819,51 @@ def test_chunk_more_blocks_than_the_index(dt):
 @pytest.mark.parametrize("d", [64, 128])
 def test_chunk_pages_that_end_inside_tiles(dt, page, d):
     _divided(dt, [(1000, 150), (777, 3), (2049, 65)], 4, 2, d, page, [(0, 0), (1, 3), (2, 2)], left=600, sinks=70, causal=True)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("kind", ["tokens the same", "tokens overlapping", "heads the same", "pages the same", "tokens far apart",
+                                  "pages far apart"])
+def test_chunk_pools_of_any_strides(dt, kind):
+    """Strides of 0, strides below a row's length, and offsets past 2^32 bytes on every way to address
+    a row give the bits that a dense copy gives; an output may lie where the queries do."""
+    import torch
+    ca = _ca()
+    g, D, P, page, Hk = _gen(60), 64, 5, 16, 2
+    shape, unit = (P, page, Hk, D), 128 // torch.finfo(_torch(dt)).bits  # elements of 16 bytes
+    strides = {"tokens the same": (Hk * D, 0, D, 1), "tokens overlapping": (page * Hk * D, unit, 4 * D, 1),
+               "heads the same": (page * D, D, 0, 1), "pages the same": (0, Hk * D, D, 1),
+               "tokens far apart": (Hk * D, (1 << 23) - unit, D, 1), "pages far apart": ((1 << 30) - unit, Hk * D, D, 1)}[kind]
+    size = sum((n - 1) * s for n, s in zip(shape, strides)) + 1
+    pools = []
+    for i in range(2):
+        if size > 1 << 24:
+            x = torch.empty(size, dtype=_torch(dt), device="cuda").as_strided(shape, strides)
+            x.copy_(_rand(g, shape, dt))
+        else:
+            x = _rand(g, (size,), dt).cuda().as_strided(shape, strides)
+        pools.append(x)
+    for lens, new in (([70, 33], [40, 2]), ([9, 80], [9, 80])):
+        table = _i32([[4, 1, 3, 0, 2], [0, 2, 4, 1, 3]])
+        starts = _i32(np.cumsum([0] + new).tolist())
+        q = _rand(g, (sum(new), 4, D), dt).cuda()
+        for w in (ca.Window(causal=True), ca.Window(left=20, right=5, sinks=3)):
+            a, la = ca.paged_chunk_attn(w, q, *pools, table, _i32(lens), starts, want_lse=True)
+            b, lb = ca.paged_chunk_attn(w, q, *(x.contiguous() for x in pools), table, _i32(lens), starts, want_lse=True)
+            assert torch.equal(a, b) and torch.equal(la, lb)
+            c = q.clone()
+            ca.paged_chunk_attn(w, c, *pools, table, _i32(lens), starts, out=c)
+            assert torch.equal(c, a)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_chunk_cut_blocks_may_be_written_over_their_queries(dt):
+    import torch
+    ca = _ca()
+    lens, w = [9000, 30, 4000], ca.Window(causal=True)
+    kp, vp, table, _ = _pages(_gen(61), dt, lens, 16, 2, 64)
+    q = _rand(_gen(62), (240, 4, 64), dt).cuda()
+    n, starts = _i32(lens), _i32([0, 10, 40, 240])
+    a, _ = ca.paged_chunk_attn(w, q, kp, vp, table, n, starts)
+    ca.paged_chunk_attn(w, q, kp, vp, table, n, starts, out=q)
+    assert torch.equal(q, a)
