@@ -881,11 +881,23 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 // neither the keys' 16-byte reads nor the values' 4-byte reads meet on a bank. What bounds
 // it: the matrix instructions, 32 cycles each.
 
+// The largest x of lanes l, l ^ 16, l ^ 32 and l ^ 48
+__device__ __forceinline__ float max_of_groups(float x) {
+  auto larger = [](uint32_t a, uint32_t b) {
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+  };
+  uint32_t y = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  y = __builtin_bit_cast(uint32_t, larger(a[0], a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return larger(b[0], b[1]);
+}
+
 template <int DP, int WAVES, bool GROUPS>
 __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     const ChunkArgs) {
   constexpr int HK = 32, NJ = DP / 16, LD = DP + 4, NC = DP / 4;
-  constexpr int RP = 256 / NC, NP = HK / RP;  // rows of a pass of the copy, passes
+  constexpr int RP = 64 / NC, NP = 8 / RP;  // rows of a wavefront's pass of the copy, passes
   __shared__ __attribute__((aligned(16))) float ks[2][HK][LD], vs[2][HK][LD];
   __shared__ uint32_t gone[4], bad[4];  // keys not there, values that are not finite
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, l16 = lane & 15;
@@ -918,7 +930,6 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
         qf[j] = x < d ? *(const f32x4*)(src + x) : f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
-    const int cc = 4 * (tid % NC), cr = tid / NC;  // this thread's piece of a row, and row
     const int32_t* table = A->P.table + it.b * A->P.table_sb;
     const float *kh = (const float*)A->kp + hk * A->P.k_sh, *vh = (const float*)A->vp + hk * A->P.v_sh;
     const int64_t k_sp = A->P.k_sp, k_st = A->P.k_st, v_sp = A->P.v_sp, v_st = A->P.v_st;
@@ -928,53 +939,72 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     auto first_key = [&](int i) __attribute__((always_inline)) {
       return KT * list.tile(it.t0 + (i >> 1)) + HK * (i & 1);
     };
-    // Entries of half tile i's rows, a half tile before the rows are loaded. GROUPS: pages of a
-    // multiple of 8 tokens, so that the rows of a wavefront's pass lie on one page and its entry
-    // and their address are scalars (the lookups in vectors cost a fifth of the instructions).
-    const int lr = cr - w * (RP / 4);  // row within the wavefront's
-    const uint32_t k_off = GROUPS ? (uint32_t)(lr * k_st + cc) * 4 : 0;  // bytes
-    const uint32_t v_off = GROUPS ? (uint32_t)(lr * v_st + cc) * 4 : 0;
-    int ent[NP];
-    auto entries = [&](int i) __attribute__((always_inline)) {
-      const int j0 = first_key(min(i, n - 1)) + (GROUPS ? w * (RP / 4) : cr);
+    // A wavefront copies rows 8 w .. 8 w + 7 of a half tile, RP of them a pass: this lane's piece of
+    // a row, and its row in the first pass. Their entries are loaded a half tile before the rows.
+    // GROUPS: pages of a multiple of 8 tokens, so that the eight lie on one page, whose entry
+    // is one scalar load and whose place is found once (one for each pass: 284 us instead of 245
+    // for 8 tokens on 16,000 each, 32 heads on 8 of 128).
+    const int cc = 4 * (lane % NC), lr = lane / NC, cr = 8 * w + lr;
+    uint32_t k_off[NP], v_off[NP];  // bytes
 #pragma unroll
-      for (int x = 0; x < NP; ++x) {
-        const int e = by_page.div(min(j0 + x * RP, it.lk - 1));
-        if constexpr (GROUPS)
-          ent[x] = ((Entries)table)[__builtin_amdgcn_readfirstlane(e)];
-        else
-          ent[x] = table[e];
+    for (int x = 0; x < NP; ++x) {
+      k_off[x] = GROUPS ? (uint32_t)((lr + x * RP) * k_st + cc) * 4 : 0;
+      v_off[x] = GROUPS ? (uint32_t)((lr + x * RP) * v_st + cc) * 4 : 0;
+    }
+    int ent[GROUPS ? 1 : NP], in = 0;
+    auto entries = [&](int i) __attribute__((always_inline)) {
+      const int j0 = first_key(min(i, n - 1));
+      if constexpr (GROUPS) {
+        const int j = min(j0 + 8 * w, it.lk - 1), e = by_page.div(j);
+        ent[0] = ((Entries)table)[__builtin_amdgcn_readfirstlane(e)];
+        in = j - e * page;
+      } else {
+#pragma unroll
+        for (int x = 0; x < NP; ++x) ent[x] = table[by_page.div(min(j0 + cr + x * RP, it.lk - 1))];
       }
     };
     f32x4 kr[NP], vr[NP];
     uint32_t missing;
     auto load = [&](int i) __attribute__((always_inline)) {
       missing = 0;
-      const int j0 = first_key(i) + (GROUPS ? w * (RP / 4) : cr);
 #pragma unroll
-      for (int x = 0; x < NP; ++x) {
-        const int j = j0 + x * RP, e = ent[x], c = min(j, it.lk - 1), in = c - by_page.div(c) * page;
-        const bool there = e >= 0 && e < pages;
-        kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (GROUPS) {
-          if (there && j < it.lk) {
-            const char* ks0 = (const char*)(kh + (e * k_sp + in * k_st));
-            const char* vs0 = (const char*)(vh + (e * v_sp + in * v_st));
-            if (j + RP / 4 <= it.lk && d == DP) {
-              kr[x] = *(const f32x4*)(ks0 + k_off);
-              vr[x] = *(const f32x4*)(vs0 + v_off);
-            } else if (j + lr < it.lk && cc < d) {
-              kr[x] = *(const f32x4*)(ks0 + k_off);
-              vr[x] = *(const f32x4*)(vs0 + v_off);
-            }
-          }
-          if (!there && j + lr < it.lk) missing |= 1u << (cr + x * RP);
+      for (int x = 0; x < NP; ++x) kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (GROUPS) {
+        const int j0 = first_key(i) + 8 * w, e = ent[0];
+        if (j0 >= it.lk) return;
+        if (e < 0 || e >= pages) {
+          missing = 0xffu << (8 * w);
+          return;
+        }
+        const char* ks0 = (const char*)kh + (uint64_t)(uint32_t)e * (uint32_t)(4 * k_sp) +
+                          (uint64_t)(uint32_t)in * (uint32_t)(4 * k_st);
+        const char* vs0 = (const char*)vh + (uint64_t)(uint32_t)e * (uint32_t)(4 * v_sp) +
+                          (uint64_t)(uint32_t)in * (uint32_t)(4 * v_st);
+        if (j0 + 8 <= it.lk && d == DP) {
+#pragma unroll
+          for (int x = 0; x < NP; ++x) kr[x] = *(const f32x4*)(ks0 + k_off[x]);
+#pragma unroll
+          for (int x = 0; x < NP; ++x) vr[x] = *(const f32x4*)(vs0 + v_off[x]);
         } else {
-          if (there && j < it.lk && cc < d) {
-            kr[x] = *(const f32x4*)(kh + e * k_sp + in * k_st + cc);
-            vr[x] = *(const f32x4*)(vh + e * v_sp + in * v_st + cc);
+#pragma unroll
+          for (int x = 0; x < NP; ++x)
+            if (j0 + lr + x * RP < it.lk && cc < d) {
+              kr[x] = *(const f32x4*)(ks0 + k_off[x]);
+              vr[x] = *(const f32x4*)(vs0 + v_off[x]);
+            }
+        }
+      } else {
+        const int j0 = first_key(i) + cr;
+#pragma unroll
+        for (int x = 0; x < NP; ++x) {
+          const int j = j0 + x * RP, e = ent[x], at = j - by_page.div(min(j, it.lk - 1)) * page;
+          if (j >= it.lk) continue;
+          if (e < 0 || e >= pages) {
+            missing |= 1u << (cr + x * RP);
+          } else if (cc < d) {
+            kr[x] = *(const f32x4*)(kh + e * k_sp + at * k_st + cc);
+            vr[x] = *(const f32x4*)(vh + e * v_sp + at * v_st + cc);
           }
-          if (!there && j < it.lk) missing |= 1u << (cr + x * RP);
         }
       }
     };
@@ -1006,11 +1036,14 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
       const int k0 = first_key(i);
       // no row sees a key; every row sees all
       if (k0 >= rz.s_end && (k0 >= rz.hi || k0 + HK <= ra.lo)) return;
-      const uint32_t hv = gone[i & 3], bv = bad[i & 3];
+      const uint32_t hv = __builtin_amdgcn_readfirstlane(gone[i & 3]);
+      const uint32_t bv = __builtin_amdgcn_readfirstlane(bad[i & 3]);
       const bool all = (k0 + HK <= ra.s_end || (k0 >= rz.lo && k0 + HK <= ra.hi)) && hv == 0;
       const float(*kt)[LD] = ks[i & 1];
       const float(*vt)[LD] = vs[i & 1];
       // four partial sums a logit: shorter chains of rounded sums
+      // products go before the other wavefronts' exponentials (1 to 2% of the time)
+      __builtin_amdgcn_s_setprio(2);
       f32x4 p[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -1025,6 +1058,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
           for (int e = 0; e < 4; ++e)
             p[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[j][e], p[u][e], 0, 0, 0);
         }
+      __builtin_amdgcn_s_setprio(0);
       float s[2][4], mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -1035,8 +1069,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
           if (!all && (!sees(mine, k0 + j) || ((hv >> j) & 1))) s[u][r] = -INFINITY;
           mx = fmaxf(mx, s[u][r]);
         }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
+      mx = max_of_groups(mx) * sl2;
       if (__builtin_amdgcn_ballot_w64(mx > m)) {
         const float m1 = fmaxf(m, mx), al = m1 > m ? __builtin_amdgcn_exp2f(m - m1) : 1.f;
         l *= al;
@@ -1193,8 +1226,9 @@ hipError_t run_f32(const ChunkProb& P, const Plan& L, const float* q, const floa
   const Classes C = Classes::of(P.Hk, per_unit(P));
   const ChunkArgs A{P, L, C, FastDiv::of(P.page), P.scale * kLog2e, q, kp, vp, out, lse, ws};
   const dim3 grid((unsigned)grid_of(P, L, C));
-  // (the rows of a pass are reached by 32-bit offsets)
-  if (P.page % 8 == 0 && P.k_st <= (1 << 23) && P.v_st <= (1 << 23))
+  // the rows of a page that a group of 8 takes are reached by 32-bit offsets from scalar bases
+  auto fits = [](int64_t sp, int64_t st) { return sp < (1 << 30) && st <= (1 << 23); };
+  if (P.page % 8 == 0 && fits(P.k_sp, P.k_st) && fits(P.v_sp, P.v_st))
     hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES, true>), grid, dim3(256), 0, st, A);
   else
     hipLaunchKernelGGL((chunk_f32_kernel<DP, WAVES, false>), grid, dim3(256), 0, st, A);
