@@ -952,8 +952,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
       v_off[x] = GROUPS ? (uint32_t)((lr + x * RP) * v_st + cc) * 4 : 0;
     }
     int ent[GROUPS ? 1 : NP], in = 0;
-    auto entries = [&](int i) __attribute__((always_inline)) {
-      const int j0 = first_key(min(i, n - 1));
+    auto entries = [&](int j0) __attribute__((always_inline)) {  // j0: the half tile's first key
       if constexpr (GROUPS) {
         const int j = min(j0 + 8 * w, it.lk - 1), e = by_page.div(j);
         ent[0] = ((Entries)table)[__builtin_amdgcn_readfirstlane(e)];
@@ -965,12 +964,12 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     };
     f32x4 kr[NP], vr[NP];
     uint32_t missing;
-    auto load = [&](int i) __attribute__((always_inline)) {
+    auto load = [&](int first) __attribute__((always_inline)) {
       missing = 0;
 #pragma unroll
       for (int x = 0; x < NP; ++x) kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (GROUPS) {
-        const int j0 = first_key(i) + 8 * w, e = ent[0];
+        const int j0 = first + 8 * w, e = ent[0];
         if (j0 >= it.lk) return;
         if (e < 0 || e >= pages) {
           missing = 0xffu << (8 * w);
@@ -994,7 +993,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
             }
         }
       } else {
-        const int j0 = first_key(i) + cr;
+        const int j0 = first + cr;
 #pragma unroll
         for (int x = 0; x < NP; ++x) {
           const int j = j0 + x * RP, e = ent[x], at = j - by_page.div(min(j, it.lk - 1)) * page;
@@ -1011,20 +1010,19 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     auto store = [&](int i) __attribute__((always_inline)) {
       if (missing) atomicOr(&gone[i & 3], missing);
 #pragma unroll
-      for (int x = 0; x < NP; ++x) {
-        const int r = cr + x * RP;
-        bool fine = true;
+      for (int x = 0; x < NP; ++x) *(f32x4*)&ks[i & 1][cr + x * RP][cc] = kr[x];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) fine &= fabsf(vr[x][e]) < INFINITY;
-        if (__builtin_expect(!fine, 0)) {
+      for (int x = 0; x < NP; ++x) {
+        // 0, or NaN if a value is not finite
+        const float z = fmaf(vr[x][0], 0.f, vr[x][1] * 0.f) + fmaf(vr[x][2], 0.f, vr[x][3] * 0.f);
+        if (__builtin_expect(z != 0.f, 0)) {
           // zero times it would reach rows that do not see it: those that do get NaN at the end
-          atomicOr(&bad[i & 3], 1u << r);
+          atomicOr(&bad[i & 3], 1u << (cr + x * RP));
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (!(fabsf(vr[x][e]) < INFINITY)) vr[x][e] = 0.f;
         }
-        *(f32x4*)&ks[i & 1][r][cc] = kr[x];
-        *(f32x4*)&vs[i & 1][r][cc] = vr[x];
+        *(f32x4*)&vs[i & 1][cr + x * RP][cc] = vr[x];
       }
     };
     f32x4 o[NJ];
@@ -1032,8 +1030,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     bool poison = false;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto compute = [&](int i) __attribute__((always_inline)) {
-      const int k0 = first_key(i);
+    auto compute = [&](int i, int k0) __attribute__((always_inline)) {
       // no row sees a key; every row sees all
       if (k0 >= rz.s_end && (k0 >= rz.hi || k0 + HK <= ra.lo)) return;
       const uint32_t hv = __builtin_amdgcn_readfirstlane(gone[i & 3]);
@@ -1101,17 +1098,21 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     if (tid < 4) gone[tid] = bad[tid] = 0;
     __syncthreads();
     if (n > 0) {
-      entries(0);
-      load(0);
-      entries(1);
+      int k0 = first_key(0), k1 = first_key(1);  // first keys of half tiles i and i + 1
+      entries(k0);
+      load(k0);
+      entries(k1);
       store(0);
       __syncthreads();
       for (int i = 0; i < n; ++i) {
-        if (i + 1 < n) load(i + 1);
-        entries(i + 2);
+        const int k2 = first_key(min(i + 2, n - 1));
+        if (i + 1 < n) load(k1);
+        entries(k2);
         // the flags of half tile i + 2 (those of i - 2 were read before the last barrier)
         if (tid == 0) gone[(i + 2) & 3] = bad[(i + 2) & 3] = 0;
-        if (wreal) compute(i);
+        if (wreal) compute(i, k0);
+        k0 = k1;
+        k1 = k2;
         if (i + 1 < n) store(i + 1);
         __syncthreads();
       }
