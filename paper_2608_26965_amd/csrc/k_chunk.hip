@@ -95,6 +95,27 @@ struct BlockSpan {
   }
 };
 
+// The order in which a block walks its tiles: the sinks', then the window's. Where the window of
+// the sequence's last token begins inside this block's, from there to the last tile, and on from
+// the first: blocks beside each other, whose windows are shifted, then read the same keys at a
+// time (2 x 1,560 rows on windows of 4,679: 519 -> 509 us. Taken modulo the window's length
+// by blocks further from the last token too: 178 -> 183 us for windows of 1,023).
+struct BlockTiles {
+  int ns, wrap, off, back;
+  __device__ __forceinline__ BlockTiles() {}
+  __device__ __forceinline__ BlockTiles(const WinMask& m, const TileList& l, int lk) {
+    const int nw = l.n - l.ns, from = max(l.ns, max(0, lk - 1 - m.left) / KT) - l.b0;
+    const int turn = from < nw ? from : 0;
+    ns = l.ns;
+    wrap = l.n - turn;
+    off = l.b0 - l.ns + turn;
+    back = off - nw;
+  }
+  __device__ __forceinline__ int tile(int t) const {
+    return t + (t < ns ? 0 : t < wrap ? off : back);
+  }
+};
+
 // Sum of x over the threads before this one, and over all of them
 __device__ __forceinline__ int64_t plan_scan(int64_t x, int64_t (&sums)[kPlan / 64],
                                              int64_t* total) {
@@ -572,7 +593,9 @@ struct PagedTiles : WalkRows {
   uint32_t lds0;
   int w, lane;
   Place pv, pk;  // of the tile whose values, and of the one whose keys are next
+  BlockTiles order;
 
+  __device__ __forceinline__ int tile(int t) const { return order.tile(t); }
   __device__ __forceinline__ int key(int t) const {
     return KT * tile(t) + 16 * w + (GROUPS ? 0 : lane & 15);
   }
@@ -691,6 +714,7 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
     PagedTiles<D, GROUPS> T;
     T.mask = WinMask{A->P.m.left, A->P.m.right, A->P.m.sinks, A->P.m.causal};
     T.list = visible_tiles<KT>(T.mask, span.p0, span.p1, it.lk);
+    T.order = BlockTiles(T.mask, T.list, it.lk);
     T.t0 = it.t0;
     T.t1 = it.t1;
     T.lk = it.lk;
@@ -911,7 +935,7 @@ __global__ __launch_bounds__(256, WAVES) void chunk_f32_kernel(
     const int G = A->P.G, d = A->P.d, off = it.lk - it.lq, rows = it.lq * G;
     const WinMask mask{A->P.m.left, A->P.m.right, A->P.m.sinks, A->P.m.causal};
     const BlockSpan span(it.a, kF32Rows, G, it.lq, it.lk);
-    const TileList list = visible_tiles<KT>(mask, span.p0, span.p1, it.lk);
+    const BlockTiles list(mask, visible_tiles<KT>(mask, span.p0, span.p1, it.lk), it.lk);
     const int w0 = it.a * kF32Rows + 16 * w, wreal = max(0, min(16, rows - w0));
     // the wavefront's last row, this lane's
     const int wl = min(w0 + max(wreal, 1), rows) - 1, row = min(w0 + l16, wl);
