@@ -223,19 +223,10 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   const int idle = left == 0 ? 0
                              : (int)((int64_t)(C.held - left) * max(0, 2 * mean - longest) / C.held);
   const bool whole = max((int64_t)longest - share, (int64_t)idle) <= kJoinCost + share / 20;
-  // (a share is what is left beside the whole blocks: some tiles for each workgroup, so that no two
-  // shares begin at the same tile and every part of a block has some)
-  const int rounds = (int)max((int64_t)0, min((int64_t)kMostRounds, (share - kShareTiles) / longest));
-  // Few tiles: fewer shares (the joining of more parts of a block costs more than they save), as
-  // many on each compute unit
-  int n = C.held;
-  if (rounds == 0) {
-    const int units = 8 / C.g * kXcdUnits;
-    n = (int)min((int64_t)n, min((all + kShareTiles - 1) / kShareTiles, 1 + kMostParts * all / longest));
-    if (n > units) n -= n % units;
+  if (whole) {
+    if (tid == 0) *(PlanHead*)ws = PlanHead{seen, C.held, 0, 1};
+    return;
   }
-  if (tid == 0) *(PlanHead*)ws = PlanHead{seen, n, 0, whole};
-  if (whole) return;
   // cost of the blocks before one
   auto before_block = [&](int i) -> int64_t {
     if (i == seen) return cost;
@@ -247,13 +238,39 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
     const int h = i / seen;
     return h * cost + before_block(i - h * seen);
   };
-  for (int u = tid; u <= n; u += kPlan) {
+  // (a share is what is left beside the whole blocks: some tiles for each workgroup, so that no two
+  // shares begin at the same tile and every part of a block has some)
+  int rounds = (int)max((int64_t)0, min((int64_t)kMostRounds, (share - kShareTiles) / longest));
+  int n = C.held;  // shares
+  // One more round whole and the few blocks beside it in equal shares for as many workgroups as
+  // get some tiles: less to join where that evens out the work as well (2 x 40 heads of 13
+  // blocks of about 100 tiles, 512 at a time: 1,024 whole and 16 cut, not 512 and 528)
+  int64_t rest = 0;
+  bool even = true;
+  if (rounds < kMostRounds && (int64_t)(rounds + 1) * C.held <= count) {
+    rest = all - cost_of((rounds + 1) * C.held);
+    if ((int64_t)(rounds + 1) * longest + rest / C.held + kStart <= share + kJoinCost) {
+      even = false;
+      ++rounds;
+      n = (int)max((int64_t)1, min((int64_t)n, min(rest / kShareTiles, kMostParts * rest / longest)));
+    }
+  }
+  // Few tiles: fewer shares (the joining of more parts of a block costs more than they save), as
+  // many on each compute unit
+  if (rounds == 0) {
+    const int units = 8 / C.g * kXcdUnits;
+    n = (int)min((int64_t)n, min((all + kShareTiles - 1) / kShareTiles, 1 + kMostParts * all / longest));
+    if (n > units) n -= n % units;
+  }
+  const int turn = rounds > 0 ? C.held : n;  // workgroups that have something to do
+  if (tid == 0) *(PlanHead*)ws = PlanHead{seen, turn, 0, 0};
+  for (int u = tid; u <= turn; u += kPlan) {
     int hs = C.heads, block = 0, t = 0;
     if (u < n) {
       // all workgroups' whole blocks, what the shares before leave to be done by the
       // workgroups before u beside their own whole blocks
-      int64_t pos = all * u / n;
-      if (rounds > 0) {
+      int64_t pos = even ? all * u / n : cost_of(rounds * C.held) + rest * u / n;
+      if (even && rounds > 0) {
         pos += cost_of(rounds * C.held);
         for (int k = 0; k < rounds; ++k) pos -= cost_of(k * C.held + u) - cost_of(k * C.held);
       }
@@ -291,7 +308,7 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
     place[u] = hs * seen + block;
     tile[u] = t;
     Turn* x = turns + u;
-    if (u < n) {
+    if (u < turn) {
       x->hs = hs;
       x->block = block;
       x->t = t;

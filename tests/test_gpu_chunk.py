@@ -795,6 +795,17 @@ def test_chunk_whole_rounds_and_shares(dt, kw):
 
 
 @pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d,held", [(128, 64), (64, 96)])
+@pytest.mark.parametrize("rounds,extra", [(1, 1), (1, 2), (1, 9), (2, 1), (2, 3), (3, 5)])
+def test_chunk_whole_rounds_and_a_few_blocks(dt, d, held, rounds, extra):
+    """`held` blocks of a key head run at a time: some rounds of them, and a few blocks more, of one length and of two."""
+    n, rows = rounds * held + extra, 128 if dt == "bf16" else 64
+    for lens, kw in (([2000] * n, dict()), ([2000 + 100 * (b % 2) for b in range(n)], dict(causal=True))):
+        _divided(dt, [(a, rows) for a in lens], 8, 8, d, 32, [(0, 0), (n - 1, 7), (n - 2, 3), (held - 1, 1), (held, 2), (n // 2, 4)],
+                 **kw)
+
+
+@pytest.mark.parametrize("dt", DT)
 def test_chunk_many_sequences(dt):
     """More sequences than the planning workgroup takes at a time, with and without new tokens; more than a call
     without a plan has, and as many."""
