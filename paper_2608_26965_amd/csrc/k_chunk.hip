@@ -922,11 +922,12 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 // One wavefront per 16 rows, on the fp32 matrix instructions (v_mfma_f32_16x16x4_f32): S^T =
 // K Q^T leaves lane l with row l % 16 and the logits of keys 4 (l / 16) + r, which is
 // the P^T operand of O^T = V^T P^T as it stands. Half tiles of 32 keys go through registers
-// to LDS, one ahead of the one that is computed; rows of DP + 4 floats there, so that
-// neither the keys' 16-byte reads nor the values' 4-byte reads meet on a bank. What bounds
-// it: the matrix instructions, 32 cycles each (8,192 causal tokens, 8 heads of 64: 702 us, 98
-// TFLOP/s of the 154 of a large product; 8 single tokens on 16,000 each, 32 heads on 8 of 128: 238
-// us, 4.4 TB/s).
+// to LDS, one ahead of the one that is computed; rows of DP + 4 floats there spread the keys'
+// 16-byte reads and the values' 4-byte reads over the banks (counted: conflicts are 19% of the
+// cycles in which LDS is active, these 7% of all). What bounds it: the matrix instructions, 32
+// cycles each and busy 68% of the time (8,192 causal tokens, 8 heads of 64: 702 us, 98 TFLOP/s of
+// the 154 of a large product), or the cache (8 single tokens on 16,000 each, 32 heads on 8 of 128:
+// 238 us, 4.4 TB/s).
 
 // The largest x of lanes l, l ^ 16, l ^ 32 and l ^ 48
 __device__ __forceinline__ float max_of_groups(float x) {
