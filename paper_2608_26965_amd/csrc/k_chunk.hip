@@ -1217,7 +1217,7 @@ Plan plan_of(const ChunkProb& P) {
   // tiles of a block: the table's, or those of the sinks and of the window of its tokens
   int64_t tiles = ((int64_t)P.max_pages * P.page + KT - 1) / KT;
   const int64_t span = (int64_t)P.m.left + (P.m.causal ? 0 : P.m.right) + L.rows / P.G + 2;
-  tiles = std::min(tiles, span / KT + 2 + (P.m.sinks + KT - 1) / KT);
+  tiles = std::min(tiles, span / KT + 2 + ((int64_t)P.m.sinks + KT - 1) / KT);
   L.direct = P.B <= kDirectBatch && L.blocks < kDirectBlocks && tiles <= kDirectTiles;
   if (L.direct) {
     L.block_at = L.turn_at = L.cut_at = L.part_at = L.bytes = 0;

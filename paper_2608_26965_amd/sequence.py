@@ -643,8 +643,9 @@ def _chunk(k_pages, v_pages, w, table, lens, starts, q, out, scale, k, v, slots)
 def cache_write(k, v, k_pages, v_pages, slots):
     """Writes the packed new keys and values k, v [T,Hk,d] (any strides) to their
     slots (int64 [T], as cache_grow gives them: page * its index + place in the
-    page); rows with a slot outside the pools are left out. k_pages, v_pages:
-    [pages, page, Hk, d], any strides. Returns nothing. Not recorded by autograd."""
+    page); rows with a slot outside the pools are left out, no two rows may have the
+    same one. k_pages, v_pages: [pages, page, Hk, d], any strides. Returns nothing. Not
+    recorded by autograd."""
     if torch.is_grad_enabled():
         _unrecorded((k, v), (k_pages, v_pages))
     _on(k, v, k_pages, v_pages, slots)

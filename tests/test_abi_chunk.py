@@ -149,6 +149,17 @@ def test_chunk_workspace_does_not_grow_with_the_table(kw):
     assert got[1] <= 2 * got[0] + (1 << 20) or got[1] < (1 << 29)
 
 
+def test_chunk_sinks_of_any_number_bound_the_tiles():
+    """A window of few keys beside sinks without end is as long as the table."""
+    L, lib = _lib()
+    got = []
+    for kw in (dict(), dict(left=100, sinks=2 ** 31 - 1), dict(left=100, sinks=2 ** 31 - 64), dict(left=100, sinks=1 << 24)):
+        n = ctypes.c_size_t(0)
+        assert lib.ca_paged_chunk_workspace_size(_chunk(max_pages=1 << 20, **kw), n) == L.CA_OK
+        got.append(n.value)
+    assert got[0] > 0 and got == got[:1] * 4
+
+
 def _args(requires_grad=False):
     import torch
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16, requires_grad=requires_grad)

@@ -878,3 +878,19 @@ def test_chunk_cut_blocks_may_be_written_over_their_queries(dt):
     a, _ = ca.paged_chunk_attn(w, q, kp, vp, table, n, starts)
     ca.paged_chunk_attn(w, q, kp, vp, table, n, starts, out=q)
     assert torch.equal(q, a)
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("H,Hk", [(200, 1), (300, 2), (257, 1)])
+def test_chunk_more_heads_than_a_block_has_rows(dt, H, Hk):
+    """A token's query heads fill a block and go on in the next one; alone, and cut into parts."""
+    _chunk_check(dt, [(40, 3), (7, 7), (300, 1)], H, Hk, 64, 16, seed=H, causal=True)
+    _divided(dt, [(4000, 2), (700, 9)], H, Hk, 64, 16, [(0, 0), (0, 127), (0, H - 1), (1, 64)], causal=True)
+
+
+@pytest.mark.parametrize("dt", DT)
+def test_chunk_sinks_without_end(dt):
+    """Windows beside sinks that reach beyond the last key."""
+    for sinks in (2 ** 31 - 1, 5000):
+        _chunk_check(dt, [(3000, 3), (90, 90), (1, 1)], 2, 1, 64, 16, left=5, sinks=sinks, causal=True)
+        _chunk_check(dt, [(300, 3), (90, 90)], 2, 1, 64, 16, left=5, right=2, sinks=sinks)
