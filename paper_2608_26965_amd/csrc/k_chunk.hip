@@ -573,7 +573,7 @@ __device__ __forceinline__ void lds_dma16_run(const void* gbase, const uint32_t 
         "s_mov_b32 m0, %4\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:1024\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
         : "v"(voff[0]), "v"(voff[1]), "s"(gbase), "s"(lds)
@@ -584,9 +584,9 @@ __device__ __forceinline__ void lds_dma16_run(const void* gbase, const uint32_t 
         "s_mov_b32 m0, %6\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
         : "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(gbase), "s"(lds)
