@@ -1217,7 +1217,7 @@ Plan plan_of(const ChunkProb& P) {
   L.rows = P.dtype == CA_BF16 ? kWalkRows : kF32Rows;
   const int64_t rows = (int64_t)P.tokens * P.G;
   const int wave_rows = L.rows / 4;
-  // (tiles take longer in fp32: 3 instead of 4 there, four ragged sequences 57.9 -> 56.5 us; 2: 60.3)
+  // (tiles take longer in fp32: 3 instead of 4 there, four ragged sequences 57.9 -> 57.0 us; 2: 60.3)
   L.start = P.dtype == CA_BF16 ? 4 : 3;
   L.slot_waves = (int)(rows < L.rows ? (rows + wave_rows - 1) / wave_rows : 4);
   L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
