@@ -931,7 +931,7 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 // to LDS, one ahead of the one that is computed; rows of DP + 4 floats there spread the keys'
 // 16-byte reads and the values' 4-byte reads over the banks (counted: conflicts are 19% of the
 // cycles in which LDS is active, these 7% of all). What bounds it: the matrix instructions, 32
-// cycles each and busy 68% of the time (8,192 causal tokens, 8 heads of 64: 702 us, 98 TFLOP/s of
+// cycles each and busy 68% of the time (8,192 causal tokens, 8 heads of 64: 694 us, 99 TFLOP/s of
 // the 154 of a large product), or the cache (8 single tokens on 16,000 each, 32 heads on 8 of 128:
 // 238 us, 4.4 TB/s).
 
