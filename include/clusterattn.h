@@ -567,10 +567,23 @@ typedef struct {
  * the pools, page * (its table entry) + place in the page, -1 where there is no
  * page and in rows from starts[batch] on. positions (device int32 [tokens]): the
  * token's place in its sequence (as ca_rope reads it), 0 in rows from
- * starts[batch] on. */
+ * starts[batch] on.
+ *
+ * Where state[2] > 0 a sequence has rows for the first of its new tokens only, or
+ * for none, and lens[b] counts tokens that are not written in this step:
+ * ca_paged_chunk_attn, whose rows are a sequence's last tokens, would take its rows
+ * for later ones and read places without a token. ca_cache_grow_seen also says how
+ * far the rows go, seen (device int32 [batch]): lens[b] less the new tokens of b that
+ * have no row (lens[b], as clamped, where all have one). Calls that take seen for
+ * lens are right whatever n_new was, and the tokens left out are the next step's
+ * first ones. */
 CA_API int ca_cache_grow(const ca_pages* p, const int32_t* lens, const int32_t* n_new,
                          int32_t* table, int32_t* free_pages, int32_t* state, int32_t* starts,
                          int64_t* slots, int32_t* positions, void* stream);
+CA_API int ca_cache_grow_seen(const ca_pages* p, const int32_t* lens, const int32_t* n_new,
+                              int32_t* table, int32_t* free_pages, int32_t* state,
+                              int32_t* starts, int64_t* slots, int32_t* positions, int32_t* seen,
+                              void* stream);
 
 /* Gives back the pages that hold no token which the next one of its sequence sees:
  * an entry i of row b keeps its page where a token j of its places (i * page <= j <

@@ -90,6 +90,19 @@ def cache_grow(table, free, lens, new, page, pages, tokens):
             slots[:tokens] + [-1] * rest, positions[:tokens] + [0] * rest)
 
 
+def lens_with_rows(lens, new, most, tokens):
+    """lens (cut to [0, most]) less the new tokens that have no row: the rows go to the first `tokens` new
+    tokens, by sequence and place."""
+    seen, row = [], 0
+    for n, m in zip(lens, new):
+        n = min(max(int(n), 0), most)
+        for j in range(n - min(max(int(m), 0), n), n):
+            n -= row >= tokens
+            row += 1
+        seen.append(n)
+    return seen
+
+
 def cache_release(table, free, lens, page, pages, left=-1, sinks=0):
     """Pages without a token that the sequence's next one sees go to free's end, the first of
     them last; their entries become -1."""

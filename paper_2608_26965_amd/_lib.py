@@ -34,6 +34,7 @@ EXPORTS = (
     "ca_paged_workspace_size",
     "ca_paged_attn",
     "ca_cache_grow",
+    "ca_cache_grow_seen",
     "ca_cache_release",
     "ca_cache_release_workspace_size",
     "ca_cache_write",
@@ -163,6 +164,7 @@ def load() -> ctypes.CDLL:
     lib.ca_paged_attn.argtypes = [ctypes.POINTER(CaPaged)] + [_vp] * 8 + [ctypes.c_size_t, _vp]
     pages, chunk = ctypes.POINTER(CaPages), ctypes.POINTER(CaChunk)
     lib.ca_cache_grow.argtypes = [pages] + [_vp] * 9
+    lib.ca_cache_grow_seen.argtypes = [pages] + [_vp] * 10
     lib.ca_cache_release.argtypes = [pages] + [_vp] * 5 + [ctypes.c_size_t, _vp]
     lib.ca_cache_release_workspace_size.argtypes = [pages, size]
     lib.ca_cache_write.argtypes = [chunk] + [_vp] * 6

@@ -366,6 +366,24 @@ int check_pages(const ca_pages* p, ca::PagesProb* P) {
 
 constexpr int kMostTokens = 1 << 24;
 
+int grow(const char* where, const ca_pages* p, const int32_t* lens, const int32_t* n_new,
+         int32_t* table, int32_t* free_pages, int32_t* state, int32_t* starts, int64_t* slots,
+         int32_t* positions, int32_t* seen, void* stream) {
+  ca::PagesProb P;
+  int s = check_pages(p, &P);
+  if (s) return s;
+  if (p->tokens < 1 || p->tokens > kMostTokens)
+    return fail(CA_E_INVALID, "tokens = %d must be in [1, 2^24]", p->tokens);
+  if (!lens || !n_new || !table || !free_pages || !state || !starts || !slots || !positions)
+    return fail(CA_E_INVALID, "lens, n_new, table, free_pages, state, starts, slots and positions are required");
+  P.lens = lens;
+  P.table = table;
+  P.free = free_pages;
+  P.state = state;
+  return device_status(
+      ca::launch_grow(P, n_new, starts, slots, positions, seen, (hipStream_t)stream), where);
+}
+
 int check_chunk(const ca_chunk* p, ca::ChunkProb* P) {
   if (!p) return fail(CA_E_INVALID, "chunk is NULL");
   int s;
@@ -947,19 +965,16 @@ int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages, const v
 int ca_cache_grow(const ca_pages* p, const int32_t* lens, const int32_t* n_new, int32_t* table,
                   int32_t* free_pages, int32_t* state, int32_t* starts, int64_t* slots,
                   int32_t* positions, void* stream) {
-  ca::PagesProb P;
-  int s = check_pages(p, &P);
-  if (s) return s;
-  if (p->tokens < 1 || p->tokens > kMostTokens)
-    return fail(CA_E_INVALID, "tokens = %d must be in [1, 2^24]", p->tokens);
-  if (!lens || !n_new || !table || !free_pages || !state || !starts || !slots || !positions)
-    return fail(CA_E_INVALID, "lens, n_new, table, free_pages, state, starts, slots and positions are required");
-  P.lens = lens;
-  P.table = table;
-  P.free = free_pages;
-  P.state = state;
-  return device_status(ca::launch_grow(P, n_new, starts, slots, positions, (hipStream_t)stream),
-                       "ca_cache_grow");
+  return grow("ca_cache_grow", p, lens, n_new, table, free_pages, state, starts, slots, positions,
+              nullptr, stream);
+}
+
+int ca_cache_grow_seen(const ca_pages* p, const int32_t* lens, const int32_t* n_new, int32_t* table,
+                       int32_t* free_pages, int32_t* state, int32_t* starts, int64_t* slots,
+                       int32_t* positions, int32_t* seen, void* stream) {
+  if (!seen) return fail(CA_E_INVALID, "seen is NULL");
+  return grow("ca_cache_grow_seen", p, lens, n_new, table, free_pages, state, starts, slots,
+              positions, seen, stream);
 }
 
 int ca_cache_release_workspace_size(const ca_pages* p, size_t* bytes) {

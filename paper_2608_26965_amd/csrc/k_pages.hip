@@ -73,7 +73,7 @@ __device__ __forceinline__ int find_in(const T* list, T i) {
 template <int N, bool SLOTS>
 __global__ __launch_bounds__(N) void grow_kernel(const PagesProb P, const int32_t* n_new,
                                                  int32_t* starts, int64_t* slots,
-                                                 int32_t* positions) {
+                                                 int32_t* positions, int32_t* seen) {
   constexpr int NW = N / 64, kItems = N > 256 ? 8 : 4;  // entries that a thread looks at in one go
   __shared__ int64_t first_item[N];  // entries of the sequences before
   __shared__ int64_t first_token[N];
@@ -96,7 +96,11 @@ __global__ __launch_bounds__(N) void grow_kernel(const PagesProb P, const int32_
     int64_t total, items;
     const int64_t before = tokens + scan_before<NW, int64_t>(n, sums, &total);
     const int64_t item0 = scan_before<NW, int64_t>(entries, sums, &items);
-    if (b < P.B) starts[b] = (int32_t)min(before, (int64_t)P.tokens);
+    if (b < P.B) {
+      starts[b] = (int32_t)min(before, (int64_t)P.tokens);
+      // (the first of its new tokens have the rows that there are)
+      if (seen) seen[b] = s_len[tid] - n + (int)min(max(P.tokens - before, (int64_t)0), (int64_t)n);
+    }
     first_item[tid] = item0;
     first_token[tid] = before;
     __syncthreads();
@@ -304,15 +308,15 @@ __global__ __launch_bounds__(256) void write_kernel(const WriteProb P, const T* 
 }  // namespace
 
 hipError_t launch_grow(const PagesProb& P, const int32_t* n_new, int32_t* starts, int64_t* slots,
-                       int32_t* positions, hipStream_t st) {
+                       int32_t* positions, int32_t* seen, hipStream_t st) {
   // Few sequences and tokens: four wavefronts, whose barriers and sums are quicker
   const bool few = P.B <= 256 && P.tokens <= kFewTokens;
   if (few)
     hipLaunchKernelGGL((grow_kernel<256, true>), dim3(1), dim3(256), 0, st, P, n_new, starts, slots,
-                       positions);
+                       positions, seen);
   else
     hipLaunchKernelGGL((grow_kernel<1024, false>), dim3(1), dim3(1024), 0, st, P, n_new, starts,
-                       slots, positions);
+                       slots, positions, seen);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || few) return e;
   hipLaunchKernelGGL(slots_kernel, dim3((P.tokens + 255) / 256), dim3(256), 0, st, P, n_new, starts,

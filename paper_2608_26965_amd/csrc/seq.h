@@ -161,7 +161,7 @@ struct PagesProb {
 };
 
 hipError_t launch_grow(const PagesProb& P, const int32_t* n_new, int32_t* starts, int64_t* slots,
-                       int32_t* positions, hipStream_t st);
+                       int32_t* positions, int32_t* seen, hipStream_t st);  // seen: may be NULL
 size_t release_bytes(const PagesProb& P);
 hipError_t launch_release(const PagesProb& P, char* ws, hipStream_t st);
 

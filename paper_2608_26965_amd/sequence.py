@@ -521,7 +521,7 @@ class CacheStep(NamedTuple):
 
 
 @_kept
-def _pages(page, free, state, table, lens, new, tokens, left, sinks, out):
+def _pages(page, free, state, table, lens, new, tokens, left, sinks, out, seen=None):
     """(descriptor, bytes of workspace) of a cache_grow (new given) or a
     cache_release."""
     if len(free[0]) != 1 or free[1][0] != 1:
@@ -539,6 +539,10 @@ def _pages(page, free, state, table, lens, new, tokens, left, sinks, out):
         _int32(new, "new", (batch,))
         if new[1][0] != 1 and batch > 1:
             raise ValueError("new must be contiguous")
+        if seen is not None:
+            _int32(seen, "seen", (batch,))
+            if seen[1][0] != 1 and batch > 1:
+                raise ValueError("seen must be contiguous")
         if out is not None:
             starts, slots, positions = out
             _int32(starts, "out.starts", (batch + 1,))
@@ -552,7 +556,7 @@ def _pages(page, free, state, table, lens, new, tokens, left, sinks, out):
     return c, _bytes("ca_cache_release_workspace_size", c) if new is None else 0
 
 
-def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, out=None) -> CacheStep:
+def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, seen=None, out=None) -> CacheStep:
     """Pages for the new tokens of a step, and where they go. page_table: int32
     [B, max_pages], changed in place; lens: int32 [B], the sequences' tokens, the
     new ones, the last new[b] of them (int32 [B]), included; tokens: rows of the
@@ -562,19 +566,32 @@ def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, out=None) -> Ca
     stay, their tokens have slot -1, and pool.state[1] says how many pages
     lacked. Repeating the call changes nothing. Returns CacheStep, in `out` (one
     of an earlier call of the same sizes) if given; rows behind the last sequence
-    have slot -1 and position 0."""
+    have slot -1 and position 0.
+
+    Where the sum of `new` may pass `tokens` (pool.state[2] says by how much), the last
+    sequences have rows for the first of their new tokens only, or none, and lens
+    counts tokens that this step does not write. seen (int32 [B], written if given)
+    then holds lens as far as the rows go: give it to paged_chunk_attn and cache_release
+    in the place of lens (with lens itself the attention would take the rows of the
+    sequence that is cut for its last tokens), and go on from it in the next step."""
     tokens = _int(tokens, "tokens", 1)
-    _on_ints(pool.free, pool.state, page_table, lens, new, *(out or ()))
+    if seen is not None and seen.data_ptr() in (lens.data_ptr(), new.data_ptr()):
+        raise ValueError("seen: expected a tensor of its own (lens and new are read after it is written)")
+    _on_ints(pool.free, pool.state, page_table, lens, new, *(out or ()), *(() if seen is None else (seen,)))
     c, _ = _pages(pool.page, _geo(pool.free), _geo(pool.state), _geo(page_table), _geo(lens), _geo(new),
-                  tokens, -1, 0, None if out is None else tuple(_geo(t) for t in out))
+                  tokens, -1, 0, None if out is None else tuple(_geo(t) for t in out),
+                  None if seen is None else _geo(seen))
     if out is None:
         out = CacheStep(lens.new_empty(lens.shape[0] + 1), lens.new_empty(tokens, dtype=torch.int64),
                         lens.new_empty((1, tokens)))
     starts, slots, positions = out
-    _call("ca_cache_grow", lens.device, c, lens.data_ptr(), new.data_ptr(), page_table.data_ptr(),
-          pool.free.data_ptr(), pool.state.data_ptr(), starts.data_ptr(), slots.data_ptr(),
-          positions.data_ptr())
-    _wrote(page_table, pool.state, starts, slots, positions)
+    args = (lens.device, c, lens.data_ptr(), new.data_ptr(), page_table.data_ptr(), pool.free.data_ptr(),
+            pool.state.data_ptr(), starts.data_ptr(), slots.data_ptr(), positions.data_ptr())
+    if seen is None:
+        _call("ca_cache_grow", *args)
+    else:
+        _call("ca_cache_grow_seen", *args, seen.data_ptr())
+    _wrote(page_table, pool.state, starts, slots, positions, seen)
     return CacheStep(starts, slots, positions)
 
 
