@@ -26,6 +26,7 @@ from dataclasses import dataclass
 from typing import NamedTuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import CA_BF16, CA_F32
@@ -66,17 +67,35 @@ def _on(like, *tensors):
             raise ValueError(f"expected all tensors on {like.device}, got one on {t.device}")
 
 
-def _unrecorded(read, written):
-    """Where autograd records, tells what the call does not do."""
-    for t in written:
-        if t is not None and t.requires_grad:
-            raise ValueError("the call would write a tensor that requires gradients, unrecorded by "
-                             "autograd: give it detached, or call under torch.no_grad()")
-    for t in read:
-        if t is not None and t.requires_grad:
-            warnings.warn("not recorded by autograd: no gradient reaches the inputs that require one "
-                          "(window_attn_backward and rope with inverse=True form them)", stacklevel=3)
-            return
+def _recording():
+    """Whether autograd records, backwards or forwards."""
+    return torch.is_grad_enabled() or forward_ad._current_level >= 0
+
+
+def _tangent(t):
+    return t is not None and forward_ad.unpack_dual(t).tangent is not None
+
+
+def _unrecorded(read, written, gradients=()):
+    """Where autograd records, tells what the call does not do. gradients: also read, by a call that
+    is a backward pass itself."""
+    if torch.is_grad_enabled():
+        for t in written:
+            if t is not None and t.requires_grad:
+                raise ValueError("the call would write a tensor that requires gradients, unrecorded by "
+                                 "autograd: give it detached, or call under torch.no_grad()")
+        for t in read:
+            if t is not None and t.requires_grad:
+                warnings.warn("not recorded by autograd: no gradient reaches the inputs that require one "
+                              "(window_attn_backward and rope with inverse=True form them)", stacklevel=3)
+                break
+    if forward_ad._current_level >= 0:
+        if any(map(_tangent, written)):
+            raise ValueError("the call would write a tensor that has a tangent, which it would leave as it "
+                             "is: give the tensor's primal")
+        if any(map(_tangent, (*read, *gradients))):
+            warnings.warn("not recorded by autograd: the tangents of the inputs do not reach the results",
+                          stacklevel=3)
 
 
 def _wrote(*tensors):
@@ -288,7 +307,7 @@ def rope(r: Rope, q, k=None, *, grid=None, start=None, positions=None, inverse=F
         raise ValueError("give either grid or positions")
     if k is None and k_out is not None:
         raise ValueError("k_out goes with k")
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((q, k), (q_out, k_out))
     _on(q, k, positions, q_out, k_out)
     c = _rope(r, _geo(q), None if k is None else _geo(k), None if q_out is None else _geo(q_out),
@@ -362,7 +381,7 @@ def window_attn(w: Window, q, k, v, *, scale=None, len_q=None, len_k=None, layou
     lengths in a padded batch. Returns (out, lse [B,H,nq] fp32 or None); rows
     that see no key, and rows past len_q, are 0 with lse -inf. Not recorded by
     autograd; window_attn_backward forms the gradients of out (lse has none)."""
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((q, k, v), (out,))
     _on(q, k, v, out, len_q, len_k)
     c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), None if out is None else _geo(out), _scale(scale),
@@ -385,8 +404,8 @@ def window_attn_backward(w: Window, dout, q, k, v, out, lse, *, scale=None, len_
     dq, dk, dv: outputs of the inputs' shapes (any strides, for example slices
     of a fused projection's gradient), new dense tensors by default."""
     given = dq, dk, dv
-    if torch.is_grad_enabled():
-        _unrecorded((), given)
+    if _recording():
+        _unrecorded((), given, (dout, q, k, v, out, lse))
     _on(q, k, v, out, lse, dout, len_q, len_k, dq, dk, dv)
     c, nbytes = _window(w, _geo(q), _geo(k), _geo(v), _geo(out), _scale(scale),
                         None if len_q is None else _geo(len_q),
@@ -441,7 +460,7 @@ def cache_append(k, v, k_pages, v_pages, page_table, lens):
     already). k_pages, v_pages: [pages, page, Hk, d], any strides;
     page_table: int32 [B, max_pages]; lens: int32 [B]. Returns nothing. Not
     recorded by autograd."""
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((k, v), (k_pages, v_pages))
     _on(k, v, k_pages, v_pages, page_table, lens)
     if k.dim() != 4:
@@ -463,7 +482,7 @@ def paged_attn(q, k_pages, v_pages, page_table, lens, *, left=-1, sinks=0, scale
     None); a sequence of no tokens gives 0 and -inf. The workspace goes with
     the table's width, not the lengths. Not recorded by autograd, and without a
     backward pass."""
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((q, k_pages, v_pages), (out,))
     _on(q, k_pages, v_pages, page_table, lens, out)
     if q.dim() != 3:
@@ -663,7 +682,7 @@ def cache_write(k, v, k_pages, v_pages, slots):
     page); rows with a slot outside the pools are left out, no two rows may have the
     same one. k_pages, v_pages: [pages, page, Hk, d], any strides. Returns nothing. Not
     recorded by autograd."""
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((k, v), (k_pages, v_pages))
     _on(k, v, k_pages, v_pages, slots)
     c, _ = _chunk(_geo(k_pages), _geo(v_pages), None, None, None, None, None, None, None, _geo(k), _geo(v),
@@ -685,7 +704,7 @@ def paged_chunk_attn(w: Window, q, k_pages, v_pages, page_table, lens, starts, *
     other. Returns (out [T,H,d], lse [T,H] fp32 or None); a query that sees no key has
     0 and -inf. Rows behind the last sequence are left as they were (in new
     tensors: as they come). Not recorded by autograd, and without a backward pass."""
-    if torch.is_grad_enabled():
+    if _recording():
         _unrecorded((q, k_pages, v_pages), (out, lse))
     _on(q, k_pages, v_pages, page_table, lens, starts, out, lse)
     if q.dim() != 3:
