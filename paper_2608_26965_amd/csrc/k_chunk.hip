@@ -37,6 +37,7 @@ constexpr int kXcdUnits = 32;    // compute units of an XCD
 constexpr int kMostHeld = 8 * kXcdUnits * 3;  // workgroups that run at a time, at most
 constexpr int kShareTiles = 4;   // tiles of a share, at least
 constexpr int kMostParts = 128;  // of a block, about
+constexpr int kStart = 4;        // what starting a block costs, in tiles
 constexpr int kJoinCost = 16;    // what cutting and joining costs
 constexpr int kSnap = 2;         // shares begin no nearer to a block's ends, in tiles
 constexpr int kMostRounds = 8;   // of whole blocks before the shares
@@ -84,7 +85,6 @@ struct Plan {
   int rows;        // of a block
   int slot_waves;  // wavefronts of a block that have rows, at most
   int blocks;      // at most, for one key head
-  int start;       // what starting a block costs, in tiles
   int direct;      // not planned: a workgroup takes one block, which it finds by itself
   size_t block_at, turn_at, cut_at, part_at, bytes;
 };
@@ -199,9 +199,9 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
         a = s_n[lo] - 1 - (i - first[lo]);
         const BlockSpan s(a, L.rows, P.G, s_lq[lo], s_lk[lo]);
         tiles = visible_tiles<KT>(P.m, s.p0, s.p1, s_lk[lo]).n;
-        longest = max(longest, tiles + L.start);
+        longest = max(longest, tiles + kStart);
       }
-      const int64_t c = cost + plan_scan(i < blocks ? tiles + L.start : 0, sums, &total);
+      const int64_t c = cost + plan_scan(i < blocks ? tiles + kStart : 0, sums, &total);
       if (i < blocks) {
         list[seen + i] = Block{b0 + lo, a, tiles, s_lq[lo], s_lk[lo], s_start[lo], c};
         if (((seen + i) & ((1 << step) - 1)) == 0) index[(seen + i) >> step] = c;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
   bool even = true;
   if (rounds < kMostRounds && (int64_t)(rounds + 1) * C.held <= count) {
     rest = all - cost_of((rounds + 1) * C.held);
-    if ((int64_t)(rounds + 1) * longest + quotient(rest, C.held) + L.start <= share + kJoinCost) {
+    if ((int64_t)(rounds + 1) * longest + quotient(rest, C.held) + kStart <= share + kJoinCost) {
       even = false;
       ++rounds;
       n = (int)max((int64_t)1, min((int64_t)n, min(rest / kShareTiles, quotient(kMostParts * rest, longest))));
@@ -305,9 +305,9 @@ __global__ __launch_bounds__(kPlan) void chunk_plan_kernel(const ChunkProb P, co
       }
       block = lo;
       const int64_t c = before_block(lo), e = before_block(lo + 1);
-      t = max(0, (int)(off - c) - L.start);
+      t = max(0, (int)(off - c) - kStart);
       if (t < kSnap) t = 0;
-      if (t > 0 && (int)(e - c) - L.start - t < kSnap) {  // at the next block's beginning instead
+      if (t > 0 && (int)(e - c) - kStart - t < kSnap) {  // at the next block's beginning instead
         t = 0;
         if (++block == seen) {
           block = 0;
@@ -1217,8 +1217,6 @@ Plan plan_of(const ChunkProb& P) {
   L.rows = P.dtype == CA_BF16 ? kWalkRows : kF32Rows;
   const int64_t rows = (int64_t)P.tokens * P.G;
   const int wave_rows = L.rows / 4;
-  // (tiles take longer in fp32: 3 instead of 4 there, four ragged sequences 57.9 -> 57.0 us; 2: 60.3)
-  L.start = P.dtype == CA_BF16 ? 4 : 3;
   L.slot_waves = (int)(rows < L.rows ? (rows + wave_rows - 1) / wave_rows : 4);
   L.blocks = (int)(rows / L.rows + (P.B < P.tokens ? P.B : P.tokens));
   const Classes C = Classes::of(P.Hk, per_unit(P));
