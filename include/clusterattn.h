@@ -392,7 +392,8 @@ CA_API int ca_attn_compensated_noalloc(const ca_problem* p, const void* qp, cons
  *   contiguous): each >= 0 and a multiple of 16 bytes' worth of elements, bases
  *   16-byte aligned. A stride of 0 repeats an input; rows of an output must not
  *   overlap (outputs with a stride of 0 over more than one row are refused),
- *   nor an output another tensor of the call, but for ca_rope in place.
+ *   nor an output another tensor of the call, but for ca_rope in place and
+ *   ca_paged_chunk_attn, whose out may be q (base and strides the same).
  * - Query head h of `heads` reads key head h / (heads / heads_k); heads_k
  *   divides heads.
  * - Head dimensions: bf16 64 or 128, fp32 any multiple of 4 up to 128 (rotary:
@@ -543,7 +544,10 @@ CA_API int ca_paged_attn(const ca_paged* p, const void* q, const void* k_pages,
  * device int32 free_pages[pages], the next page to be taken last. state: device
  * int32 [3]: the number of free pages; pages that the last ca_cache_grow lacked;
  * new tokens for which it had no rows. A free page must not stand twice in the
- * stack, nor in a table. */
+ * stack, nor in a table. A page may stand in several rows of the table (a common
+ * beginning) if it is full: ca_cache_grow leaves an entry that holds a page as it
+ * is, so sequences that go on inside a shared page would write over each other
+ * (copy such a page to one of its own first). */
 typedef struct {
   int32_t batch, page, pages, max_pages; /* as in ca_paged; max_pages * page < 2^30 */
   int32_t tokens;                        /* ca_cache_grow: rows of slots and positions, >= 1 */
@@ -592,7 +596,8 @@ CA_API int ca_cache_grow_seen(const ca_pages* p, const int32_t* lens, const int3
  * place, on top (what ca_cache_grow took goes back as it came), and become -1.
  * lens[b] = 0 gives back all of a finished sequence, a smaller length than before
  * the pages of rejected tokens, left and sinks those behind a window. A page that
- * stands in several rows (a common beginning) must not go back from two of them.
+ * stands in several rows (a common beginning) must not go back from two of them, nor
+ * from one while another holds it.
  * ws: workspace (ca_cache_release_workspace_size, 256-byte aligned). */
 CA_API int ca_cache_release(const ca_pages* p, const int32_t* lens, int32_t* table,
                             int32_t* free_pages, int32_t* state, void* ws, size_t ws_bytes,

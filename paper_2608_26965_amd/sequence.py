@@ -581,11 +581,12 @@ def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, seen=None, out=
     new ones, the last new[b] of them (int32 [B]), included; tokens: rows of the
     packed arrays, at least the sum of `new` (the program knows it, or a bound for
     arrays of a fixed size). Entries that a new token lies on and that hold no page
-    (-1, or any value outside the pool) get one; where the pool runs short they
-    stay, their tokens have slot -1, and pool.state[1] says how many pages
-    lacked. Repeating the call changes nothing. Returns CacheStep, in `out` (one
-    of an earlier call of the same sizes) if given; rows behind the last sequence
-    have slot -1 and position 0.
+    (-1, or any value outside the pool) get one; entries that hold one stay, so pages
+    that rows share (a common beginning) have to be full: sequences that go on inside
+    one would write over each other. Where the pool runs short the entries stay, their
+    tokens have slot -1, and pool.state[1] says how many pages lacked. Repeating the
+    call changes nothing. Returns CacheStep, in `out` (one of an earlier call of the
+    same sizes) if given; rows behind the last sequence have slot -1 and position 0.
 
     Where the sum of `new` may pass `tokens` (pool.state[2] says by how much), the last
     sequences have rows for the first of their new tokens only, or none, and lens
@@ -620,7 +621,8 @@ def cache_release(pool: PagePool, page_table, lens, *, left=-1, sinks=0, ws=None
     the first `sinks`): all of a finished sequence (lens 0), those of
     rejected tokens (lens less than it was), those behind a window. Their entries
     become -1. page_table: int32 [B, max_pages], changed in place. A page that
-    several rows share must not go back from two of them. Returns nothing."""
+    several rows share must not go back from two of them, nor from one while another
+    holds it. Returns nothing."""
     _on_ints(pool.free, pool.state, page_table, lens)
     c, nbytes = _pages(pool.page, _geo(pool.free), _geo(pool.state), _geo(page_table), _geo(lens), None,
                        0, int(left), int(sinks), None)
@@ -702,8 +704,8 @@ def paged_chunk_attn(w: Window, q, k_pages, v_pages, page_table, lens, starts, *
     divisor of H; page_table: int32 [B, max_pages]. Who sees whom is w, as in
     window_attn: Window(causal=True) for text, Window() where the new tokens see each
     other. Returns (out [T,H,d], lse [T,H] fp32 or None); a query that sees no key has
-    0 and -inf. Rows behind the last sequence are left as they were (in new
-    tensors: as they come). Not recorded by autograd, and without a backward pass."""
+    0 and -inf. Rows before the first and behind the last sequence are left as they were
+    (in new tensors: as they come). out may be q itself. Not recorded by autograd, and without a backward pass."""
     if _recording():
         _unrecorded((q, k_pages, v_pages), (out, lse))
     _on(q, k_pages, v_pages, page_table, lens, starts, out, lse)
