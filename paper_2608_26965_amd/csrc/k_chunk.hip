@@ -15,9 +15,9 @@
 //
 // What bounds it: the matrix cores for prompts (bf16, 8,192 tokens on 24,576, 32 heads on 8 of
 // 128: 3.33 to 3.52 ms, 1,090 to 1,160 TFLOP/s, four fifths of what a large matrix product reaches),
-// the cache for few new tokens (16 rows on 262,144, 16 heads of 64: 221 us, 4.9 TB/s), the three
-// launches for little of both (8 sequences, 5 tokens each on up to 16,000: 25 us, of which the
-// plan and the joining are 12).
+// the cache for few new tokens (16 rows on 262,144, 16 heads of 64: 222 us, 4.8 TB/s; a kernel that
+// only reads reaches 5.4 over 1 GiB), the three launches for little of both (8 sequences, 5 tokens
+// each on up to 16,000: 25 us, of which the plan and the joining are 12).
 #include <math.h>
 
 #include <algorithm>
@@ -37,7 +37,9 @@ constexpr int kXcdUnits = 32;    // compute units of an XCD
 constexpr int kMostHeld = 8 * kXcdUnits * 3;  // workgroups that run at a time, at most
 constexpr int kShareTiles = 4;   // tiles of a share, at least
 constexpr int kMostParts = 128;  // of a block, about
-constexpr int kStart = 4;        // what starting a block costs, in tiles
+// What starting a block costs, in tiles. (3 in fp32: four ragged sequences 55.2 instead of 56.0 us,
+// 24 of 4,565 tokens 56.9 instead of 52.1, one of 2,923 tokens 47.8 instead of 41.1.)
+constexpr int kStart = 4;
 constexpr int kJoinCost = 16;    // what cutting and joining costs
 constexpr int kSnap = 2;         // shares begin no nearer to a block's ends, in tiles
 constexpr int kMostRounds = 8;   // of whole blocks before the shares
@@ -102,7 +104,7 @@ struct BlockSpan {
 // The order in which a block walks its tiles: the sinks', then the window's. Where the window of
 // the sequence's last token begins inside this block's, from there to the last tile, and on from
 // the first: blocks beside each other, whose windows are shifted, then read the same keys at a
-// time (2 x 1,560 rows on windows of 4,679: 519 -> 509 us. Taken modulo the window's length
+// time (2 x 1,560 rows on windows of 4,679: 508 -> 503 us. Taken modulo the window's length
 // by blocks further from the last token too: 178 -> 183 us for windows of 1,023).
 struct BlockTiles {
   int ns, wrap, off, back;
@@ -830,7 +832,9 @@ __global__ __launch_bounds__(256, (D == 64 ? 3 : 2)) void chunk_bf16_kernel(
 
 // A workgroup joins the rows of one wavefront, lanes as they were in the attention. Of few
 // parts its wavefronts take a quarter of the chunks each, of many every fourth part, and the
-// quarters are workgroups of their own.
+// quarters are workgroups of their own. (The whole call, taken for few and for many: one block in
+// 8 parts 22.0 and 21.3 us, four ragged sequences in fp32 in up to 8 55.2 and 56.0; 13 parts 22.5 and
+// 21.8, 25 parts 24.9 and 21.7, 48 parts 30.4 and 23.0, 128 parts 60.5 and 40.7.)
 constexpr int kJoinGrid = 8192, kFewParts = 8;
 
 template <typename T, int D>
@@ -931,9 +935,9 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkProb P, cons
 // to LDS, one ahead of the one that is computed; rows of DP + 4 floats there spread the keys'
 // 16-byte reads and the values' 4-byte reads over the banks (counted: conflicts are 19% of the
 // cycles in which LDS is active, these 7% of all). What bounds it: the matrix instructions, 32
-// cycles each and busy 68% of the time (8,192 causal tokens, 8 heads of 64: 694 us, 99 TFLOP/s of
+// cycles each and busy 68% of the time (8,192 causal tokens, 8 heads of 64: 702 us, 98 TFLOP/s of
 // the 154 of a large product), or the cache (8 single tokens on 16,000 each, 32 heads on 8 of 128:
-// 238 us, 4.4 TB/s).
+// 237 us, 4.4 TB/s).
 
 // The largest x of lanes l, l ^ 16, l ^ 32 and l ^ 48
 __device__ __forceinline__ float max_of_groups(float x) {

@@ -6,14 +6,19 @@
 // 256 sequences of up to 32,768 tokens grow by a token and give pages back in 12 us
 // on the device, 64 that grow by up to 4,096 each in 18. The writes of keys and values are
 // bound by memory traffic, each read and written once (32,760 rows of 40 heads of 128: 246 us,
-// 5.4 TB/s).
+// 5.45 TB/s; a plain copy of 2 GiB reaches 6.3).
 #include "seq.h"
 
 namespace ca {
 
 namespace {
 
-constexpr int kFewTokens = 2048;  // whose slots the growing workgroup writes too
+// Steps of so few tokens and sequences: the growing workgroup, of four wavefronts, writes the
+// slots too. Growing and giving back on the device, against the larger workgroup and a launch
+// for the slots: 16 sequences, 64 tokens 9.2 and 13.9 us; 256 sequences, 2,048 tokens 13.0 and
+// 15.9, 4,096 tokens 19.4 and 17.4; 2,048 tokens of 700 sequences 16.7 and 17.6, of 2,000 30.9
+// and 27.3.
+constexpr int kFewTokens = 2048, kFewSequences = 256;
 
 // Sum of x over the threads before this one, and over all of them (NW wavefronts)
 template <int NW, typename T>
@@ -309,8 +314,7 @@ __global__ __launch_bounds__(256) void write_kernel(const WriteProb P, const T* 
 
 hipError_t launch_grow(const PagesProb& P, const int32_t* n_new, int32_t* starts, int64_t* slots,
                        int32_t* positions, int32_t* seen, hipStream_t st) {
-  // Few sequences and tokens: four wavefronts, whose barriers and sums are quicker
-  const bool few = P.B <= 256 && P.tokens <= kFewTokens;
+  const bool few = P.B <= kFewSequences && P.tokens <= kFewTokens;
   if (few)
     hipLaunchKernelGGL((grow_kernel<256, true>), dim3(1), dim3(256), 0, st, P, n_new, starts, slots,
                        positions, seen);

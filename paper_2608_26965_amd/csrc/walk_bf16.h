@@ -245,7 +245,7 @@ __device__ __forceinline__ void walk_bf16(Tiles& T, char* smem, int* redo,
     float p[8];
     // Products go before the other wavefront's exponentials, and every other tile before the
     // other wavefront's: of equal ones the older goes first, whose workgroup then ended 9% before
-    // the younger one of its compute unit (4% of the time)
+    // the younger one of its compute unit (8,192 tokens on 24,576: 3.48 -> 3.40 ms)
     if constexpr (Tiles::kBegun) __builtin_amdgcn_s_setprio(1 + PAR);
 #pragma unroll
     for (int n = 0; n < 4 * SV; ++n) {
