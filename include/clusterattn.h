@@ -564,7 +564,9 @@ typedef struct {
  * one: the first such entry, by sequence and place, the last of the stack, and so
  * on. Entries that hold one stay, so a call repeated changes nothing. Where the
  * stack runs short the later entries stay as they are and state[1] says how
- * many; it is 0 else.
+ * many; it is 0 else. Their tokens have no slot and are not written: for this step's
+ * attention they are not there, and a later step has to bring them again (a page
+ * found for them then holds nothing of theirs).
  *
  * starts[b] = the sum of n_new[0 .. b - 1], at most `tokens` (state[2] says how many
  * tokens are beyond). slots (device int64 [tokens]): the place of a row's token in

@@ -584,8 +584,9 @@ def cache_grow(pool: PagePool, page_table, lens, new, tokens, *, seen=None, out=
     (-1, or any value outside the pool) get one; entries that hold one stay, so pages
     that rows share (a common beginning) have to be full: sequences that go on inside
     one would write over each other. Where the pool runs short the entries stay, their
-    tokens have slot -1, and pool.state[1] says how many pages lacked. Repeating the
-    call changes nothing. Returns CacheStep, in `out` (one of an earlier call of the
+    tokens have slot -1, and pool.state[1] says how many pages lacked; those tokens are
+    not there for the step's attention, and a later step has to bring them again.
+    Repeating the call changes nothing. Returns CacheStep, in `out` (one of an earlier call of the
     same sizes) if given; rows behind the last sequence have slot -1 and position 0.
 
     Where the sum of `new` may pass `tokens` (pool.state[2] says by how much), the last
